@@ -1,0 +1,129 @@
+/*
+ * attnfuse_llm.h -- operators of language models around the attention of
+ * attnfuse.h, in the same library: the norm and rotation of queries and keys.
+ *
+ * The conventions of attnfuse.h hold (ownership, streams, RoPE tables, error
+ * codes, validation before any HIP call), with two additions:
+ *
+ * Strides.  Inputs that a program takes as slices of larger tensors have a
+ *           stride for each dimension but the last, in elements.  The last
+ *           dimension is contiguous, every stride is >= 0 and a multiple of 16
+ *           bytes, and every pointer 16-byte aligned.
+ * Positions and slots are read on the device and cannot be refused by the
+ *           call: each entry point says what one out of range does.
+ */
+#ifndef ATTNFUSE_LLM_H
+#define ATTNFUSE_LLM_H
+
+#include "attnfuse.h"
+
+#ifdef __cplusplus
+extern "C" {
+#endif
+
+/*
+ * Norm and rotation of every head's query and key rows in one pass.  For a row
+ * x of D values at position p:
+ *     y = q_weight o x / sqrt(mean(x^2) + eps)   (k_weight for keys)
+ *     out = R_p y                                (out = y for AF_ROPE_NONE)
+ * in fp32, rounded once.
+ *
+ *   Q [B,H,S,D], K [B,H_kv,S,D]   inputs (dtype), with strides
+ *   Qr, Kr                        outputs (dtype), contiguous; Qr may be Q and
+ *                                 Kr may be K where that is contiguous.  K and
+ *                                 Kr may both be NULL (H_kv is then ignored).
+ *   q_weight, k_weight            [D], of weight_dtype (AF_DTYPE_*), or NULL: 1
+ *   eps                           finite, >= 0
+ *   positions                     device int32 [B,S], contiguous, or NULL:
+ *                                 0..S-1.  A row whose position is not in [0,
+ *                                 rope_table_rows) comes out as NaN.  Not read
+ *                                 for AF_ROPE_NONE.
+ *   rope, rope_theta, rope_table, rope_table_rows   as attnfuse_fwd (rows >= S
+ *                                 without positions, >= 1 with them)
+ *   B, H, H_kv >= 1 and <= 16384, 1 <= S <= 2^20; D in {64, 128} (others:
+ *   UNSUPPORTED).  H need not be a multiple of H_kv.
+ */
+int attnfuse_qknorm_rope(const void* Q, const void* K, void* Qr, void* Kr, const void* q_weight, const void* k_weight,
+                         int weight_dtype, float eps,
+                         long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                         long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                         int B, int H, int H_kv, int S, int D, int dtype,
+                         int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                         const int* positions, void* stream);
+
+/* Bytes of workspace of attnfuse_qknorm_rope_bwd where a weight's gradient is
+ * wanted (the workgroups' partial sums, at most 1025 x D fp32).  H_kv = 0: no
+ * keys.  Returns 0 for invalid sizes. */
+size_t attnfuse_qknorm_rope_bwd_workspace_bytes(int B, int H, int H_kv, int S, int D, int dtype);
+
+/*
+ * Backward of attnfuse_qknorm_rope.  With r = (mean(x^2) + eps)^-1/2, xh = x r,
+ * dy = R_p^T dout and g = w o dy:
+ *     dx = r (g - xh mean(g o xh)),   dw = sum over all rows of dy o xh
+ * The sums of dw are fp32, in an order that the sizes alone fix, and rounded once.
+ *
+ *   Q, K, weights, eps, strides, positions, rope...   as the forward's
+ *   dQr, dKr            the gradients of its outputs (dtype), contiguous
+ *   dQ, dK              outputs (dtype), with strides (those of a dimension
+ *                       longer than 1 at least D); must not alias inputs
+ *   dq_weight, dk_weight  outputs [D] of weight_dtype, or both NULL: not wanted
+ *                       (with K = NULL dk_weight is ignored).  Also where the
+ *                       weights are NULL (1).
+ *   workspace           of at least attnfuse_qknorm_rope_bwd_workspace_bytes
+ *                       bytes, 16-byte aligned, where dq_weight is wanted
+ * A row whose position is out of range gives a NaN dx and makes dw NaN.
+ */
+int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, const void* dKr, void* dQ, void* dK,
+                             void* dq_weight, void* dk_weight, const void* q_weight, const void* k_weight,
+                             int weight_dtype, float eps,
+                             long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                             long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                             long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
+                             long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
+                             void* workspace, size_t workspace_bytes,
+                             int B, int H, int H_kv, int S, int D, int dtype,
+                             int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                             const int* positions, void* stream);
+
+/*
+ * The same for T new tokens whose keys and values go to a paged cache: Qr [T,H,
+ * D] gets the normed and rotated queries, the pages of K_pages the normed and
+ * rotated keys and those of V_pages the values as they are.
+ *
+ *   Q [T,H,D], K, V [T,H_kv,D]    inputs (dtype); strides per token and head
+ *   Qr [T,H,D]                    output (dtype), contiguous; must not alias
+ *   K_pages, V_pages              [num_pages, H_kv, page_size, D] (dtype), with
+ *                                 strides per page, head and place (those of a
+ *                                 dimension longer than 1 at least D)
+ *   page_size                     a power of two, 16 .. 2^20 (others:
+ *                                 UNSUPPORTED); num_pages * page_size < 2^31
+ *   slots                         device int64 [T]: page * page_size + place of
+ *                                 the token's key and value.  A slot outside
+ *                                 [0, num_pages * page_size) is not written (-1
+ *                                 for the padding of a batch).  No two tokens
+ *                                 of a call may have the same slot: which of
+ *                                 them is left there is then not defined.
+ *   positions                     device int32 [T]; needed (and read) with RoPE
+ *                                 only.  Out of range: as attnfuse_qknorm_rope
+ *                                 (the cached key is NaN too).
+ *   norm                          0: rotation alone (eps is ignored; weights
+ *                                 must be NULL), else as attnfuse_qknorm_rope
+ *   1 <= T <= 2^20; H, H_kv <= 16384.  Other slots of the pages are left as
+ *   they are.
+ */
+int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
+                                const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
+                                int norm, float eps,
+                                long long q_stride_t, long long q_stride_h, long long k_stride_t, long long k_stride_h,
+                                long long v_stride_t, long long v_stride_h,
+                                long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                                long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                                int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
+                                int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                                const int* positions, void* stream);
+
+#ifdef __cplusplus
+}
+#endif
+
+#endif /* ATTNFUSE_LLM_H */

@@ -39,6 +39,15 @@ SIGNATURES = {
     "attnfuse_version": (_I, []),
 }
 
+# Signatures of every symbol include/attnfuse_llm.h declares.
+LLM_SIGNATURES = {
+    "attnfuse_qknorm_rope": (_I, [_P] * 6 + [_I, _F] + [_L] * 6 + [_I] * 7 + [_F, _P, _I, _P, _P]),
+    "attnfuse_qknorm_rope_bwd_workspace_bytes": (ctypes.c_size_t, [_I] * 6),
+    "attnfuse_qknorm_rope_bwd": (_I, [_P] * 10 + [_I, _F] + [_L] * 12 + [_P, ctypes.c_size_t] + [_I] * 7
+                                 + [_F, _P, _I, _P, _P]),
+    "attnfuse_qknorm_rope_append": (_I, [_P] * 9 + [_I, _I, _F] + [_L] * 12 + [_I] * 8 + [_F, _P, _I, _P, _P]),
+}
+
 # Symbols of csrc/binding.h, which only this package calls.
 BINDING_SIGNATURES = {
     "af_fwd_workspace_bytes": (ctypes.c_size_t, [_I, _I, _I, _I, _I, _I, _I, _I, _I, _I, _I, _L]),
@@ -63,7 +72,7 @@ def load():
                 f"{LIB_PATH} is missing: build it with `python -m paper_2609_13612_amd.build` "
                 "(there is no non-HIP fallback)")
         lib = ctypes.CDLL(LIB_PATH)
-        for name, (res, args) in {**SIGNATURES, **BINDING_SIGNATURES}.items():
+        for name, (res, args) in {**SIGNATURES, **LLM_SIGNATURES, **BINDING_SIGNATURES}.items():
             fn = getattr(lib, name)
             fn.restype = res
             fn.argtypes = args

@@ -1,4 +1,4 @@
-"""Python binding of the C ABI in include/attnfuse.h -- argument marshalling only.
+"""Python binding of the C ABI in include/attnfuse.h and attnfuse_llm.h -- argument marshalling only.
 
 Each function takes torch tensors that already live on the GPU, checks their
 shape/dtype/contiguity against the call, passes raw device pointers and the
@@ -541,6 +541,158 @@ def attnfuse_rope_bwd(dqr, dkr=None, *, rope="neox", theta=10000.0, out_q=None, 
 
 def attnfuse_rope_table_bytes(rows, D):
     return _lib.load().attnfuse_rope_table_bytes(rows, D)
+
+
+# ---------------------------------------------------------------- include/attnfuse_llm.h
+def _rows(t, name, shape, dtype, device):
+    """The strides, in elements, of a tensor of rows that may lie apart: exactly that shape, type and device, each row
+    contiguous and 16-byte aligned.  A dimension of one row has stride 0."""
+    if not isinstance(t, torch.Tensor):
+        raise TypeError(f"{name} must be a torch tensor")
+    if t.device != device:
+        raise ValueError(f"{name} must be on {device} (it is on {t.device})")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} must be {dtype} (it is {t.dtype})")
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} must have shape {tuple(shape)} (it has {tuple(t.shape)})")
+    st = [s if n > 1 else 0 for s, n in zip(t.stride()[:-1], t.shape[:-1])]
+    if (t.stride(-1) != 1 and t.shape[-1] > 1) or t.data_ptr() % 16 or any(s * t.element_size() % 16 for s in st):
+        raise ValueError(f"{name} must have contiguous rows, each 16-byte aligned")
+    return st
+
+
+def _norm_weights(qw, kw, D, dtype, device):
+    """The library's code for the type of the norm weights: fp32 or the rows' own, the same for both."""
+    given = [w for w in (qw, kw) if w is not None]
+    if not given:
+        return DTYPE[torch.float32]
+    for w, name in ((qw, "q_weight"), (kw, "k_weight")):
+        if w is not None:
+            if isinstance(w, torch.Tensor) and w.dtype not in (torch.float32, dtype):
+                raise ValueError(f"{name} must be {torch.float32} or {dtype} (it is {w.dtype})")
+            _need(w, name, (D,), w.dtype if isinstance(w, torch.Tensor) else dtype, device)
+            if w.data_ptr() % 16:
+                raise ValueError(f"{name} must be 16-byte aligned")
+    if given[0].dtype != given[-1].dtype:
+        raise ValueError("q_weight and k_weight must have the same dtype")
+    return DTYPE[given[0].dtype]
+
+
+def _position_table(rope, theta, D, n, device, positions, shape, max_positions, rope_table):
+    """The table of a call whose rows are at `positions`, or at 0..n-1 without any."""
+    if positions is None or ROPE[rope] == ROPE["none"]:
+        return _table(rope, theta, D, n, device, rope_table)
+    _need(positions, "positions", shape, torch.int32, device)
+    if rope_table is None and max_positions is None:
+        raise ValueError("positions need max_positions (every position is below it) or rope_table")
+    return _table(rope, theta, D, 1 if max_positions is None else int(max_positions), device, rope_table)
+
+
+def _qknorm_shape(q, k):
+    dev = _device(q)
+    if q.dim() != 4 or (k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 4)):
+        raise ValueError("q must be [B, H, S, D] and k [B, H_kv, S, D]")
+    B, H, S, D = q.shape
+    Hkv = 0 if k is None else k.shape[1]
+    qs = _rows(q, "q", (B, H, S, D), q.dtype, dev)
+    ks = [0, 0, 0] if k is None else _rows(k, "k", (B, Hkv, S, D), q.dtype, dev)
+    return dev, (B, H, Hkv, S, D), qs, ks
+
+
+def attnfuse_qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0, positions=None,
+                         max_positions=None, out_q=None, out_k=None, rope_table=None):
+    """Qr, Kr: the rows of q and k over their root mean square, times the weights, rotated at their positions (0..S-1, or
+    ``positions`` int32 [B, S], all below ``max_positions``); see attnfuse_qknorm_rope in include/attnfuse_llm.h.  q and k
+    may be slices whose rows lie apart; Qr and Kr are contiguous."""
+    dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
+    wt = _norm_weights(q_weight, k_weight, D, q.dtype, dev)
+    out_q = _opt(out_q, "out_q", (B, H, S, D), q.dtype, dev)
+    if k is not None:
+        out_k = _opt(out_k, "out_k", (B, Hkv, S, D), q.dtype, dev)
+    elif out_k is not None or k_weight is not None:
+        raise ValueError("out_k and k_weight need k")
+    tp, tr = _tab(tab := _position_table(rope, theta, D, S, dev, positions, (B, S), max_positions, rope_table))
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_qknorm_rope(_ptr(q), _ptr(k), _ptr(out_q), _ptr(out_k), _ptr(q_weight), _ptr(k_weight), wt,
+                                                float(eps), *qs, *ks, B, H, Hkv, S, D, DTYPE[q.dtype], ROPE[rope],
+                                                float(theta), tp, tr, _ptr(positions), _stream())
+    _check(code, "attnfuse_qknorm_rope")
+    return out_q, out_k
+
+
+def attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, H_kv, S, D, dtype=torch.bfloat16):
+    return _lib.load().attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, H_kv, S, D, DTYPE[dtype])
+
+
+def attnfuse_qknorm_rope_bwd(q, k, dqr, dkr, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0,
+                             positions=None, max_positions=None, weight_grads=True, dq=None, dk=None, workspace=None,
+                             rope_table=None):
+    """dQ, dK, dq_weight, dk_weight of attnfuse_qknorm_rope (k and dkr None: of q alone; without ``weight_grads`` the last
+    two are None); see attnfuse_qknorm_rope_bwd.  dQ and dK lie in memory as q and k do, without gaps."""
+    dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
+    wt = _norm_weights(q_weight, k_weight, D, q.dtype, dev)
+    _need(dqr, "dqr", (B, H, S, D), q.dtype, dev)
+    dq = torch.empty_like(q) if dq is None else dq
+    dqs, dks, dwq, dwk, wbytes = _rows(dq, "dq", q.shape, q.dtype, dev), [0, 0, 0], None, None, 0
+    if k is not None:
+        _need(dkr, "dkr", (B, Hkv, S, D), q.dtype, dev)
+        dk = torch.empty_like(k) if dk is None else dk
+        dks = _rows(dk, "dk", k.shape, q.dtype, dev)
+    elif dkr is not None or dk is not None or k_weight is not None:
+        raise ValueError("dkr, dk and k_weight need k")
+    if weight_grads:
+        t = torch.float32 if wt else torch.bfloat16
+        dwq = torch.empty(D, device=dev, dtype=t)
+        dwk = None if k is None else torch.empty(D, device=dev, dtype=t)
+        workspace, wbytes = _workspace(workspace, attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, Hkv, S, D, q.dtype), dev)
+    tp, tr = _tab(tab := _position_table(rope, theta, D, S, dev, positions, (B, S), max_positions, rope_table))
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_qknorm_rope_bwd(
+            _ptr(q), _ptr(k), _ptr(dqr), _ptr(dkr), _ptr(dq), _ptr(dk), _ptr(dwq), _ptr(dwk), _ptr(q_weight), _ptr(k_weight),
+            wt, float(eps), *qs, *ks, *dqs, *dks, _ptr(workspace), wbytes, B, H, Hkv, S, D, DTYPE[q.dtype], ROPE[rope],
+            float(theta), tp, tr, _ptr(positions), _stream())
+    _check(code, "attnfuse_qknorm_rope_bwd")
+    return dq, dk, dwq, dwk
+
+
+def _pages(k_cache, v_cache, Hkv, D, dtype, device):
+    """(pages, page size, strides of both) of a paged cache [num_pages, H_kv, page_size, D]."""
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("the caches must be [num_pages, H_kv, page_size, D]")
+    shape = (k_cache.shape[0], Hkv, k_cache.shape[2], D)
+    return shape[0], shape[2], (_rows(k_cache, "k_cache", shape, dtype, device),
+                                _rows(v_cache, "v_cache", shape, dtype, device))
+
+
+def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weight=None, *, norm=True, eps=1e-6,
+                                rope="neox", theta=10000.0, positions=None, max_positions=None, out_q=None,
+                                rope_table=None):
+    """Qr [T, H, D]: the queries of T new tokens, normed (unless ``norm`` is False) and rotated at ``positions`` (int32
+    [T], all below ``max_positions``); their keys, likewise, and values are written to the pages [num_pages, H_kv,
+    page_size, D] at ``slots`` (int64 [T]: page * page_size + place; -1: nowhere); see attnfuse_qknorm_rope_append in
+    include/attnfuse_llm.h.  q, k, v and the pages may lie apart (a fused projection's slices, pages [num_pages, page_size,
+    H_kv, D] transposed)."""
+    dev = _device(q)
+    if q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("q must be [T, H, D] and k/v [T, H_kv, D]")
+    T, H, D = q.shape
+    Hkv = k.shape[1]
+    qs = _rows(q, "q", (T, H, D), q.dtype, dev)
+    ks, vs = _rows(k, "k", (T, Hkv, D), q.dtype, dev), _rows(v, "v", (T, Hkv, D), q.dtype, dev)
+    wt = _norm_weights(q_weight, k_weight, D, q.dtype, dev)
+    pages, page, (kps, vps) = _pages(k_cache, v_cache, Hkv, D, q.dtype, dev)
+    _need(slots, "slots", (T,), torch.int64, dev)
+    out_q = _opt(out_q, "out_q", (T, H, D), q.dtype, dev)
+    if ROPE[rope] != ROPE["none"] and positions is None:
+        raise ValueError("positions are needed with RoPE")
+    tp, tr = _tab(tab := _position_table(rope, theta, D, 1, dev, positions, (T,), max_positions, rope_table))
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_qknorm_rope_append(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(out_q), _ptr(k_cache), _ptr(v_cache), _ptr(slots), _ptr(q_weight), _ptr(k_weight),
+            wt, int(bool(norm)), float(eps), *qs, *ks, *vs, *kps, *vps, T, H, Hkv, D, pages, page, DTYPE[q.dtype],
+            ROPE[rope], float(theta), tp, tr, _ptr(positions), _stream())
+    _check(code, "attnfuse_qknorm_rope_append")
+    return out_q
 
 
 def attnfuse_strerror(code):

@@ -1,6 +1,6 @@
 """torch.autograd functions over the C ABI: the fused attention (and its
-block-sparse and bias / relu forms) as differentiable operations for training
-code.
+block-sparse and bias / relu forms) and the norm and rotation of queries and
+keys as differentiable operations for training code.
 
 ``attention`` runs attnfuse_fwd, keeps Q, K, V, O and the row statistic LSE
 (Section 4.4: the forward saves one scalar per row), and its backward runs
@@ -66,6 +66,31 @@ class _BiasNormAttention(torch.autograd.Function):
         q, k, v, o, lse, bias = ctx.saved_tensors
         dq, dk, dv = api.attnfuse_bwd_bias_norm(q, k, v, o, do.contiguous(), lse, bias=bias, **ctx.cfg)
         return dq, dk, dv, None, None, None, None, None, None, None
+
+
+class _QkNormRope(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, rope_table, eps, rope, theta, max_positions):
+        ctx.cfg = dict(eps=eps, rope=rope, theta=theta, max_positions=max_positions)
+        ctx.save_for_backward(q, k, q_weight, k_weight, positions, rope_table)
+        return api.attnfuse_qknorm_rope(q, k, q_weight, k_weight, positions=positions, rope_table=rope_table, **ctx.cfg)
+
+    @staticmethod
+    def backward(ctx, dqr, dkr):
+        q, k, qw, kw, positions, table = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        dq, dk, dqw, dkw = api.attnfuse_qknorm_rope_bwd(
+            q, k, dqr.contiguous(), None if k is None else dkr.contiguous(), qw, kw, positions=positions, rope_table=table,
+            weight_grads=want[2] or want[3], **ctx.cfg)
+        return dq, dk, dqw if want[2] else None, dkw if want[3] else None, None, None, None, None, None, None
+
+
+def qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0, positions=None,
+                max_positions=None, rope_table=None):
+    """Differentiable norm and rotation of query and key rows: (Qr, Kr), or Qr without k; gradients for q, k and the
+    weights.  Arguments as api.attnfuse_qknorm_rope."""
+    qr, kr = _QkNormRope.apply(q, k, q_weight, k_weight, positions, rope_table, eps, rope, theta, max_positions)
+    return qr if k is None else (qr, kr)
 
 
 def attention(q, k, v, *, rope="none", theta=10000.0, mask="causal", window=None, alibi_slopes=None, scale=None,

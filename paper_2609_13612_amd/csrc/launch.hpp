@@ -88,6 +88,32 @@ struct RopeParams {
   const float2* table;
 };
 
+// Norm and rotation of query and key rows (qknorm.hip).  Index 0 is q, 1 k, 2 v;
+// strides in elements: batch (of a cache: page), head, position.
+enum { QKNORM_FWD = 0, QKNORM_BWD = 1, QKNORM_APPEND = 2 };
+constexpr int QKNORM_HPT16 = 4, QKNORM_HPT32 = 2;   // heads a thread takes: bf16, fp32
+
+struct QkNormParams {
+  const void* x[3];       // inputs; rows at b xs[.][0] + h xs[.][1] + n xs[.][2]
+  void* y[3];             // outputs: forward [B, heads, S, D]; append q' [T, H, D], the key and value pages; backward dx
+  const void* dy[2];      // backward: the gradients of the outputs, [B, heads, S, D]
+  const void* w[2];       // weights [D], nullptr: 1
+  void* dw[2];            // backward: their gradients [D], of the weights' type
+  long long xs[3][3], ys[3][3];
+  int heads[2];           // H, H_kv (0: no k)
+  int B, S;               // append: 1, the tokens
+  bool w32, norm;         // weights are fp32; append: norm the rows
+  float eps;
+  const float2* table;    // [rows][D/2] (cos, sin)
+  int rows;
+  const int* positions;   // [B, S], nullptr: 0..S-1
+  const long long* slots; // append: [T]
+  long long nslots;       // append: pages * page size
+  int page_shift;
+  int wgs[2];             // backward: workgroups of q and of k
+  float* part;            // backward: [wgs[0] + wgs[1]][D], their sums of the weights' gradients (nullptr: none wanted)
+};
+
 // Waves per workgroup, four or eight, of a dense bf16 forward that has both
 // forms; rope: the rotation of its key tiles in the loop (ROPE_NONE where they
 // are copied to LDS as they are); bias: 0 without one, 1 where one row serves
@@ -110,6 +136,7 @@ int launch_decode(int D, int rope, bool alibi, const DecodeParams& p, hipStream_
 int launch_rope(bool fp32, int D, int rope, bool inverse, const RopeParams& p, hipStream_t st);
 // x0 (bf16) rotated into y0 (fp16); x1 unused.
 int launch_rope_f16(int D, int rope, const RopeParams& p, hipStream_t st);
+int launch_qknorm(int what, bool fp32, int D, int rope, const QkNormParams& p, hipStream_t st);
 int launch_rope_table(float2* table, int rows, int D, double theta, hipStream_t st);
 
 // Static device scratch of the decode entry point that allocates nothing: its
