@@ -1,6 +1,7 @@
 /*
  * attnfuse_llm.h -- operators of language models around the attention of
- * attnfuse.h, in the same library: the norm and rotation of queries and keys.
+ * attnfuse.h, in the same library: the norm and rotation of queries and keys,
+ * paged caches, and windows whose first tokens stay visible (sinks).
  *
  * The conventions of attnfuse.h hold (ownership, streams, RoPE tables, error
  * codes, validation before any HIP call), with two additions:
@@ -121,6 +122,75 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
                                 int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
                                 int rope, float rope_theta, const float* rope_table, int rope_table_rows,
                                 const int* positions, void* stream);
+
+/* Bytes of device workspace of attnfuse_decode_paged and attnfuse_decode_sinks:
+ * a partial (max, sum, accumulator) per (sequence, query head) and part of the
+ * visible cache.  S_kv is the most keys a sequence may have (max_pages *
+ * page_size); window 0 without one.  Returns 0
+ * for invalid sizes. */
+size_t attnfuse_decode_paged_workspace_bytes(int B, int H, int H_kv, int S_kv, int D, int window, int sinks);
+
+/*
+ * attnfuse_decode over a paged cache: one query per sequence, at position L - 1
+ * of its L = cache_lens[b] cached keys, which were rotated when they were
+ * written (attnfuse_qknorm_rope_append).  Key n of sequence b lies in page
+ * block_table[b][n / page_size] at place n % page_size.  Under SLIDING_WINDOW
+ * the query sees the last `window` keys and the first `sinks` keys.
+ *
+ *   Q [B,H,D]                     the newest token's queries (bf16)
+ *   K_pages, V_pages              [num_pages, H_kv, page_size, D] (bf16), with
+ *                                 strides per page, head and place (place: at
+ *                                 most 2^24)
+ *   block_table                   device int32 [B, max_pages], contiguous.  An
+ *                                 entry outside [0, num_pages) holds no keys:
+ *                                 they are not visible.  Entries behind a
+ *                                 sequence's length, or between its sinks and
+ *                                 its window, are not used.
+ *   page_size                     a power of two, 16 .. 2^20 (others:
+ *                                 UNSUPPORTED); max_pages * page_size <= 2^20
+ *   cache_lens                    device int32 [B] or NULL (every sequence has
+ *                                 max_pages * page_size keys); larger values are
+ *                                 clamped to that
+ *   O [B,H,D] (bf16), LSE [B,H] fp32; a sequence with no visible key gets O = 0,
+ *   LSE = -inf
+ *   workspace                     >= attnfuse_decode_paged_workspace_bytes(B, H,
+ *                                 H_kv, max_pages * page_size, D, window, sinks)
+ *   mask                          NONE, CAUSAL: every cached key; or
+ *                                 SLIDING_WINDOW with window >= 1
+ *   sinks                         >= 0; only with SLIDING_WINDOW, and without
+ *                                 ALiBi where > 0 (else AF_ERR_UNSUPPORTED)
+ *   rope, rope_theta, rope_table, alibi_slopes, softmax_scale   as
+ *                                 attnfuse_decode (rope_table_rows >= max_pages *
+ *                                 page_size).  The rotated query is not rounded
+ *                                 to fp16: keys may have any bf16 value, and the
+ *                                 LSE is that of the cached keys to 2^-16 of the
+ *                                 scores' magnitudes.
+ *   D in {64, 128}; any H a multiple of H_kv (a group of more than 32 query heads
+ *   reads the cache once for each 32)
+ *
+ * A sequence's result depends on its own keys and length only, not on the other
+ * sequences.  What lies in places that are not visible is never used, whatever
+ * it is.
+ */
+int attnfuse_decode_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table,
+                          const int* cache_lens, void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                          long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                          long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                          int B, int H, int H_kv, int D, int num_pages, int page_size, int max_pages,
+                          int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                          int mask, int window, int sinks,
+                          const float* alibi_slopes, float softmax_scale, void* stream);
+
+/*
+ * attnfuse_decode (a contiguous cache [B,H_kv,S_kv,D]) with sinks: the last
+ * `window` keys and the first `sinks` keys of each sequence are visible.
+ * window >= 1, sinks >= 1, bf16; arguments, results and workspace otherwise as
+ * attnfuse_decode_paged.
+ */
+int attnfuse_decode_sinks(const void* Q, const void* K, const void* V, const int* cache_lens, void* O, float* LSE,
+                          void* workspace, size_t workspace_bytes, int B, int H, int H_kv, int S_kv, int D,
+                          int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                          int window, int sinks, float softmax_scale, void* stream);
 
 #ifdef __cplusplus
 }

@@ -455,9 +455,14 @@ def _decode_args(q, k_cache, v_cache, cache_lens, out, lse):
 
 def attnfuse_decode(q, k_cache, v_cache, cache_lens=None, *, rope="none", theta=10000.0, mask="causal",
                     window=None, alibi_slopes=None, scale=None, out=None, lse=None, workspace=None,
-                    rope_table=None):
+                    rope_table=None, sinks=0):
     """O [B,H,D], LSE [B,H] of one query per sequence against a KV cache of
-    already-rotated keys; see attnfuse_decode in include/attnfuse.h."""
+    already-rotated keys; see attnfuse_decode in include/attnfuse.h, and for
+    ``sinks`` > 0 (first keys that stay visible under a sliding window)
+    attnfuse_decode_sinks in include/attnfuse_llm.h."""
+    if sinks:
+        return _decode_sinks(q, k_cache, v_cache, cache_lens, rope, theta, mask, window, alibi_slopes, scale, out, lse,
+                             workspace, rope_table, sinks)
     if _native is not None:
         r = _native.decode(q, k_cache, v_cache, cache_lens, out, lse, workspace, alibi_slopes, rope_table, _TABLES,
                            ROPE.get(rope, -1), theta, MASK.get(mask, -1), window, scale, 0)
@@ -693,6 +698,75 @@ def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None,
             ROPE[rope], float(theta), tp, tr, _ptr(positions), _stream())
     _check(code, "attnfuse_qknorm_rope_append")
     return out_q
+
+
+def attnfuse_decode_paged_workspace_bytes(B, H, H_kv, S_kv, D, window=0, sinks=0):
+    return _lib.load().attnfuse_decode_paged_workspace_bytes(B, H, H_kv, S_kv, D, window or 0, sinks)
+
+
+def _need_sinks(sinks, mask, window, alibi_slopes):
+    """Sinks belong to a sliding window, without ALiBi."""
+    if sinks < 0 or mask != "sliding_window" or not window or window < 1:
+        raise ValueError("sinks (>= 1) need mask='sliding_window' and a window")
+    if alibi_slopes is not None:
+        raise ValueError("sinks do not go with ALiBi slopes")
+
+
+def _decode_sinks(q, k_cache, v_cache, cache_lens, rope, theta, mask, window, alibi_slopes, scale, out, lse, workspace,
+                  rope_table, sinks):
+    _need_sinks(sinks, mask, window, alibi_slopes)
+    dev, (B, H, Hkv, S_kv, D), out, lse = _decode_args(q, k_cache, v_cache, cache_lens, out, lse)
+    if q.dtype != torch.bfloat16:
+        raise ValueError("decode with sinks takes bf16 tensors")
+    nbytes = attnfuse_decode_paged_workspace_bytes(B, H, Hkv, S_kv, D, window, sinks)
+    workspace, wbytes = _workspace(workspace, nbytes, dev)
+    r, th, _, w, sc = _variant(rope, theta, mask, window, None, scale, D)
+    tp, tr = _tab(tab := _table(rope, theta, D, S_kv, dev, rope_table))
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_decode_sinks(_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(cache_lens), _ptr(out),
+                                                 _ptr(lse), _ptr(workspace), wbytes, B, H, Hkv, S_kv, D, r, th, tp, tr, w,
+                                                 sinks, sc, _stream())
+    _check(code, "attnfuse_decode_sinks")
+    return out, lse
+
+
+def attnfuse_decode_paged(q, k_cache, v_cache, block_table, cache_lens=None, *, rope="none", theta=10000.0, mask="causal",
+                          window=None, sinks=0, alibi_slopes=None, scale=None, out=None, lse=None, workspace=None,
+                          rope_table=None):
+    """O [B,H,D], LSE [B,H] of one query per sequence against pages [num_pages, H_kv, page_size, D] of already-rotated
+    keys and their values, key n of sequence b in page ``block_table[b, n // page_size]`` (int32 [B, max_pages]); see
+    attnfuse_decode_paged in include/attnfuse_llm.h.  The pages may lie apart (pages [num_pages, page_size, H_kv, D]
+    transposed)."""
+    dev = _device(q)
+    if q.dim() != 3 or q.dtype != torch.bfloat16:
+        raise ValueError("q must be a bf16 tensor [B, H, D]")
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("the caches must be [num_pages, H_kv, page_size, D]")
+    B, H, D = q.shape
+    Hkv = k_cache.shape[1]
+    _need(q, "q", (B, H, D), q.dtype, dev)
+    pages, page, (kps, vps) = _pages(k_cache, v_cache, Hkv, D, q.dtype, dev)
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be an int32 tensor [B, max_pages]")
+    S = block_table.shape[1] * page
+    _need(block_table, "block_table", (B, block_table.shape[1]), torch.int32, dev)
+    if cache_lens is not None:
+        _need(cache_lens, "cache_lens", (B,), torch.int32, dev)
+    if sinks:
+        _need_sinks(sinks, mask, window, alibi_slopes)
+    out = _opt(out, "out", (B, H, D), q.dtype, dev)
+    lse = _opt(lse, "lse", (B, H), torch.float32, dev)
+    r, th, m, w, sc = _variant(rope, theta, mask, window, alibi_slopes, scale, D, H, dev)
+    nbytes = attnfuse_decode_paged_workspace_bytes(B, H, Hkv, S, D, w if m == MASK["sliding_window"] else 0, sinks)
+    workspace, wbytes = _workspace(workspace, nbytes, dev)
+    tp, tr = _tab(tab := _table(rope, theta, D, S, dev, rope_table))
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_decode_paged(
+            _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(cache_lens), _ptr(out), _ptr(lse),
+            _ptr(workspace), wbytes, *kps, *vps, B, H, Hkv, D, pages, page, block_table.shape[1], r, th, tp, tr, m, w, sinks,
+            _ptr(alibi_slopes), sc, _stream())
+    _check(code, "attnfuse_decode_paged")
+    return out, lse
 
 
 def attnfuse_strerror(code):

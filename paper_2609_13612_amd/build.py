@@ -31,7 +31,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", f"-I{INCLUDE}"
           "-Wall", "-Wno-unused-function"]
 
 SOURCES = ["api.cpp", "rope.hip", "fwd_bf16.hip", "fwd_prerot.hip", "fwd_norope.hip", "fwd_fp32.hip", "bwd_bf16.hip",
-           "bwd_dkdv.hip", "bwd_dkdv_split.hip", "bwd_fp32.hip", "decode.hip", "api_llm.cpp", "qknorm.hip"]
+           "bwd_dkdv.hip", "bwd_dkdv_split.hip", "bwd_fp32.hip", "decode.hip", "api_llm.cpp", "qknorm.hip",
+           "decode_paged.hip"]
 # Code-generation options of single translation units.  The dK/dV kernels
 # run faster when the machine scheduler keeps its first schedule instead of
 # re-scheduling high-register-pressure regions without memory-op clustering

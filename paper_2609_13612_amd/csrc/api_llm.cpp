@@ -72,6 +72,82 @@ bool qknorm_wgs(int B, int H, int H_kv, int S, int D, int dtype, int (&wgs)[2]) 
   return true;
 }
 
+// Page size -> shift, or -1 where the kernels have none.
+int page_shift_of(int page_size) {
+  for (int s = 4; s <= 20; ++s)
+    if ((1 << s) == page_size) return s;
+  return -1;
+}
+
+// ---------------------------------------------------------------- decode
+struct PagedLayout {
+  int hgroups, chunk, nsplit;
+  size_t ml, acc, total;
+};
+
+// Visible 32-key tiles per workgroup: a power of two from 4 (one for each of its
+// waves) that leaves at most about 1024 workgroups.
+PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int sinks) {
+  PagedLayout L{};
+  L.hgroups = (H / H_kv + 31) / 32;
+  long long tiles = (S + 31) / 32;
+  if (window > 0) {
+    const long long most = (window + 30LL) / 32 + 1 + (sinks + 31LL) / 32;   // a window's edges cut two tiles
+    tiles = tiles < most ? tiles : most;
+  }
+  const long long units = (long long)B * H_kv * L.hgroups;
+  L.chunk = 4;
+  while (L.chunk < tiles && units * ((tiles + L.chunk - 1) / L.chunk) > 1024) L.chunk *= 2;
+  L.nsplit = (int)((tiles + L.chunk - 1) / L.chunk);
+  const size_t parts = (size_t)B * H * L.nsplit;
+  L.ml = 0;
+  L.acc = align256(parts * 2 * sizeof(float));
+  L.total = L.acc + align256(parts * D * sizeof(float));
+  return L;
+}
+
+bool decode_sizes(int B, int H, int H_kv, int S, int D) {
+  return B >= 1 && H >= 1 && H_kv >= 1 && H % H_kv == 0 && S >= 1 && S <= kMaxS && D >= 2 && D % 2 == 0 &&
+         (long long)B * H * ((S + 63) / 64) < (1LL << 31);
+}
+
+// The checks and the launch that both decode calls share; p holds the cache.
+int decode_impl(af::PagedParams& p, const void* Q, const void* K, const void* V, const int* cache_lens, void* O, float* LSE,
+                void* workspace, size_t workspace_bytes, int B, int H, int H_kv, int S, int D, int rope, float rope_theta,
+                const float* rope_table, int rope_table_rows, int mask, int window, int sinks, const float* alibi_slopes,
+                float softmax_scale, void* stream) {
+  if (!Q || !K || !V || !O || !LSE || !workspace) return AF_ERR_INVALID_ARG;
+  for (const void* x : {Q, K, V, (const void*)O, (const void*)workspace})
+    if (!aligned16(x)) return AF_ERR_INVALID_ARG;
+  if (!aligned4(LSE) || !aligned4(cache_lens) || !aligned4(p.table) || !aligned4(alibi_slopes)) return AF_ERR_INVALID_ARG;
+  if (any_alias({O, LSE, workspace}, {Q, K, V, cache_lens, p.table, alibi_slopes}) || outs_alias({O, LSE, workspace}))
+    return AF_ERR_INVALID_ARG;
+  if (!decode_sizes(B, H, H_kv, S, D)) return AF_ERR_INVALID_ARG;
+  int rc = check_rope(rope, rope_theta);
+  if (rc != AF_OK || (rc = check_attn(mask, window, softmax_scale)) != AF_OK) return rc;
+  if (sinks < 0 || (sinks > 0 && mask != AF_MASK_SLIDING_WINDOW)) return AF_ERR_INVALID_ARG;
+  const void* outs[] = {O, LSE, workspace};
+  if ((rc = check_table(rope, rope_table, rope_table_rows, S, outs, 3)) != AF_OK) return rc;
+  if (mask != AF_MASK_SLIDING_WINDOW) window = 0;
+  window = window < S ? window : S;
+  sinks = sinks < S ? sinks : S;
+  const PagedLayout L = paged_layout(B, H, H_kv, S, D, window, sinks);
+  if (workspace_bytes < L.total) return AF_ERR_INVALID_ARG;
+  if (!supported_d(D) || (sinks > 0 && alibi_slopes)) return AF_ERR_UNSUPPORTED;
+
+  p.q = Q; p.k = K; p.v = V; p.lens = cache_lens;
+  p.o = O; p.lse = LSE;
+  p.part_ml = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.ml);
+  p.part_acc = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.acc);
+  p.B = B; p.H = H; p.Hkv = H_kv; p.S = S;
+  p.window = window; p.sinks = sinks;
+  p.chunk = L.chunk; p.nsplit = L.nsplit; p.hgroups = L.hgroups;
+  p.slopes = alibi_slopes;
+  p.scale = softmax_scale;
+  p.rope = reinterpret_cast<const float2*>(rope_table);
+  return map_launch(af::launch_decode_paged(D, rope, alibi_slopes != nullptr, p, static_cast<hipStream_t>(stream)));
+}
+
 }  // namespace
 
 extern "C" {
@@ -219,9 +295,8 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
   if (rope != AF_ROPE_NONE && !positions) return AF_ERR_INVALID_ARG;
   const void* outs[] = {Qr, K_pages, V_pages};
   if ((rc = check_table(rope, rope_table, rope_table_rows, 1, outs, 3)) != AF_OK) return rc;
-  int shift = 0;
-  while (shift < 20 && (1 << shift) < page_size) ++shift;
-  if (!supported_d(D) || page_size < 16 || (1 << shift) != page_size) return AF_ERR_UNSUPPORTED;
+  const int shift = page_shift_of(page_size);
+  if (!supported_d(D) || shift < 0) return AF_ERR_UNSUPPORTED;
 
   af::QkNormParams p{};
   p.x[0] = Q; p.x[1] = K; p.x[2] = V;
@@ -245,6 +320,50 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
   p.page_shift = shift;
   return map_launch(
       af::launch_qknorm(af::QKNORM_APPEND, dtype == AF_DTYPE_FP32, D, rope, p, static_cast<hipStream_t>(stream)));
+}
+
+size_t attnfuse_decode_paged_workspace_bytes(int B, int H, int H_kv, int S_kv, int D, int window, int sinks) {
+  if (!decode_sizes(B, H, H_kv, S_kv, D) || window < 0 || sinks < 0) return 0;
+  return paged_layout(B, H, H_kv, S_kv, D, window < S_kv ? window : S_kv, sinks < S_kv ? sinks : S_kv).total;
+}
+
+int attnfuse_decode_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table,
+                          const int* cache_lens, void* O, float* LSE, void* workspace, size_t workspace_bytes,
+                          long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                          long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                          int B, int H, int H_kv, int D, int num_pages, int page_size, int max_pages,
+                          int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                          int mask, int window, int sinks,
+                          const float* alibi_slopes, float softmax_scale, void* stream) {
+  if (!block_table || num_pages < 1 || page_size < 1 || max_pages < 1) return AF_ERR_INVALID_ARG;
+  if ((long long)max_pages * page_size > kMaxS) return AF_ERR_INVALID_ARG;
+  if (!strides_ok({{num_pages, kp_stride_p}, {H_kv, kp_stride_h}, {page_size, kp_stride_s}}, 0, AF_DTYPE_BF16, false) ||
+      !strides_ok({{num_pages, vp_stride_p}, {H_kv, vp_stride_h}, {page_size, vp_stride_s}}, 0, AF_DTYPE_BF16, false) ||
+      kp_stride_s > (1 << 24) || vp_stride_s > (1 << 24))
+    return AF_ERR_INVALID_ARG;
+  const int shift = page_shift_of(page_size);
+  if (shift < 0) return AF_ERR_UNSUPPORTED;
+  af::PagedParams p{};
+  p.table = block_table;
+  p.max_pages = max_pages; p.num_pages = num_pages; p.page_shift = shift;
+  p.ks[0] = kp_stride_p; p.ks[1] = kp_stride_h; p.ks[2] = kp_stride_s;
+  p.vs[0] = vp_stride_p; p.vs[1] = vp_stride_h; p.vs[2] = vp_stride_s;
+  return decode_impl(p, Q, K_pages, V_pages, cache_lens, O, LSE, workspace, workspace_bytes, B, H, H_kv,
+                     max_pages * page_size, D, rope, rope_theta, rope_table, rope_table_rows, mask, window, sinks,
+                     alibi_slopes, softmax_scale, stream);
+}
+
+int attnfuse_decode_sinks(const void* Q, const void* K, const void* V, const int* cache_lens, void* O, float* LSE,
+                          void* workspace, size_t workspace_bytes, int B, int H, int H_kv, int S_kv, int D,
+                          int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                          int window, int sinks, float softmax_scale, void* stream) {
+  if (sinks < 1) return AF_ERR_INVALID_ARG;
+  af::PagedParams p{};
+  p.ks[0] = p.vs[0] = (long long)H_kv * S_kv * D;
+  p.ks[1] = p.vs[1] = (long long)S_kv * D;
+  p.ks[2] = p.vs[2] = D;
+  return decode_impl(p, Q, K, V, cache_lens, O, LSE, workspace, workspace_bytes, B, H, H_kv, S_kv, D, rope, rope_theta,
+                     rope_table, rope_table_rows, AF_MASK_SLIDING_WINDOW, window, sinks, nullptr, softmax_scale, stream);
 }
 
 }  // extern "C"

@@ -1,0 +1,442 @@
+// Decode attention over a paged key/value cache, or a contiguous one under a
+// sliding window whose first tokens stay visible; bf16, fp32 accumulation.
+//
+// One query per sequence: with L cached keys it sits at position L - 1 and sees
+// the keys n < L of its window, n >= L - window, and the sinks, n < sinks.  Each
+// K and V element is used once per query head of its group, so the kernel is
+// bound by reading the visible part of the cache once.
+//
+// The visible 32-key tiles of a sequence are numbered from 0: first the tiles
+// that hold sinks, then those of the window.  Workgroup = 4 waves = `chunk` of
+// those tiles of one (sequence, K/V head, up to 32 query heads), the waves taking
+// tiles in turn; which tiles depends on the sequence's own length alone, so its
+// result does too.  The four waves' (max, sum, O) are joined through LDS and
+// leave as one partial per workgroup, or as the result where a sequence is
+// one workgroup's; a second kernel joins the partials.
+//
+// A tile is two units of 16 keys.  Pages hold a multiple of 16, so a unit lies in
+// one page and its address is wave-uniform: the page numbers are scalar loads,
+// two a tile, one tile ahead of the keys.
+//
+// Products: S^T = K Q'^T (32 keys x 32 columns, the group's heads repeated), K
+// straight from memory into registers as the A operand; O^T += V^T P^T, V
+// through the wave's own LDS tile for the transposed read.  Without RoPE the
+// bf16 query and keys meet exactly.  With it the query, rotated in fp32, is
+// split into two bf16 values, q = hi + lo to 2^-16 of itself, and meets the
+// cached keys in two products: the matrix units are idle nine tenths of the
+// time, and neither range nor the LSE suffers from a 16-bit query.  P is rounded to
+// bf16 (2^-8 of each weight at most, as the bf16 O is); sums, maxima and O stay
+// fp32 to the end.
+#include "common.hpp"
+#include "launch.hpp"
+
+namespace af {
+
+template <int D>
+struct PagedCfg {
+  static constexpr int NW = 4;
+  static constexpr int KS = D / 16;               // MFMA k-steps over the head dimension
+  static constexpr int MT = D / 32;               // 32-row output tiles over the head dimension
+  static constexpr int VP = D + 16;               // V tile pitch (transpose reads)
+  static constexpr int VT = 32 * VP;              // one wave's V tile (elements)
+  static constexpr int VPL = 32 * (D / 8) / 64;   // 16-byte V chunks per lane per tile
+  static constexpr int XCH = MT * (NW - 1) * 16 * 64 * 4;   // bytes of the waves' exchange of O: every tile but the own
+  static constexpr int SMEM = NW * VT * 2 > XCH ? NW * VT * 2 : XCH;
+};
+
+// The visible tiles of a sequence with L keys: tiles [0, ns), then [t0, t0 + n - ns).
+struct Visible {
+  int L, lo, sinks, ns, t0, n;
+  __device__ __forceinline__ Visible(const PagedParams& p, int b) {
+    L = p.lens ? min(p.lens[b], p.S) : p.S;
+    L = max(L, 0);
+    lo = p.window > 0 ? max(0, L - p.window) : 0;
+    sinks = min(p.sinks, lo);                     // (those still in the window are the window's)
+    t0 = lo >> 5;
+    ns = min((sinks + 31) >> 5, t0);
+    n = ns + ((L + 31) >> 5) - t0;
+  }
+  __device__ __forceinline__ int tile(int i) const { return i < ns ? i : t0 + i - ns; }
+  __device__ __forceinline__ bool key(int n_) const { return n_ < L && (n_ >= lo || n_ < sinks); }
+};
+
+template <int D, int ROPE, bool ALIBI, bool PAGED>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
+void paged_split_kernel(PagedParams p) {
+  using C = PagedCfg<D>;
+  constexpr int NQ = ROPE == ROPE_NONE ? 1 : 2;   // bf16 parts of the query
+  __shared__ __attribute__((aligned(16))) unsigned char smem[C::SMEM];
+  __shared__ float xml[2][C::NW][32];             // the waves' max and sum per column
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, lg = lane >> 5;
+  const int split = (int)(blockIdx.x % p.nsplit);
+  const int unit = (int)(blockIdx.x / p.nsplit);
+  const int hg = unit % p.hgroups, bg = unit / p.hgroups;
+  const int b = bg / p.Hkv, g = bg % p.Hkv;
+  const int G = p.H / p.Hkv, h0 = hg * 32, nh = min(32, G - h0);   // this workgroup's heads of the group
+  const Visible vis(p, b);
+  const int i_end = min((split + 1) * p.chunk, vis.n);
+  const int i_begin = split * p.chunk;
+  if (i_begin >= i_end) {                         // (workgroup-uniform)
+    if (p.nsplit == 1) {                          // an empty sequence: nothing else writes its rows
+      for (int j = tid; j < nh * (D / 8); j += 256)
+        st16(static_cast<uint16_t*>(p.o) + ((size_t)b * p.H + g * G + h0) * D + 8 * j, u32x4{0, 0, 0, 0});
+      if (tid < nh) p.lse[(size_t)b * p.H + g * G + h0 + tid] = -INFINITY;
+    }
+    return;
+  }
+  const int L = vis.L, pos = L - 1;
+
+  const int h = g * G + h0 + lq % nh;             // head of this lane's column
+  const float c2 = p.scale * kLog2e;
+  const float slope2 = ALIBI ? p.slopes[h] * kLog2e : 0.f;
+  const uint16_t* __restrict__ K = static_cast<const uint16_t*>(p.k) + g * p.ks[1];
+  const uint16_t* __restrict__ V = static_cast<const uint16_t*>(p.v) + g * p.vs[1];
+  const int* __restrict__ table = PAGED ? p.table + (size_t)b * p.max_pages : nullptr;
+
+  uint16_t* Vw = reinterpret_cast<uint16_t*>(smem) + wave * C::VT;
+  const int tr_key = 4 * lg + ((lane & 15) >> 2);
+  const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
+
+  f32x16 acc[C::MT];
+#pragma unroll
+  for (int i = 0; i < C::MT; ++i) acc[i] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f;
+
+  // The page of each unit of a tile (-1: none there, its keys are not visible).
+  auto pages_of = [&](int n0, int (&pg)[2]) {
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      if constexpr (PAGED) {
+        const int e = table[min((n0 + 16 * u) >> p.page_shift, p.max_pages - 1)];
+        pg[u] = (unsigned)e < (unsigned)p.num_pages ? e : -1;
+      } else {
+        pg[u] = b;
+      }
+    }
+  };
+  u32x4 kreg[C::KS], vreg[C::VPL];
+  // Rows that are not there (no page; past a contiguous cache) read another
+  // row's finite memory: page 0, or the last row.  Their keys are masked and
+  // their V rows cleared before use.
+  auto load_tile = [&](int n0, const int (&pg)[2]) {
+    const uint16_t* kb[2];
+    const uint16_t* vb[2];
+    int last[2];                                  // last row of the unit that may be read
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int n = n0 + 16 * u;
+      long long place;
+      if constexpr (PAGED) {
+        place = n & ((1 << p.page_shift) - 1);
+        last[u] = 15;
+      } else {
+        place = min(n, p.S - 1);
+        last[u] = max(0, min(15, p.S - 1 - n));
+      }
+      const long long page = max(pg[u], 0);
+      kb[u] = K + page * p.ks[0] + place * p.ks[2];
+      vb[u] = V + page * p.vs[0] + place * p.vs[2];
+    }
+    const int u = lq >> 4, r = min(lq & 15, u ? last[1] : last[0]);
+    const uint16_t* krow = (u ? kb[1] : kb[0]) + (long long)r * p.ks[2] + 8 * lg;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) kreg[s] = ld16(krow + 16 * s);
+#pragma unroll
+    for (int i = 0; i < C::VPL; ++i) {
+      constexpr int RPI = 512 / D;                // rows an instruction reads
+      const int vu = (i * RPI) >> 4;              // (an instruction stays inside a unit)
+      const int vr = min((i * RPI & 15) + lane / (D / 8), last[vu]);
+      vreg[i] = ld16(vb[vu] + (long long)vr * p.vs[2] + 8 * (lane % (D / 8)));
+    }
+  };
+
+  int i = i_begin + wave;
+  int pg[2] = {-1, -1}, pn[2] = {-1, -1};         // pages of the tile in flight, of the one after it
+  if (i < i_end) {
+    pages_of(32 * vis.tile(i), pg);
+    load_tile(32 * vis.tile(i), pg);
+    if (i + C::NW < i_end) pages_of(32 * vis.tile(i + C::NW), pn);
+  }
+
+  // Query operand (B of S^T = K Q'^T): lane holds column lq's head, dims 16s + 8lg .. +7.
+  u32x4 qreg[NQ][C::KS];
+  {
+    const uint16_t* Qh = static_cast<const uint16_t*>(p.q) + ((size_t)b * p.H + h) * D;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) qreg[0][s] = ld16(Qh + 16 * s + 8 * lg);
+    if constexpr (ROPE != ROPE_NONE) {
+      const float2* t = p.rope + (size_t)pos * (D / 2);
+      auto split2 = [&](int s, int w, float x0, float x1) {
+        const uint32_t hi = pack_bf16(x0, x1);
+        qreg[0][s][w] = hi;
+        qreg[1][s][w] = pack_bf16(x0 - bf_lo(hi), x1 - bf_hi(hi));
+      };
+      if constexpr (ROPE == ROPE_NEOX) {
+#pragma unroll
+        for (int s = 0; s < C::KS / 2; ++s) {
+          float4 cs[4];
+          load_cs(cs, t + 16 * s + 8 * lg);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float a0 = bf_lo(qreg[0][s][w]), a1 = bf_hi(qreg[0][s][w]);
+            float b0 = bf_lo(qreg[0][s + C::KS / 2][w]), b1 = bf_hi(qreg[0][s + C::KS / 2][w]);
+            rotate_pair<false>(a0, b0, cs[w].x, cs[w].y);
+            rotate_pair<false>(a1, b1, cs[w].z, cs[w].w);
+            split2(s, w, a0, a1);
+            split2(s + C::KS / 2, w, b0, b1);
+          }
+        }
+      } else {
+#pragma unroll
+        for (int s = 0; s < C::KS; ++s) {
+          float4 cs[2];
+          load_cs(cs, t + 8 * s + 4 * lg);
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            float x0 = bf_lo(qreg[0][s][w]), x1 = bf_hi(qreg[0][s][w]);
+            rotate_pair<false>(x0, x1, (w & 1) ? cs[w >> 1].z : cs[w >> 1].x, (w & 1) ? cs[w >> 1].w : cs[w >> 1].y);
+            split2(s, w, x0, x1);
+          }
+        }
+      }
+    }
+  }
+
+  for (; i < i_end; i += C::NW) {
+    const int n0 = 32 * vis.tile(i);
+    // some key of the tile is not visible: past the end, before the window, or without a page
+    const bool edge = n0 + 32 > L || (n0 < vis.lo && n0 + 32 > vis.sinks) || pg[0] < 0 || pg[1] < 0;   // (wave-uniform)
+    auto seen = [&](int r) { return vis.key(n0 + r) && (r < 16 ? pg[0] : pg[1]) >= 0; };
+    if (edge) {   // what lies in rows that are not visible may be anything: 0 x NaN is NaN
+#pragma unroll
+      for (int k = 0; k < C::VPL; ++k)
+        if (!seen(k * (512 / D) + lane / (D / 8))) vreg[k] = u32x4{0, 0, 0, 0};
+    }
+#pragma unroll
+    for (int k = 0; k < C::VPL; ++k)   // (this wave's earlier transpose reads are done: LDS is in order per wave)
+      *reinterpret_cast<u32x4*>(Vw + (k * (512 / D) + lane / (D / 8)) * C::VP + 8 * (lane % (D / 8))) = vreg[k];
+    f32x16 st = f32x16{};
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s)
+#pragma unroll
+      for (int q = 0; q < NQ; ++q) st = mfma32(kreg[s], qreg[q][s], st);
+    uint32_t hidden = 0;   // bit r: element r's key is not visible
+    if (edge) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) hidden |= (uint32_t)!seen(8 * (r >> 2) + 4 * lg + (r & 3)) << r;
+    }
+    if (i + C::NW < i_end) {
+      pg[0] = pn[0];
+      pg[1] = pn[1];
+      load_tile(32 * vis.tile(i + C::NW), pg);
+      if (i + 2 * C::NW < i_end) pages_of(32 * vis.tile(i + 2 * C::NW), pn);
+    }
+
+    // element r: key n0 + 8 (r/4) + 4 lg + r%4 of column lq
+    if constexpr (ALIBI) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r)
+        st[r] = __builtin_fmaf(st[r], c2, slope2 * (float)(n0 + 8 * (r >> 2) + 4 * lg + (r & 3) - pos));
+    }
+    if (edge) {
+#pragma unroll
+      for (int r = 0; r < 16; ++r) st[r] = (hidden >> r) & 1 ? -INFINITY : st[r];
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, st[r]);
+    mx = pair_max(mx);
+    if constexpr (!ALIBI) mx *= c2;
+    const float m_new = fmaxf(m_run, mx);
+    if (__any(m_new > m_run + 8.f)) {   // raise the reference max (wave-uniform)
+      const float alpha = (m_run == -INFINITY) ? 0.f : fast_exp2(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int k = 0; k < C::MT; ++k) acc[k] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = (m_run == -INFINITY) ? 0.f : m_run;
+    float pv[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      pv[r] = fast_exp2(ALIBI ? (st[r] - m_use) : __builtin_fmaf(st[r], c2, -m_use));
+      l_run += pv[r];
+    }
+    u32x4 pop[2];
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int w = 0; w < 4; ++w) pop[hf][w] = pack_bf16(pv[8 * hf + 2 * w], pv[8 * hf + 2 * w + 1]);
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int mt = 0; mt < C::MT; ++mt) {
+        const uint16_t* base = Vw + (16 * hf + tr_key) * C::VP + 32 * mt + tr_col;
+        const u32x2 lo2 = lds_read_tr16(base);
+        const u32x2 hi2 = lds_read_tr16(base + 8 * C::VP);
+        acc[mt] = mfma32(u32x4{lo2[0], lo2[1], hi2[0], hi2[1]}, pop[hf], acc[mt]);
+      }
+  }
+
+  // Join the waves: each scales its O to the common max and hands the 32-dim
+  // tiles of the other waves over; wave w sums tile w.
+  const float l_tot = pair_sum(l_run);
+  if (lg == 0) {
+    xml[0][wave][lq] = m_run;
+    xml[1][wave][lq] = l_tot;
+  }
+  __syncthreads();   // (and every wave is past its V tile: the exchange reuses it)
+  float M = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int w = 0; w < C::NW; ++w) M = fmaxf(M, xml[0][w][lq]);
+#pragma unroll
+  for (int w = 0; w < C::NW; ++w) {
+    const float m = xml[0][w][lq];
+    if (m != -INFINITY) l += xml[1][w][lq] * fast_exp2(m - M);
+  }
+  const float a = (m_run == -INFINITY) ? 0.f : fast_exp2(m_run - M);
+  float* xch = reinterpret_cast<float*>(smem) + lane;
+  auto slot = [&](int from, int mt) { return ((from * (C::MT - 1) + mt - (mt > from)) * 16) * 64; };
+#pragma unroll
+  for (int mt = 0; mt < C::MT; ++mt) {
+    acc[mt] *= a;
+    if (mt != wave || wave >= C::MT) {
+      // (waves past the tiles, at D = 64, hand over every tile: two slots each)
+      const int at = wave < C::MT ? slot(wave, mt) : ((C::MT * (C::MT - 1) + (wave - C::MT) * C::MT + mt) * 16) * 64;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) xch[at + r * 64] = acc[mt][r];
+    }
+  }
+  __syncthreads();
+  if (wave >= C::MT) return;
+  f32x16 o = f32x16{};
+#pragma unroll
+  for (int mt = 0; mt < C::MT; ++mt)
+    if (mt == wave) o = acc[mt];
+#pragma unroll
+  for (int w = 0; w < C::NW; ++w) {
+    if (w == wave) continue;
+    const int at = w < C::MT ? slot(w, wave) : ((C::MT * (C::MT - 1) + (w - C::MT) * C::MT + wave) * 16) * 64;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) o[r] += xch[at + r * 64];
+  }
+  if (lq >= nh) return;
+  const size_t bh = (size_t)b * p.H + h;
+  if (p.nsplit == 1) {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* O = static_cast<uint16_t*>(p.o) + bh * D + 32 * wave + 4 * lg;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<u32x2*>(O + 8 * q) = u32x2{pack_bf16(o[4 * q] * inv, o[4 * q + 1] * inv),
+                                                   pack_bf16(o[4 * q + 2] * inv, o[4 * q + 3] * inv)};
+    if (wave == 0 && lg == 0) p.lse[bh] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+  } else {
+    float* dst = p.part_acc + (bh * p.nsplit + split) * D + 32 * wave + 4 * lg;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<float4*>(dst + 8 * q) = float4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
+    if (wave == 0 && lg == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (bh * p.nsplit + split)) = float2{M, l};
+  }
+}
+
+// Join the partials of one (sequence, query head), none of an empty sequence: D /
+// 4 lanes hold the dims, the groups of lanes take every NG-th partial.
+template <int D>
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
+  constexpr int LPR = D / 4, NG = 256 / LPR;
+  __shared__ float4 red[NG][LPR];
+  __shared__ float wml[2][4];
+  const int t = threadIdx.x, c = t % LPR, grp = t / LPR;
+  const size_t bh = blockIdx.x;
+  const Visible vis(p, (int)(bh / p.H));
+  const int n = (vis.n + p.chunk - 1) / p.chunk;   // partials
+  uint16_t* O = static_cast<uint16_t*>(p.o) + bh * D + 4 * c;
+  const float* ml = p.part_ml + 2 * bh * p.nsplit;
+  const float* acc = p.part_acc + bh * p.nsplit * D + 4 * c;
+  float m = -INFINITY, l = 0.f;
+  for (int i = t; i < n; i += 256) {
+    const float2 v = *reinterpret_cast<const float2*>(ml + 2 * i);
+    const float M = fmaxf(m, v.x);
+    if (M != -INFINITY) {
+      l = l * fast_exp2(m - M) + v.y * fast_exp2(v.x - M);
+      m = M;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float m2 = __shfl_xor(m, o), l2 = __shfl_xor(l, o), M = fmaxf(m, m2);
+    if (M != -INFINITY) {
+      l = l * fast_exp2(m - M) + l2 * fast_exp2(m2 - M);
+      m = M;
+    }
+  }
+  if ((t & 63) == 0) {
+    wml[0][t >> 6] = m;
+    wml[1][t >> 6] = l;
+  }
+  __syncthreads();
+  float M = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) M = fmaxf(M, wml[0][w]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w)
+    if (wml[0][w] != -INFINITY) l += wml[1][w] * fast_exp2(wml[0][w] - M);
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+  for (int i = grp; i < n; i += NG) {
+    const float mi = ml[2 * i];
+    const float w = mi == -INFINITY ? 0.f : fast_exp2(mi - M);
+    const float4 x = *reinterpret_cast<const float4*>(acc + (size_t)i * D);
+    sum.x = __builtin_fmaf(w, x.x, sum.x);
+    sum.y = __builtin_fmaf(w, x.y, sum.y);
+    sum.z = __builtin_fmaf(w, x.z, sum.z);
+    sum.w = __builtin_fmaf(w, x.w, sum.w);
+  }
+  red[grp][c] = sum;
+  __syncthreads();
+  if (grp == 0) {
+#pragma unroll
+    for (int i = 1; i < NG; ++i) {
+      const float4 x = red[i][c];
+      sum.x += x.x;
+      sum.y += x.y;
+      sum.z += x.z;
+      sum.w += x.w;
+    }
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    *reinterpret_cast<u32x2*>(O) = u32x2{pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv)};
+    if (t == 0) p.lse[bh] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+  }
+}
+
+// ---------------------------------------------------------------- launch
+template <int D, int ROPE, bool ALIBI>
+static int launch_one(const PagedParams& p, hipStream_t st) {
+  const dim3 grid((unsigned)((long long)p.nsplit * p.hgroups * p.B * p.Hkv));
+  if (p.table) hipLaunchKernelGGL((paged_split_kernel<D, ROPE, ALIBI, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((paged_split_kernel<D, ROPE, ALIBI, false>), grid, dim3(256), 0, st, p);
+  if (p.nsplit > 1) hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)(p.B * p.H)), dim3(256), 0, st, p);
+  return hipGetLastError() == hipSuccess ? 0 : -3;
+}
+
+template <int D>
+static int dispatch_rope(int rope, bool alibi, const PagedParams& p, hipStream_t st) {
+  switch (rope) {
+    case ROPE_NONE: return alibi ? launch_one<D, ROPE_NONE, true>(p, st) : launch_one<D, ROPE_NONE, false>(p, st);
+    case ROPE_NEOX: return alibi ? launch_one<D, ROPE_NEOX, true>(p, st) : launch_one<D, ROPE_NEOX, false>(p, st);
+    case ROPE_INTERLEAVED:
+      return alibi ? launch_one<D, ROPE_INTERLEAVED, true>(p, st) : launch_one<D, ROPE_INTERLEAVED, false>(p, st);
+  }
+  return -2;
+}
+
+int launch_decode_paged(int D, int rope, bool alibi, const PagedParams& p, hipStream_t st) {
+  if (D == 64) return dispatch_rope<64>(rope, alibi, p, st);
+  if (D == 128) return dispatch_rope<128>(rope, alibi, p, st);
+  return -2;
+}
+
+}  // namespace af

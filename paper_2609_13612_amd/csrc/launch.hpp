@@ -114,6 +114,28 @@ struct QkNormParams {
   float* part;            // backward: [wgs[0] + wgs[1]][D], their sums of the weights' gradients (nullptr: none wanted)
 };
 
+// Decode over a paged cache, or over a contiguous one with sinks (decode_paged.hip).
+struct PagedParams {
+  const void* q;          // [B, H, D]
+  const void* k;          // pages, or the contiguous cache (a sequence is then a page of S keys)
+  const void* v;
+  long long ks[3], vs[3]; // their strides in elements: page, head, place
+  const int* table;       // [B, max_pages] page numbers, or nullptr: contiguous
+  int max_pages, num_pages, page_shift;
+  const int* lens;        // device [B] cache lengths, or nullptr (all S)
+  void* o;                // [B, H, D]
+  float* lse;             // [B, H]
+  float* part_ml;         // workspace [B, H, nsplit, 2]: partial max and sum (log2 units)
+  float* part_acc;        // workspace [B, H, nsplit, D]
+  int B, H, Hkv, S;       // S: the most keys a sequence may have
+  int window, sinks;      // window 0: every cached key; sinks: first keys that stay visible
+  int chunk, nsplit;      // visible 32-key tiles per workgroup; workgroups per sequence and head group
+  int hgroups;            // groups of up to 32 query heads of a K/V head
+  const float* slopes;
+  float scale;
+  const float2* rope;     // [rows >= S][D/2] (cos, sin)
+};
+
 // Waves per workgroup, four or eight, of a dense bf16 forward that has both
 // forms; rope: the rotation of its key tiles in the loop (ROPE_NONE where they
 // are copied to LDS as they are); bias: 0 without one, 1 where one row serves
@@ -136,6 +158,7 @@ int launch_decode(int D, int rope, bool alibi, const DecodeParams& p, hipStream_
 int launch_rope(bool fp32, int D, int rope, bool inverse, const RopeParams& p, hipStream_t st);
 // x0 (bf16) rotated into y0 (fp16); x1 unused.
 int launch_rope_f16(int D, int rope, const RopeParams& p, hipStream_t st);
+int launch_decode_paged(int D, int rope, bool alibi, const PagedParams& p, hipStream_t st);
 int launch_qknorm(int what, bool fp32, int D, int rope, const QkNormParams& p, hipStream_t st);
 int launch_rope_table(float2* table, int rows, int D, double theta, hipStream_t st);
 

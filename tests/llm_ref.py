@@ -65,3 +65,26 @@ def visible(S, window, sinks):
 
 def scale_of(D, scale):
     return 1.0 / math.sqrt(D) if scale is None else scale
+
+
+def decode(q, keys, values, seen, pos, *, rope="none", theta=10000.0, slopes=None, scale=None):
+    """One query of each head, q [H, D] at position pos, against the visible keys ``seen`` (their positions) of keys and
+    values [H_kv, n, D]: O [H, D], LSE [H], the sum of p |v|, and the largest scale sum |q' k| of a head (what the scores'
+    roundings are relative to)."""
+    H, D = q.shape
+    G = H // keys.shape[0]
+    o, lse, pv, mag = torch.zeros(H, D, dtype=torch.float64), torch.full((H,), -math.inf, dtype=torch.float64), None, None
+    pv, mag = torch.zeros_like(o), torch.zeros(H, dtype=torch.float64)
+    if len(seen) == 0:
+        return o, lse, pv, mag
+    qr = rotate(f64(q), torch.full((H,), pos), rope, theta)
+    for h in range(H):
+        k, v = f64(keys[h // G])[seen], f64(values[h // G])[seen]
+        s = scale_of(D, scale) * (k @ qr[h])
+        if slopes is not None:
+            s = s - float(slopes[h]) * (pos - seen.double())
+        lse[h] = torch.logsumexp(s, 0)
+        p = torch.softmax(s, 0)
+        o[h], pv[h] = p @ v, p @ v.abs()
+        mag[h] = scale_of(D, scale) * (k.abs() @ qr[h].abs()).max() + (0 if slopes is None else abs(float(slopes[h])) * pos)
+    return o, lse, pv, mag

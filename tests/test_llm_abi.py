@@ -83,8 +83,34 @@ APPEND_BAD = {
                   dict(page=8, rope=0, positions=None, table=None)],
 }
 
+PAGED = dict(Q=A, Kp=A + 0x1000, Vp=A + 0x2000, table=A + 0x3000, lens=A + 0x4000, O=A + 0x5000, LSE=A + 0x6000,
+             ws=A + 0x7000, wbytes=1 << 20, kpp=2 * 16 * D, kph=16 * D, kps=D, vpp=2 * 16 * D, vph=16 * D, vps=D, B=2, H=4,
+             H_kv=2, D=D, pages=8, page=16, max_pages=4, rope=1, theta=1e4, rtable=TABLE, rows=64, mask=1, window=0, sinks=0,
+             slopes=None, scale=0.125, stream=None)
+PAGED_BAD = {
+    INVALID: [dict(Q=None), dict(Kp=None), dict(Vp=None), dict(table=None), dict(O=None), dict(LSE=None), dict(ws=None),
+              dict(Kp=ODD), dict(table=A + 0x3002), dict(lens=A + 1), dict(LSE=A + 2), dict(wbytes=1023), dict(O=A),
+              dict(ws=A + 0x2000), dict(LSE=A + 0x4000), dict(ws=TABLE), dict(kps=D + 4), dict(vph=-8), dict(kps=1 << 25),
+              dict(B=0), dict(H=3), dict(H_kv=0), dict(pages=0), dict(page=0), dict(max_pages=0),
+              dict(max_pages=(1 << 16) + 1), dict(rows=63), dict(rtable=None), dict(theta=-1.0), dict(mask=3),
+              dict(mask=2), dict(mask=2, window=-1), dict(sinks=1), dict(sinks=-1, mask=2, window=4), dict(scale=0.0),
+              dict(scale=NAN), dict(rope=5)],
+    UNSUPPORTED: [dict(page=8), dict(page=48), dict(D=96), dict(mask=2, window=4, sinks=1, slopes=A + 0x8000),
+                  dict(D=96, lens=None, rope=0, rtable=None)],
+}
+STREAM = dict(Q=A, K=A + 0x1000, V=A + 0x2000, lens=A + 0x4000, O=A + 0x5000, LSE=A + 0x6000, ws=A + 0x7000, wbytes=1 << 20,
+              B=2, H=4, H_kv=2, S_kv=100, D=D, rope=1, theta=1e4, rtable=TABLE, rows=100, window=10, sinks=2, scale=0.125,
+              stream=None)
+STREAM_BAD = {
+    INVALID: [dict(Q=None), dict(K=ODD), dict(O=A + 0x1000), dict(ws=None), dict(wbytes=64), dict(S_kv=0),
+              dict(S_kv=(1 << 20) + 1), dict(window=0), dict(sinks=0), dict(sinks=-2), dict(rows=99), dict(scale=INF)],
+    UNSUPPORTED: [dict(D=96), dict(D=256, lens=None)],
+}
 
-@pytest.mark.parametrize("name,base,over,code", refusals("attnfuse_qknorm_rope", NORM, NORM_BAD)
+
+@pytest.mark.parametrize("name,base,over,code", refusals("attnfuse_decode_paged", PAGED, PAGED_BAD)
+                         + refusals("attnfuse_decode_sinks", STREAM, STREAM_BAD)
+                         + refusals("attnfuse_qknorm_rope", NORM, NORM_BAD)
                          + refusals("attnfuse_qknorm_rope_bwd", BWD, BWD_BAD)
                          + refusals("attnfuse_qknorm_rope_append", APPEND, APPEND_BAD))
 def test_refuses(name, base, over, code):
@@ -97,4 +123,15 @@ def test_qknorm_workspace_bytes():
     assert f(1, 32, 8, 8192, 128, 0) == 1024 * 128 * 4
     assert f(1, 1, 0, 1, 64, 1) == 64 * 4                     # no keys
     for bad in ((0, 1, 1, 1, 64, 0), (1, 1, 1, 0, 64, 0), (1, 1, 1, 1, 96, 0), (1, 1, 1, 1, 64, 2), (1, 1, -1, 1, 64, 0)):
+        assert f(*bad) == 0
+
+
+def test_decode_workspace_bytes():
+    f = _lib.load().attnfuse_decode_paged_workspace_bytes
+    assert f(1, 4, 2, 128, 64, 0, 0) == 256 + 4 * 64 * 4              # one part: four tiles
+    assert f(1, 4, 2, 129, 64, 0, 0) == 256 + 4 * 2 * 64 * 4          # two
+    assert f(1, 4, 2, 1 << 20, 64, 32, 4) == 256 + 4 * 64 * 4         # a window's two tiles and the sinks'
+    assert f(1, 4, 2, 1 << 20, 64, 97, 4) == 256 + 4 * 2 * 64 * 4
+    for bad in ((0, 4, 2, 128, 64, 0, 0), (1, 3, 2, 128, 64, 0, 0), (1, 4, 2, 0, 64, 0, 0), (1, 4, 2, 128, 64, -1, 0),
+                (1, 4, 2, 128, 64, 0, -1)):
         assert f(*bad) == 0
