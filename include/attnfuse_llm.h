@@ -123,6 +123,35 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
                                 int rope, float rope_theta, const float* rope_table, int rope_table_rows,
                                 const int* positions, void* stream);
 
+/*
+ * attnfuse_fwd under a sliding window whose first tokens stay visible: query i
+ * sees key j when j <= i and (j > i - window or j < sinks); positions (RoPE) are
+ * those in the sequence for sinks too.
+ *
+ *   window >= 1, sinks >= 1       any values; from window + sinks >= S on this is
+ *                                 the causal mask
+ *   workspace                     device memory (16-byte aligned) of at least
+ *                                 attnfuse_fwd_sinks_workspace_bytes bytes for
+ *                                 the rotated keys; 0 bytes, and it may be NULL,
+ *                                 without RoPE and for AF_DTYPE_FP32
+ *   other arguments and results as attnfuse_fwd; no ALiBi
+ */
+size_t attnfuse_fwd_sinks_workspace_bytes(int B, int H_kv, int S, int D, int dtype, int rope);
+int attnfuse_fwd_sinks(const void* Q, const void* K, const void* V, void* O, float* LSE, void* workspace,
+                       size_t workspace_bytes, int B, int H, int H_kv, int S, int D, int dtype,
+                       int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                       int window, int sinks, float softmax_scale, void* stream);
+
+/* Backward of attnfuse_fwd_sinks; workspace of attnfuse_bwd_sinks_workspace_bytes
+ * (0 for invalid sizes), of which the last part, as there, is not required;
+ * otherwise as attnfuse_bwd. */
+size_t attnfuse_bwd_sinks_workspace_bytes(int B, int H, int H_kv, int S, int D, int rope, int window, int sinks);
+int attnfuse_bwd_sinks(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,
+                       void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes,
+                       int B, int H, int H_kv, int S, int D, int dtype,
+                       int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                       int window, int sinks, float softmax_scale, void* stream);
+
 /* Bytes of device workspace of attnfuse_decode_paged and attnfuse_decode_sinks:
  * a partial (max, sum, accumulator) per (sequence, query head) and part of the
  * visible cache.  S_kv is the most keys a sequence may have (max_pages *

@@ -46,6 +46,10 @@ LLM_SIGNATURES = {
     "attnfuse_qknorm_rope_bwd": (_I, [_P] * 10 + [_I, _F] + [_L] * 12 + [_P, ctypes.c_size_t] + [_I] * 7
                                  + [_F, _P, _I, _P, _P]),
     "attnfuse_qknorm_rope_append": (_I, [_P] * 9 + [_I, _I, _F] + [_L] * 12 + [_I] * 8 + [_F, _P, _I, _P, _P]),
+    "attnfuse_fwd_sinks_workspace_bytes": (ctypes.c_size_t, [_I] * 6),
+    "attnfuse_fwd_sinks": (_I, [_P] * 6 + [ctypes.c_size_t] + [_I] * 7 + [_F, _P, _I, _I, _I, _F, _P]),
+    "attnfuse_bwd_sinks_workspace_bytes": (ctypes.c_size_t, [_I] * 8),
+    "attnfuse_bwd_sinks": (_I, [_P] * 10 + [ctypes.c_size_t] + [_I] * 7 + [_F, _P, _I, _I, _I, _F, _P]),
     "attnfuse_decode_paged_workspace_bytes": (ctypes.c_size_t, [_I] * 7),
     "attnfuse_decode_paged": (_I, [_P] * 8 + [ctypes.c_size_t] + [_L] * 6 + [_I] * 8 + [_F, _P, _I, _I, _I, _I, _P, _F,
                                                                                        _P]),

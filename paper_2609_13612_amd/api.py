@@ -212,8 +212,12 @@ def _fwd_scratch(q, B, H, Hkv, S, D, r, m, w, blocks=0, norm=0, extra=0):
 
 
 def attnfuse_fwd(q, k, v, *, rope="none", theta=10000.0, mask="causal", window=None,
-                 alibi_slopes=None, scale=None, out=None, lse=None, rope_table=None):
-    """O, LSE = attention(q, k, v); see attnfuse_fwd in include/attnfuse.h."""
+                 alibi_slopes=None, scale=None, out=None, lse=None, rope_table=None, sinks=0):
+    """O, LSE = attention(q, k, v); see attnfuse_fwd in include/attnfuse.h, and for
+    ``sinks`` > 0 (first keys that stay visible under a sliding window)
+    attnfuse_fwd_sinks in include/attnfuse_llm.h."""
+    if sinks:
+        return _fwd_sinks(q, k, v, rope, theta, mask, window, alibi_slopes, scale, out, lse, rope_table, sinks)
     if _native is not None:
         r = _native.fwd(q, k, v, out, lse, alibi_slopes, rope_table, _TABLES, ROPE.get(rope, -1), theta,
                         MASK.get(mask, -1), window, scale, 0, 0, 0, 0, 0, 0, 0, 0)
@@ -246,8 +250,12 @@ def attnfuse_bwd_workspace_bytes(B, H, H_kv, S, D, rope="none"):
 
 
 def attnfuse_bwd(q, k, v, o, do, lse, *, rope="none", theta=10000.0, mask="causal", window=None,
-                 alibi_slopes=None, scale=None, dq=None, dk=None, dv=None, workspace=None, rope_table=None):
-    """dQ, dK, dV of attnfuse_fwd; see attnfuse_bwd in include/attnfuse.h."""
+                 alibi_slopes=None, scale=None, dq=None, dk=None, dv=None, workspace=None, rope_table=None, sinks=0):
+    """dQ, dK, dV of attnfuse_fwd; see attnfuse_bwd in include/attnfuse.h (with
+    ``sinks`` attnfuse_bwd_sinks in include/attnfuse_llm.h)."""
+    if sinks:
+        return _bwd_sinks(q, k, v, o, do, lse, rope, theta, mask, window, alibi_slopes, scale, dq, dk, dv, workspace,
+                          rope_table, sinks)
     if _native is not None:
         r = _native.bwd(q, k, v, o, do, lse, dq, dk, dv, workspace, alibi_slopes, rope_table, _TABLES,
                         ROPE.get(rope, -1), theta, MASK.get(mask, -1), window, scale, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0, 0)
@@ -710,6 +718,45 @@ def _need_sinks(sinks, mask, window, alibi_slopes):
         raise ValueError("sinks (>= 1) need mask='sliding_window' and a window")
     if alibi_slopes is not None:
         raise ValueError("sinks do not go with ALiBi slopes")
+
+
+def _fwd_sinks(q, k, v, rope, theta, mask, window, alibi_slopes, scale, out, lse, rope_table, sinks):
+    _need_sinks(sinks, mask, window, alibi_slopes)
+    dev = _device(q)
+    B, H, Hkv, S, D = _shape(q, k)
+    _inputs(q, k, v, dev)
+    out = _opt(out, "out", q.shape, q.dtype, dev)
+    lse = _opt(lse, "lse", (B, H, S), torch.float32, dev)
+    r, th, _, w, sc = _variant(rope, theta, mask, window, None, scale, D)
+    tp, tr = _tab(tab := _table(rope, theta, D, S, dev, rope_table))
+    nbytes = _lib.load().attnfuse_fwd_sinks_workspace_bytes(B, Hkv, S, D, DTYPE[q.dtype], r)
+    ws = torch.empty(nbytes, device=dev, dtype=torch.uint8) if nbytes else None
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_fwd_sinks(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(ws), nbytes, B, H, Hkv, S,
+                                              D, DTYPE[q.dtype], r, th, tp, tr, w, int(sinks), sc, _stream())
+    _check(code, "attnfuse_fwd_sinks")
+    return out, lse
+
+
+def attnfuse_bwd_sinks_workspace_bytes(B, H, H_kv, S, D, rope, window, sinks):
+    return _lib.load().attnfuse_bwd_sinks_workspace_bytes(B, H, H_kv, S, D, ROPE[rope], window, sinks)
+
+
+def _bwd_sinks(q, k, v, o, do, lse, rope, theta, mask, window, alibi_slopes, scale, dq, dk, dv, workspace, rope_table, sinks):
+    _need_sinks(sinks, mask, window, alibi_slopes)
+    dev = _device(q)
+    B, H, Hkv, S, D = _shape(q, k)
+    _bwd_inputs(q, k, v, o, do, lse, dev, lse_needed=True)
+    dq, dk, dv = _grads(q, k, dq, dk, dv, dev)
+    r, th, _, w, sc = _variant(rope, theta, mask, window, None, scale, D)
+    workspace, wbytes = _workspace(workspace, attnfuse_bwd_sinks_workspace_bytes(B, H, Hkv, S, D, rope, w, sinks), dev)
+    tp, tr = _tab(tab := _table(rope, theta, D, S, dev, rope_table))
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_bwd_sinks(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(do), _ptr(lse), _ptr(dq), _ptr(dk),
+                                              _ptr(dv), _ptr(workspace), wbytes, B, H, Hkv, S, D, DTYPE[q.dtype], r, th, tp,
+                                              tr, w, int(sinks), sc, _stream())
+    _check(code, "attnfuse_bwd_sinks")
+    return dq, dk, dv
 
 
 def _decode_sinks(q, k_cache, v_cache, cache_lens, rope, theta, mask, window, alibi_slopes, scale, out, lse, workspace,

@@ -16,11 +16,11 @@ from . import api
 
 class _Attention(torch.autograd.Function):
     @staticmethod
-    def forward(ctx, q, k, v, alibi_slopes, rope, theta, mask, window, scale):
+    def forward(ctx, q, k, v, alibi_slopes, rope, theta, mask, window, scale, sinks):
         o, lse = api.attnfuse_fwd(q, k, v, rope=rope, theta=theta, mask=mask, window=window,
-                                  alibi_slopes=alibi_slopes, scale=scale)
+                                  alibi_slopes=alibi_slopes, scale=scale, sinks=sinks)
         ctx.save_for_backward(q, k, v, o, lse, alibi_slopes)
-        ctx.cfg = dict(rope=rope, theta=theta, mask=mask, window=window, scale=scale)
+        ctx.cfg = dict(rope=rope, theta=theta, mask=mask, window=window, scale=scale, sinks=sinks)
         ctx.mark_non_differentiable(lse)
         return o, lse
 
@@ -28,7 +28,7 @@ class _Attention(torch.autograd.Function):
     def backward(ctx, do, _dlse):
         q, k, v, o, lse, slopes = ctx.saved_tensors
         dq, dk, dv = api.attnfuse_bwd(q, k, v, o, do.contiguous(), lse, alibi_slopes=slopes, **ctx.cfg)
-        return dq, dk, dv, None, None, None, None, None, None
+        return dq, dk, dv, None, None, None, None, None, None, None
 
 
 class _BlockSparseAttention(torch.autograd.Function):
@@ -94,10 +94,10 @@ def qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox
 
 
 def attention(q, k, v, *, rope="none", theta=10000.0, mask="causal", window=None, alibi_slopes=None, scale=None,
-              return_lse=False):
+              return_lse=False, sinks=0):
     """Differentiable fused attention: O [B, H, S, D] (and the non-differentiable
     LSE [B, H, S] with ``return_lse``); arguments as api.attnfuse_fwd."""
-    o, lse = _Attention.apply(q, k, v, alibi_slopes, rope, theta, mask, window, scale)
+    o, lse = _Attention.apply(q, k, v, alibi_slopes, rope, theta, mask, window, scale, sinks)
     return (o, lse) if return_lse else o
 
 

@@ -1,9 +1,11 @@
-// C-ABI entry points (declared in include/attnfuse.h): argument validation
+// C-ABI entry points (declared in include/attnfuse.h, and the sinks' of
+// include/attnfuse_llm.h): argument validation
 // and dispatch to the kernel launchers.  Every argument is checked before the
 // first HIP call; no exception leaves this file.  Nothing here allocates,
 // synchronises or keeps state: the caller owns every buffer, the RoPE table
 // included.
 #include "attnfuse.h"
+#include "attnfuse_llm.h"
 
 #include <hip/hip_runtime.h>
 
@@ -143,6 +145,29 @@ int splits_that_fit(int n, const BwdWorkspace& w, size_t bytes, size_t kv_elems)
   return room < 2 ? 1 : room < (size_t)n ? (int)room : n;
 }
 
+// ---------------------------------------------------------------- sinks
+// A window and sinks that between them show every key up to the query: the causal mask.
+bool all_visible(int S, int window, int sinks) { return (long long)window + sinks >= S; }
+
+// The pass over the sinks' queries past the window: workgroups that share 32
+// sinks' (query head, 32-row query tile) steps, one for each CU, a wave of each
+// having two steps or more; and their fp32 partial dK' and dV.
+struct FarLayout {
+  int parts = 0;
+  size_t bytes = 0;
+};
+
+FarLayout far_layout(int B, int H, int H_kv, int S, int D, int window, int sinks) {
+  FarLayout f;
+  const long long blocks = (long long)B * H_kv * ((sinks + 31) / 32);
+  const long long steps = (long long)(H / H_kv) * ((S + 31) / 32 - window / 32);
+  long long n = 256 / blocks;
+  n = n < steps / 8 ? n : steps / 8;
+  f.parts = n < 1 ? 1 : (int)n;
+  f.bytes = align256((size_t)blocks * f.parts * 2 * 32 * D * sizeof(float));
+  return f;
+}
+
 // Decode workspace: per-wave partial (max, sum) pairs, then accumulators
 // (four phase-1 waves per chunk, each writing its own partial).
 struct DecodeLayout {
@@ -193,7 +218,8 @@ int check_ext(const Ext& e, const void* const* outs, int nouts) {
 int fwd_impl(const void* Q, const void* K, const void* V, void* O, float* LSE, const int* q_block_ptr,
              const int* k_block_idx, const Ext& ext, int B, int H, int H_kv, int S, int D, int dtype, int rope,
              float rope_theta, const float* rope_table, int rope_table_rows, int mask, int window,
-             const float* alibi_slopes, float softmax_scale, void* stream, void* k16 = nullptr, size_t k16_bytes = 0) {
+             const float* alibi_slopes, float softmax_scale, void* stream, void* k16 = nullptr, size_t k16_bytes = 0,
+             int sinks = 0) {
   const bool relu = ext.norm == AF_NORM_RELU;   // no row statistic: LSE may be NULL
   if (!Q || !K || !V || !O || (!LSE && !relu)) return AF_ERR_INVALID_ARG;
   if (!aligned16(Q) || !aligned16(K) || !aligned16(V) || !aligned16(O) || !aligned16(LSE)) return AF_ERR_INVALID_ARG;
@@ -212,8 +238,13 @@ int fwd_impl(const void* Q, const void* K, const void* V, void* O, float* LSE, c
   if (ext.kind() != af::EXT_NONE && (dtype == AF_DTYPE_FP32 || alibi_slopes || q_block_ptr))
     return AF_ERR_UNSUPPORTED;
 
+  if (sinks > 0 && all_visible(S, window, sinks)) {
+    mask = AF_MASK_CAUSAL;
+    sinks = 0;
+  }
   hipStream_t st = static_cast<hipStream_t>(stream);
   af::FwdParams p{};
+  p.sinks = sinks;
   p.q = Q; p.k = K; p.v = V; p.o = O; p.lse = LSE;
   p.B = B; p.H = H; p.Hkv = H_kv; p.S = S;
   // a window of S or more keys is the causal mask; clamping keeps n + window in int range
@@ -232,8 +263,9 @@ int fwd_impl(const void* Q, const void* K, const void* V, void* O, float* LSE, c
     if (!aligned16(k16) || dtype != AF_DTYPE_BF16 || rope == AF_ROPE_NONE) return AF_ERR_INVALID_ARG;
     if (k16_bytes < (size_t)B * H_kv * S * D * 2) return AF_ERR_INVALID_ARG;
     p.k16 = k16;
-    return map_launch(af::launch_fwd_prerot(D, rope, mask, alibi, ext.kind(), p, st));
+    if (sinks == 0) return map_launch(af::launch_fwd_prerot(D, rope, mask, alibi, ext.kind(), p, st));
   }
+  if (sinks > 0 && dtype == AF_DTYPE_BF16) return map_launch(af::launch_fwd_sinks(D, rope, p, st));
   if (dtype == AF_DTYPE_BF16) return map_launch(af::launch_fwd_bf16(D, rope, mask, alibi, ext.kind(), p, st));
   return map_launch(af::launch_fwd_fp32(D, rope, mask, alibi, p, st));
 }
@@ -249,7 +281,7 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
              void* dK, void* dV, const Sparse* sparse, const Ext& ext, void* workspace, size_t workspace_bytes,
              int B, int H, int H_kv, int S, int D, int dtype, int rope, float rope_theta, const float* rope_table,
              int rope_table_rows, int mask, int window, const float* alibi_slopes, float softmax_scale,
-             void* stream) {
+             void* stream, int sinks = 0) {
   const bool relu = ext.norm == AF_NORM_RELU;   // the LSE is not used: it may be NULL
   if (relu) LSE = nullptr;
   const void* ins[] = {Q, K, V, O, dO, LSE};
@@ -265,6 +297,13 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
   if (rc != AF_OK) return rc;
   if ((rc = check_attn(mask, window, softmax_scale)) != AF_OK) return rc;
   if ((rc = check_table(rope, rope_table, rope_table_rows, S, outs, 4)) != AF_OK) return rc;
+  if (sinks > 0 && all_visible(S, window, sinks)) {
+    mask = AF_MASK_CAUSAL;
+    sinks = 0;
+  }
+  const FarLayout far = sinks > 0 ? far_layout(B, H, H_kv, S, D, window, sinks) : FarLayout{};   // in front of the rest
+  if (workspace_bytes < far.bytes) return AF_ERR_INVALID_ARG;
+  workspace_bytes -= far.bytes;
   if (workspace_bytes < bwd_workspace(B, H, H_kv, S, D, rope).part) return AF_ERR_INVALID_ARG;
   if (!supported_d(D)) return AF_ERR_UNSUPPORTED;
   if (sparse && dtype == AF_DTYPE_FP32) return AF_ERR_UNSUPPORTED;        // block-sparse: bf16 kernels only
@@ -275,7 +314,10 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
   p.q = Q; p.k = K; p.v = V; p.o = O; p.dout = dO; p.lse = LSE;
   p.dq = dQ; p.dk = dK; p.dv = dV;
   const BwdWorkspace ws = bwd_workspace(B, H, H_kv, S, D, rope);
-  char* wb = static_cast<char*>(workspace);
+  char* wb = static_cast<char*>(workspace) + far.bytes;
+  p.sinks = sinks;
+  p.far = static_cast<float*>(workspace);
+  p.far_parts = far.parts;
   p.delta = reinterpret_cast<float*>(wb + ws.delta);
   p.lse2 = reinterpret_cast<float*>(wb + ws.lse2);
   p.do16 = wb + ws.do16;
@@ -304,6 +346,7 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
   p.bias = ext.bias;
   p.bias_sb = ext.sb; p.bias_sh = ext.sh; p.bias_sq = ext.sq;
   const bool alibi = alibi_slopes != nullptr;
+  if (sinks > 0 && dtype == AF_DTYPE_BF16) return map_launch(af::launch_bwd_sinks(D, rope, p, st));
   if (dtype == AF_DTYPE_FP32) return map_launch(af::launch_bwd_fp32(D, rope, mask, alibi, p, st));
   return map_launch(af::launch_bwd_bf16(D, rope, mask, alibi, ext.kind(), p, st));
 }
@@ -409,6 +452,43 @@ int attnfuse_fwd_blocksparse(const void* Q, const void* K, const void* V, void* 
   if (S < 1 || S > kMaxSparseS) return AF_ERR_INVALID_ARG;
   return fwd_impl(Q, K, V, O, LSE, q_block_ptr, k_block_idx, Ext{}, B, H, H_kv, S, D, dtype, rope, rope_theta,
                   rope_table, rope_table_rows, mask, window, alibi_slopes, softmax_scale, stream);
+}
+
+// ---------------------------------------------------------------- include/attnfuse_llm.h
+size_t attnfuse_fwd_sinks_workspace_bytes(int B, int H_kv, int S, int D, int dtype, int rope) {
+  if (B < 1 || H_kv < 1 || S < 1 || S > kMaxS || !supported_d(D) || dtype != AF_DTYPE_BF16 ||
+      (rope != AF_ROPE_NEOX && rope != AF_ROPE_INTERLEAVED))
+    return 0;
+  return (size_t)B * H_kv * S * D * 2;
+}
+
+int attnfuse_fwd_sinks(const void* Q, const void* K, const void* V, void* O, float* LSE, void* workspace,
+                       size_t workspace_bytes, int B, int H, int H_kv, int S, int D, int dtype,
+                       int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                       int window, int sinks, float softmax_scale, void* stream) {
+  if (sinks < 1) return AF_ERR_INVALID_ARG;
+  const bool rotated = dtype == AF_DTYPE_BF16 && rope != AF_ROPE_NONE;
+  if (rotated && !workspace) return AF_ERR_INVALID_ARG;
+  return fwd_impl(Q, K, V, O, LSE, nullptr, nullptr, Ext{}, B, H, H_kv, S, D, dtype, rope, rope_theta, rope_table,
+                  rope_table_rows, AF_MASK_SLIDING_WINDOW, window, nullptr, softmax_scale, stream,
+                  rotated ? workspace : nullptr, workspace_bytes, sinks);
+}
+
+size_t attnfuse_bwd_sinks_workspace_bytes(int B, int H, int H_kv, int S, int D, int rope, int window, int sinks) {
+  const size_t base = attnfuse_bwd_workspace_bytes(B, H, H_kv, S, D, rope);
+  if (base == 0 || window < 1 || sinks < 1) return 0;
+  return base + (all_visible(S, window, sinks) ? 0 : far_layout(B, H, H_kv, S, D, window, sinks).bytes);
+}
+
+int attnfuse_bwd_sinks(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,
+                       void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes,
+                       int B, int H, int H_kv, int S, int D, int dtype,
+                       int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                       int window, int sinks, float softmax_scale, void* stream) {
+  if (sinks < 1) return AF_ERR_INVALID_ARG;
+  return bwd_impl(Q, K, V, O, dO, LSE, dQ, dK, dV, nullptr, Ext{}, workspace, workspace_bytes, B, H, H_kv, S, D, dtype,
+                  rope, rope_theta, rope_table, rope_table_rows, AF_MASK_SLIDING_WINDOW, window, nullptr, softmax_scale,
+                  stream, sinks);
 }
 
 int attnfuse_fwd_bias_norm(const void* Q, const void* K, const void* V, void* O, float* LSE,

@@ -63,10 +63,13 @@ static int reduce(int rope, const BwdParams& p, hipStream_t st) {
   return hipGetLastError() == hipSuccess ? 0 : -3;
 }
 
+int launch_bwd_dkdv_reduce(int D, int rope, const BwdParams& p, hipStream_t st) {
+  return D == 64 ? reduce<64>(rope, p, st) : reduce<128>(rope, p, st);
+}
+
 int launch_bwd_dkdv_split(int D, int rope, int mask, bool alibi, int ext, const BwdParams& p, hipStream_t st) {
   const int rc = bwd_dispatch<DkdvPass<true>>(D, rope, mask, alibi, ext, p, st);
-  if (rc != 0) return rc;
-  return D == 64 ? reduce<64>(rope, p, st) : reduce<128>(rope, p, st);
+  return rc != 0 ? rc : launch_bwd_dkdv_reduce(D, rope, p, st);
 }
 
 }  // namespace af

@@ -46,9 +46,12 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dq_kernel(BwdParams p) {
   const float c2 = p.scale * kLog2e;
   const float slope2 = ALIBI ? p.slopes[h] * kLog2e : 0.f;
   const int W = p.window;
-  int t = wave, t_end = nqb;
+  int t = wave, t_end = nqb, t_begin = 0, ns = 0;   // as in the forward
   if constexpr (MASK != MASK_NONE) t_end = qb + 1;
-  if constexpr (MASK == MASK_SLIDING_WINDOW) t += max(0, m0 - W + 1) / F32_T;
+  if constexpr (windowed(MASK)) t_begin = max(0, m0 - W + 1) / F32_T;
+  if constexpr (MASK == MASK_SINKS) ns = min((p.sinks + F32_T - 1) / F32_T, t_begin);
+  const int n_tiles = ns + t_end - t_begin;
+  auto tile_at = [&](int i) { return i < ns ? i : t_begin + i - ns; };
 
   float k[DL], cs[DL], vv[DL];   // the tile in flight; rows past S: row S-1, masked
   auto load = [&](int tile) {
@@ -57,7 +60,7 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dq_kernel(BwdParams p) {
     f32_load_cs<D, ROPE>(cs, p.table + (size_t)n * (D / 2), g);
     f32_load_row<D>(vv, V + (size_t)n * D, g);
   };
-  if (t < t_end) load(t);
+  if (t < n_tiles) load(tile_at(t));
   float q[DL], dov[DL];
   f32_load_row<D>(q, static_cast<const float*>(p.q) + row, g);
   f32_load_row<D>(dov, static_cast<const float*>(p.dout) + row, g);
@@ -78,8 +81,8 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dq_kernel(BwdParams p) {
   f32x4 dq[MT];
 #pragma unroll
   for (int i = 0; i < MT; ++i) dq[i] = f32x4{};
-  for (; t < t_end; t += F32_NW) {
-    const int n0 = t * F32_T + 4 * g;     // key of element 0
+  for (; t < n_tiles; t += F32_NW) {
+    const int n0 = tile_at(t) * F32_T + 4 * g;   // key of element 0
     float kr[DL], v[DL], kt[DL];
 #pragma unroll
     for (int i = 0; i < DL; ++i) {
@@ -87,7 +90,7 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dq_kernel(BwdParams p) {
       v[i] = vv[i];
     }
     f32_rotate<D, ROPE>(kr, cs);
-    if (t + F32_NW < t_end) load(t + F32_NW);
+    if (t + F32_NW < n_tiles) load(tile_at(t + F32_NW));
     f32_transpose<D>(kt, kr, lds + wave * F32_T * (D + 4), lq, g);
     const f32x4 s = f32_dot<D>(kr, q), dp = f32_dot<D>(v, dov);
     float ds[4];
@@ -97,6 +100,7 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dq_kernel(BwdParams p) {
       bool ok = n < S;
       if constexpr (MASK != MASK_NONE) ok = ok && (n <= m);
       if constexpr (MASK == MASK_SLIDING_WINDOW) ok = ok && (n > m - W);
+      if constexpr (MASK == MASK_SINKS) ok = ok && (n > m - W || n < p.sinks);
       const float x = ALIBI ? __builtin_fmaf(s[r], c2, slope2 * (float)(n - m)) : s[r] * c2;
       ds[r] = ok ? exp2f(x - l2) * (dp[r] - dl) : 0.f;
     }
@@ -136,7 +140,8 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dkdv_kernel(BwdParams p)
   const int W = p.window;
   int tq = 0, tq_end = (S + F32_T - 1) / F32_T;
   if constexpr (MASK != MASK_NONE) tq = kb;
-  if constexpr (MASK == MASK_SLIDING_WINDOW) tq_end = min(tq_end, (min(n0 + F32_T, S) - 1 + W - 1) / F32_T + 1);
+  if constexpr (windowed(MASK))   // (a block with sinks is seen to the end)
+    if (MASK != MASK_SINKS || n0 >= p.sinks) tq_end = min(tq_end, (min(n0 + F32_T, S) - 1 + W - 1) / F32_T + 1);
   const int nt = tq_end - tq, items = G * nt;
 
   float q[DL], cs[DL], dor[DL], dot[DL], l4[4], d4[4];   // the tile in flight
@@ -194,6 +199,7 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dkdv_kernel(BwdParams p)
       bool ok = n < S && m < S;
       if constexpr (MASK != MASK_NONE) ok = ok && (n <= m);
       if constexpr (MASK == MASK_SLIDING_WINDOW) ok = ok && (n > m - W);
+      if constexpr (MASK == MASK_SINKS) ok = ok && (n > m - W || n < p.sinks);
       const float x = ALIBI ? __builtin_fmaf(s[r], c2, slope2 * (float)(n - m)) : s[r] * c2;
       pr[r] = ok ? exp2f(x - l2[r]) : 0.f;
       ds[r] = ok ? pr[r] * (dp[r] - dl[r]) : 0.f;
@@ -236,10 +242,11 @@ static int launch_one(const BwdParams& p, hipStream_t st) {
 
 template <int D, int ROPE>
 static int dispatch_mask(int mask, bool alibi, const BwdParams& p, hipStream_t st) {
-  switch (mask) {
+  switch (p.sinks > 0 ? (int)MASK_SINKS : mask) {
     case MASK_NONE: return alibi ? launch_one<D, ROPE, MASK_NONE, true>(p, st) : launch_one<D, ROPE, MASK_NONE, false>(p, st);
     case MASK_CAUSAL: return alibi ? launch_one<D, ROPE, MASK_CAUSAL, true>(p, st) : launch_one<D, ROPE, MASK_CAUSAL, false>(p, st);
     case MASK_SLIDING_WINDOW: return alibi ? launch_one<D, ROPE, MASK_SLIDING_WINDOW, true>(p, st) : launch_one<D, ROPE, MASK_SLIDING_WINDOW, false>(p, st);
+    case MASK_SINKS: return alibi ? -2 : launch_one<D, ROPE, MASK_SINKS, false>(p, st);
   }
   return -2;
 }

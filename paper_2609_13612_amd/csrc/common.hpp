@@ -28,7 +28,10 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
 enum RopeKind { ROPE_NONE = 0, ROPE_NEOX = 1, ROPE_INTERLEAVED = 2 };
-enum MaskKind { MASK_NONE = 0, MASK_CAUSAL = 1, MASK_SLIDING_WINDOW = 2 };
+// MASK_SINKS: a sliding window whose first `sinks` keys stay visible; entry points
+// take it as a window and a number of sinks.
+enum MaskKind { MASK_NONE = 0, MASK_CAUSAL = 1, MASK_SLIDING_WINDOW = 2, MASK_SINKS = 3 };
+constexpr bool windowed(int mask) { return mask == MASK_SLIDING_WINDOW || mask == MASK_SINKS; }
 
 // ---------------------------------------------------------------- bf16 <-> fp32
 __device__ __forceinline__ float bf_lo(uint32_t w) { return __uint_as_float(w << 16); }

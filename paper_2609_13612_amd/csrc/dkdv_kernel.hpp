@@ -181,7 +181,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
   const int ntq = (S + C::BQ - 1) / C::BQ;
   int tq_begin = 0, tq_end = ntq;
   if constexpr (MASK != MASK_NONE) tq_begin = nb / C::BQ;
-  if constexpr (MASK == MASK_SLIDING_WINDOW) tq_end = min(ntq, (min(nb + C::KEYS - 1, S - 1) + W - 1) / C::BQ + 1);
+  if constexpr (windowed(MASK)) tq_end = min(ntq, (min(nb + C::KEYS - 1, S - 1) + W - 1) / C::BQ + 1);
   // Query tiles by position: tq_begin + i, or under a block-sparse mask the
   // union of the active query blocks of the workgroup's two 64-key blocks
   // (the mask by key block), with a bit per key block saying which hold it.
@@ -277,12 +277,12 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
       bool visible = nw < S;
       if constexpr (SPARSE) visible = visible && ((tl.rows[s % nq] >> jw) & 1);
       if constexpr (MASK != MASK_NONE) visible = visible && (mq + 31 >= nw);
-      if constexpr (MASK == MASK_SLIDING_WINDOW) visible = visible && (mq <= nw + 31 + W - 1);
+      if constexpr (windowed(MASK)) visible = visible && (mq <= nw + 31 + W - 1);
       if (visible) {
         bool need_mask = nw + 32 > S;
         if constexpr (RELU) need_mask = need_mask || (mq + 32 > S);   // no LSE zeroes the rows past S
         if constexpr (MASK != MASK_NONE) need_mask = need_mask || (mq < nw + 31);
-        if constexpr (MASK == MASK_SLIDING_WINDOW) need_mask = need_mask || (mq + 31 - W >= nw);
+        if constexpr (windowed(MASK)) need_mask = need_mask || (mq + 31 - W >= nw);
         // S = Q' K'^T and dP = dO V^T for 32 queries (rows) x this wave's 32 keys
         // (columns); the two MFMA chains are interleaved.
         f32x16 sc = f32x16{}, dp = f32x16{};
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
             bool ok = n < S;
             if constexpr (RELU) ok = ok && (m < S);
             if constexpr (MASK != MASK_NONE) ok = ok && (n <= m);
-            if constexpr (MASK == MASK_SLIDING_WINDOW) ok = ok && (n > m - W);
+            if constexpr (windowed(MASK)) ok = ok && (n > m - W);
             pr[r] = ok ? pr[r] : 0.f;
             if constexpr (RELU) ds[r] = ok ? ds[r] : 0.f;
           }
@@ -417,6 +417,24 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
   if (qh == 1) add(dv);
   __syncthreads();   // the exchange memory is free again: each wave's output rows go through it
 
+  if constexpr (MASK == MASK_SINKS) {   // this pass is the window's; the sinks' other queries (bwd_sinks.hip)
+    if (sp == 0 && nw < p.sinks) {        // (wave-uniform)
+      const int nfb = (p.sinks + 31) / 32;
+      const float* src = p.far + ((((size_t)bg * nfb + nw / 32) * p.far_parts * 2 + qh) * 32 + lq) * D + 4 * lg;
+      for (int j = 0; j < p.far_parts; ++j, src += (size_t)2 * 32 * D)
+#pragma unroll
+        for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+          for (int a = 0; a < 4; ++a) {
+            const float4 x = *reinterpret_cast<const float4*>(src + 32 * mt + 8 * a);
+            f32x16& y = (qh == 0) ? dk[mt] : dv[mt];
+            y[4 * a] += x.x;
+            y[4 * a + 1] += x.y;
+            y[4 * a + 2] += x.z;
+            y[4 * a + 3] += x.w;
+          }
+    }
+  }
   if constexpr (SPLIT) {   // this split's sums, for bwd_dkdv_reduce_kernel
     const size_t rows = (size_t)BG * S;
     if (n < S) {

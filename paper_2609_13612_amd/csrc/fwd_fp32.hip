@@ -36,9 +36,12 @@ __global__ __launch_bounds__(64 * F32_NW) void fwd_fp32_kernel(FwdParams p) {
   const float c2 = p.scale * kLog2e;
   const float slope2 = ALIBI ? p.slopes[h] * kLog2e : 0.f;
   const int W = p.window;
-  int t = wave, t_end = nqb;
+  int t = wave, t_end = nqb, t_begin = 0, ns = 0;   // t: a tile's number among those visited, the ns with sinks first
   if constexpr (MASK != MASK_NONE) t_end = qb + 1;
-  if constexpr (MASK == MASK_SLIDING_WINDOW) t += max(0, m0 - W + 1) / F32_T;
+  if constexpr (windowed(MASK)) t_begin = max(0, m0 - W + 1) / F32_T;
+  if constexpr (MASK == MASK_SINKS) ns = min((p.sinks + F32_T - 1) / F32_T, t_begin);
+  const int n_tiles = ns + t_end - t_begin;
+  auto tile_at = [&](int i) { return i < ns ? i : t_begin + i - ns; };
 
   float k[DL], cs[DL], vt[DL];   // the tile in flight; rows past S: row S-1, masked
   auto load = [&](int tile) {
@@ -47,7 +50,7 @@ __global__ __launch_bounds__(64 * F32_NW) void fwd_fp32_kernel(FwdParams p) {
     f32_load_cs<D, ROPE>(cs, p.table + (size_t)n * (D / 2), g);
     f32_load_t<D>(vt, V, tile * F32_T, S, lq, g);
   };
-  if (t < t_end) load(t);
+  if (t < n_tiles) load(tile_at(t));
   float q[DL];
   {
     float qc[DL];
@@ -60,8 +63,8 @@ __global__ __launch_bounds__(64 * F32_NW) void fwd_fp32_kernel(FwdParams p) {
 #pragma unroll
   for (int i = 0; i < MT; ++i) acc[i] = f32x4{};
   float m_run = -INFINITY, l_run = 0.f;   // l_run: this lane's part
-  for (; t < t_end; t += F32_NW) {
-    const int n0 = t * F32_T + 4 * g;     // key of element 0
+  for (; t < n_tiles; t += F32_NW) {
+    const int n0 = tile_at(t) * F32_T + 4 * g;   // key of element 0
     float kr[DL], v[DL];
 #pragma unroll
     for (int i = 0; i < DL; ++i) {
@@ -69,7 +72,7 @@ __global__ __launch_bounds__(64 * F32_NW) void fwd_fp32_kernel(FwdParams p) {
       v[i] = vt[i];
     }
     f32_rotate<D, ROPE>(kr, cs);
-    if (t + F32_NW < t_end) load(t + F32_NW);
+    if (t + F32_NW < n_tiles) load(tile_at(t + F32_NW));
     const f32x4 s = f32_dot<D>(kr, q);
     float x[4], mx = -INFINITY;
 #pragma unroll
@@ -79,6 +82,7 @@ __global__ __launch_bounds__(64 * F32_NW) void fwd_fp32_kernel(FwdParams p) {
       bool ok = n < S;
       if constexpr (MASK != MASK_NONE) ok = ok && (n <= m);
       if constexpr (MASK == MASK_SLIDING_WINDOW) ok = ok && (n > m - W);
+      if constexpr (MASK == MASK_SINKS) ok = ok && (n > m - W || n < p.sinks);
       x[r] = ok ? x[r] : -INFINITY;
       mx = fmaxf(mx, x[r]);
     }
@@ -137,10 +141,11 @@ static int launch_one(const FwdParams& p, hipStream_t st) {
 
 template <int D, int ROPE>
 static int dispatch_mask(int mask, bool alibi, const FwdParams& p, hipStream_t st) {
-  switch (mask) {
+  switch (p.sinks > 0 ? (int)MASK_SINKS : mask) {
     case MASK_NONE: return alibi ? launch_one<D, ROPE, MASK_NONE, true>(p, st) : launch_one<D, ROPE, MASK_NONE, false>(p, st);
     case MASK_CAUSAL: return alibi ? launch_one<D, ROPE, MASK_CAUSAL, true>(p, st) : launch_one<D, ROPE, MASK_CAUSAL, false>(p, st);
     case MASK_SLIDING_WINDOW: return alibi ? launch_one<D, ROPE, MASK_SLIDING_WINDOW, true>(p, st) : launch_one<D, ROPE, MASK_SLIDING_WINDOW, false>(p, st);
+    case MASK_SINKS: return alibi ? -2 : launch_one<D, ROPE, MASK_SINKS, false>(p, st);
   }
   return -2;
 }

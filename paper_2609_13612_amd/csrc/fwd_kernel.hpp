@@ -134,14 +134,18 @@ void fwd_bf16_kernel(FwdParams p) {
   const int ntiles = (S + C::BN - 1) / C::BN;
   int t_begin = 0, t_end = ntiles;
   if constexpr (MASK != MASK_NONE) t_end = min(ntiles, (p_end - 1) / C::BN + 1);
-  if constexpr (MASK == MASK_SLIDING_WINDOW) t_begin = max(0, p0 - W + 1) / C::BN;
-  // The tiles the workgroup visits, by position i: t_begin + i, or under a
+  if constexpr (windowed(MASK)) t_begin = max(0, p0 - W + 1) / C::BN;
+  int ns = 0;                                    // tiles with sinks, before those of the window
+  if constexpr (MASK == MASK_SINKS) ns = min((p.sinks + C::BN - 1) / C::BN, t_begin);
+  // The tiles the workgroup visits, by position i: t_begin + i (after the ns that
+  // hold sinks), or under a
   // block-sparse mask the ascending active key blocks of its query block
   // (within the same range).
   __shared__ std::conditional_t<SPARSE, TileList<false>, int> tl;
-  int ntl = t_end - t_begin;   // (block-sparse: set once the query loads are in flight)
+  int ntl = ns + t_end - t_begin;   // (block-sparse: set once the query loads are in flight)
   auto tile_at = [&](int i) -> int {
     if constexpr (SPARSE) return __builtin_amdgcn_readfirstlane((int)tl.tile[i]);
+    else if constexpr (MASK == MASK_SINKS) return i < ns ? i : t_begin + i - ns;
     else return t_begin + i;
   };
   // LDS stage of the tile at position X (K' and V): X & 1, or under a
@@ -292,6 +296,7 @@ void fwd_bf16_kernel(FwdParams p) {
     if constexpr (MASK == MASK_NONE) need_mask = n0 + C::BN > S;
     else need_mask = n0 + C::BN - 1 > mw;
     if constexpr (MASK == MASK_SLIDING_WINDOW) need_mask = need_mask || (n0 <= mw + 31 - W);
+    if constexpr (MASK == MASK_SINKS) need_mask = need_mask || (n0 <= mw + 31 - W && n0 + C::BN > p.sinks);
     if (need_mask) {   // wave-uniform: diagonal, window-edge and sequence-end tiles only
       const int de = n0 + 4 * lg - S;        // key - S of element offset 0
 #pragma unroll
@@ -303,6 +308,7 @@ void fwd_bf16_kernel(FwdParams p) {
           if constexpr (MASK == MASK_NONE) ok = de < -cr;
           else ok = dq <= -cr;
           if constexpr (MASK == MASK_SLIDING_WINDOW) ok = ok && (dq + W > -cr);
+          if constexpr (MASK == MASK_SINKS) ok = ok && (dq + W > -cr || n0 + 4 * lg - p.sinks < -cr);
           sc[kt][r] = ok ? sc[kt][r] : -INFINITY;
         }
     }

@@ -27,6 +27,7 @@ struct FwdParams {
   const int* bk_idx;      // and the active 64-key blocks of each row
   const float* bias;      // dense bias: element (b, h, i, j) at bias[b*bias_sb + h*bias_sh + i*bias_sq + j]
   long long bias_sb, bias_sh, bias_sq;
+  int sinks;              // > 0 under a sliding window: first keys that stay visible, window + sinks < S
 };
 
 constexpr int DMAX_PARTS = 256;   // a wave reads four per lane
@@ -62,6 +63,9 @@ struct BwdParams {
   const int* bq_idx;
   const float* bias;      // dense bias, as in FwdParams
   long long bias_sb, bias_sh, bias_sq;
+  int sinks;              // as FwdParams
+  float* far;             // sinks > 0: partial dK', dV of the sinks, [B*H_kv][32-key blocks of sinks][far_parts][2][32][D]
+  int far_parts;
 };
 
 struct DecodeParams {
@@ -148,6 +152,12 @@ int launch_fwd_bf16(int D, int rope, int mask, bool alibi, int ext, const FwdPar
 // The same with p.k16 filled first (RoPE kinds only): two launches.
 int launch_fwd_prerot(int D, int rope, int mask, bool alibi, int ext, const FwdParams& p, hipStream_t st);
 int launch_fwd_fp32(int D, int rope, int mask, bool alibi, const FwdParams& p, hipStream_t st);
+// A sliding window with p.sinks > 0 (forward with RoPE: p.k16 is filled first); the
+// fp32 launchers go by p.sinks themselves.
+int launch_fwd_sinks(int D, int rope, const FwdParams& p, hipStream_t st);
+int launch_bwd_sinks(int D, int rope, const BwdParams& p, hipStream_t st);
+int launch_bwd_dkdv_sinks(int D, int rope, const BwdParams& p, hipStream_t st);   // its last launch
+int launch_bwd_dkdv_reduce(int D, int rope, const BwdParams& p, hipStream_t st);  // the reduction of a split pass
 int launch_bwd_bf16(int D, int rope, int mask, bool alibi, int ext, const BwdParams& p, hipStream_t st);
 // The dK/dV pass alone (the last launch of launch_bwd_bf16).
 int launch_bwd_dkdv_bf16(int D, int rope, int mask, bool alibi, int ext, const BwdParams& p, hipStream_t st);

@@ -107,8 +107,27 @@ STREAM_BAD = {
     UNSUPPORTED: [dict(D=96), dict(D=256, lens=None)],
 }
 
+FWD = dict(Q=A, K=A + 0x1000, V=A + 0x2000, O=A + 0x3000, LSE=A + 0x4000, ws=A + 0x5000, wbytes=2 * 2 * 100 * D * 2, B=2, H=4,
+           H_kv=2, S=100, D=D, dtype=0, rope=1, theta=1e4, table=TABLE, rows=100, window=10, sinks=2, scale=0.125, stream=None)
+FWD_BAD = {
+    INVALID: [dict(Q=None), dict(LSE=None), dict(K=ODD), dict(O=A), dict(ws=None), dict(ws=ODD), dict(ws=A),
+              dict(wbytes=2 * 2 * 100 * D * 2 - 1), dict(window=0), dict(sinks=0), dict(sinks=-1), dict(H_kv=3), dict(rows=99),
+              dict(scale=-1.0), dict(S=0), dict(dtype=3), dict(rope=3)],
+    UNSUPPORTED: [dict(D=96), dict(D=96, rope=0, ws=None, table=None), dict(D=96, dtype=1, ws=None, wbytes=0)],
+}
+GRAD = dict(Q=A, K=A + 0x1000, V=A + 0x2000, O=A + 0x3000, dO=A + 0x4000, LSE=A + 0x5000, dQ=A + 0x6000, dK=A + 0x7000,
+            dV=A + 0x8000, ws=A + 0x9000, wbytes=1 << 24, B=2, H=4, H_kv=2, S=100, D=D, dtype=0, rope=1, theta=1e4, table=TABLE,
+            rows=100, window=10, sinks=2, scale=0.125, stream=None)
+GRAD_BAD = {
+    INVALID: [dict(Q=None), dict(dO=None), dict(ws=None), dict(wbytes=0), dict(wbytes=1 << 12), dict(dK=A), dict(window=-3),
+              dict(sinks=0), dict(rows=1), dict(dV=ODD)],
+    UNSUPPORTED: [dict(D=96), dict(D=256, rope=0, table=None)],
+}
 
-@pytest.mark.parametrize("name,base,over,code", refusals("attnfuse_decode_paged", PAGED, PAGED_BAD)
+
+@pytest.mark.parametrize("name,base,over,code", refusals("attnfuse_fwd_sinks", FWD, FWD_BAD)
+                         + refusals("attnfuse_bwd_sinks", GRAD, GRAD_BAD)
+                         + refusals("attnfuse_decode_paged", PAGED, PAGED_BAD)
                          + refusals("attnfuse_decode_sinks", STREAM, STREAM_BAD)
                          + refusals("attnfuse_qknorm_rope", NORM, NORM_BAD)
                          + refusals("attnfuse_qknorm_rope_bwd", BWD, BWD_BAD)
@@ -135,3 +154,16 @@ def test_decode_workspace_bytes():
     for bad in ((0, 4, 2, 128, 64, 0, 0), (1, 3, 2, 128, 64, 0, 0), (1, 4, 2, 0, 64, 0, 0), (1, 4, 2, 128, 64, -1, 0),
                 (1, 4, 2, 128, 64, 0, -1)):
         assert f(*bad) == 0
+
+
+def test_sinks_workspace_bytes():
+    lib = _lib.load()
+    f = lib.attnfuse_fwd_sinks_workspace_bytes
+    assert f(2, 2, 100, 64, 0, 1) == 2 * 2 * 100 * 64 * 2
+    assert f(2, 2, 100, 64, 0, 0) == f(2, 2, 100, 64, 1, 1) == f(0, 2, 100, 64, 0, 1) == f(2, 2, 100, 96, 0, 1) == 0
+    g, base = lib.attnfuse_bwd_sinks_workspace_bytes, lib.attnfuse_bwd_workspace_bytes
+    # 32 sinks of 2 heads are one part of each until their workgroups' waves have two steps: 2 heads x 4 query tiles = 1 part
+    assert g(1, 4, 2, 128, 64, 0, 10, 32) == base(1, 4, 2, 128, 64, 0) + 2 * 1 * 2 * 32 * 64 * 4
+    assert g(1, 4, 2, 128, 64, 0, 100, 28) == base(1, 4, 2, 128, 64, 0)     # every key is visible
+    for bad in ((0, 4, 2, 128, 64, 0, 10, 4), (1, 4, 2, 128, 64, 0, 0, 4), (1, 4, 2, 128, 64, 0, 10, 0), (1, 3, 2, 128, 64, 0, 10, 4)):
+        assert g(*bad) == 0
