@@ -175,6 +175,27 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
   f32x16 dk[C::MT], dv[C::MT];
 #pragma unroll
   for (int i = 0; i < C::MT; ++i) { dk[i] = f32x16{}; dv[i] = f32x16{}; }
+  if constexpr (MASK == MASK_SINKS) {   // this pass is the window's pairs: start from the sinks' others (bwd_sinks.hip)
+    if (sp == 0 && nw < p.sinks) {        // (wave-uniform)
+      const int nfb = (p.sinks + 31) / 32;
+      const float* src = p.far + ((((size_t)bg * nfb + nw / 32) * p.far_parts * 2 + qh) * 32 + lq) * D + 4 * lg;
+      auto add_far = [&](f32x16 (&y)[C::MT]) {
+        for (int j = 0; j < p.far_parts; ++j, src += (size_t)2 * 32 * D)
+#pragma unroll
+          for (int mt = 0; mt < C::MT; ++mt)
+#pragma unroll
+            for (int a = 0; a < 4; ++a) {
+              const float4 x = *reinterpret_cast<const float4*>(src + 32 * mt + 8 * a);
+              y[mt][4 * a] += x.x;
+              y[mt][4 * a + 1] += x.y;
+              y[mt][4 * a + 2] += x.z;
+              y[mt][4 * a + 3] += x.w;
+            }
+      };
+      if (qh == 0) add_far(dk);
+      else add_far(dv);
+    }
+  }
 
   const float c2 = p.scale * kLog2e;
   const int W = p.window;
@@ -417,24 +438,6 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
   if (qh == 1) add(dv);
   __syncthreads();   // the exchange memory is free again: each wave's output rows go through it
 
-  if constexpr (MASK == MASK_SINKS) {   // this pass is the window's; the sinks' other queries (bwd_sinks.hip)
-    if (sp == 0 && nw < p.sinks) {        // (wave-uniform)
-      const int nfb = (p.sinks + 31) / 32;
-      const float* src = p.far + ((((size_t)bg * nfb + nw / 32) * p.far_parts * 2 + qh) * 32 + lq) * D + 4 * lg;
-      for (int j = 0; j < p.far_parts; ++j, src += (size_t)2 * 32 * D)
-#pragma unroll
-        for (int mt = 0; mt < C::MT; ++mt)
-#pragma unroll
-          for (int a = 0; a < 4; ++a) {
-            const float4 x = *reinterpret_cast<const float4*>(src + 32 * mt + 8 * a);
-            f32x16& y = (qh == 0) ? dk[mt] : dv[mt];
-            y[4 * a] += x.x;
-            y[4 * a + 1] += x.y;
-            y[4 * a + 2] += x.z;
-            y[4 * a + 3] += x.w;
-          }
-    }
-  }
   if constexpr (SPLIT) {   // this split's sums, for bwd_dkdv_reduce_kernel
     const size_t rows = (size_t)BG * S;
     if (n < S) {
