@@ -617,6 +617,11 @@ def attnfuse_qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, r
     """Qr, Kr: the rows of q and k over their root mean square, times the weights, rotated at their positions (0..S-1, or
     ``positions`` int32 [B, S], all below ``max_positions``); see attnfuse_qknorm_rope in include/attnfuse_llm.h.  q and k
     may be slices whose rows lie apart; Qr and Kr are contiguous."""
+    if _native is not None:
+        r = _native.qknorm(q, k, q_weight, k_weight, out_q, out_k, positions, rope_table, _TABLES, eps, ROPE.get(rope, -1),
+                           theta, max_positions)
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_rope")
     dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
     wt = _norm_weights(q_weight, k_weight, D, q.dtype, dev)
     out_q = _opt(out_q, "out_q", (B, H, S, D), q.dtype, dev)
@@ -642,6 +647,11 @@ def attnfuse_qknorm_rope_bwd(q, k, dqr, dkr, q_weight=None, k_weight=None, *, ep
                              rope_table=None):
     """dQ, dK, dq_weight, dk_weight of attnfuse_qknorm_rope (k and dkr None: of q alone; without ``weight_grads`` the last
     two are None); see attnfuse_qknorm_rope_bwd.  dQ and dK lie in memory as q and k do, without gaps."""
+    if _native is not None:
+        r = _native.qknorm_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, rope_table, _TABLES, eps,
+                               ROPE.get(rope, -1), theta, max_positions, int(bool(weight_grads)))
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_rope_bwd")
     dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
     wt = _norm_weights(q_weight, k_weight, D, q.dtype, dev)
     _need(dqr, "dqr", (B, H, S, D), q.dtype, dev)
@@ -685,6 +695,11 @@ def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None,
     page_size, D] at ``slots`` (int64 [T]: page * page_size + place; -1: nowhere); see attnfuse_qknorm_rope_append in
     include/attnfuse_llm.h.  q, k, v and the pages may lie apart (a fused projection's slices, pages [num_pages, page_size,
     H_kv, D] transposed)."""
+    if _native is not None:
+        r = _native.append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, rope_table, _TABLES,
+                           int(bool(norm)), eps, ROPE.get(rope, -1), theta, max_positions)
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_rope_append")[0]
     dev = _device(q)
     if q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("q must be [T, H, D] and k/v [T, H_kv, D]")
@@ -722,6 +737,10 @@ def _need_sinks(sinks, mask, window, alibi_slopes):
 
 def _fwd_sinks(q, k, v, rope, theta, mask, window, alibi_slopes, scale, out, lse, rope_table, sinks):
     _need_sinks(sinks, mask, window, alibi_slopes)
+    if _native is not None:
+        r = _native.fwd_sinks(q, k, v, out, lse, rope_table, _TABLES, ROPE.get(rope, -1), theta, window, sinks, scale)
+        if r is not None:
+            return _result(r, "attnfuse_fwd_sinks")
     dev = _device(q)
     B, H, Hkv, S, D = _shape(q, k)
     _inputs(q, k, v, dev)
@@ -744,6 +763,11 @@ def attnfuse_bwd_sinks_workspace_bytes(B, H, H_kv, S, D, rope, window, sinks):
 
 def _bwd_sinks(q, k, v, o, do, lse, rope, theta, mask, window, alibi_slopes, scale, dq, dk, dv, workspace, rope_table, sinks):
     _need_sinks(sinks, mask, window, alibi_slopes)
+    if _native is not None:
+        r = _native.bwd_sinks(q, k, v, o, do, lse, dq, dk, dv, workspace, rope_table, _TABLES, ROPE.get(rope, -1), theta,
+                              window, sinks, scale)
+        if r is not None:
+            return _result(r, "attnfuse_bwd_sinks")
     dev = _device(q)
     B, H, Hkv, S, D = _shape(q, k)
     _bwd_inputs(q, k, v, o, do, lse, dev, lse_needed=True)
@@ -762,6 +786,11 @@ def _bwd_sinks(q, k, v, o, do, lse, rope, theta, mask, window, alibi_slopes, sca
 def _decode_sinks(q, k_cache, v_cache, cache_lens, rope, theta, mask, window, alibi_slopes, scale, out, lse, workspace,
                   rope_table, sinks):
     _need_sinks(sinks, mask, window, alibi_slopes)
+    if _native is not None:
+        r = _native.decode_sinks(q, k_cache, v_cache, cache_lens, out, lse, workspace, rope_table, _TABLES,
+                                 ROPE.get(rope, -1), theta, window, sinks, scale)
+        if r is not None:
+            return _result(r, "attnfuse_decode_sinks")
     dev, (B, H, Hkv, S_kv, D), out, lse = _decode_args(q, k_cache, v_cache, cache_lens, out, lse)
     if q.dtype != torch.bfloat16:
         raise ValueError("decode with sinks takes bf16 tensors")
@@ -784,6 +813,13 @@ def attnfuse_decode_paged(q, k_cache, v_cache, block_table, cache_lens=None, *, 
     keys and their values, key n of sequence b in page ``block_table[b, n // page_size]`` (int32 [B, max_pages]); see
     attnfuse_decode_paged in include/attnfuse_llm.h.  The pages may lie apart (pages [num_pages, page_size, H_kv, D]
     transposed)."""
+    if sinks:
+        _need_sinks(sinks, mask, window, alibi_slopes)
+    if _native is not None:
+        r = _native.decode_paged(q, k_cache, v_cache, block_table, cache_lens, out, lse, workspace, alibi_slopes, rope_table,
+                                 _TABLES, ROPE.get(rope, -1), theta, MASK.get(mask, -1), window, sinks, scale)
+        if r is not None:
+            return _result(r, "attnfuse_decode_paged")
     dev = _device(q)
     if q.dim() != 3 or q.dtype != torch.bfloat16:
         raise ValueError("q must be a bf16 tensor [B, H, D]")
@@ -799,8 +835,6 @@ def attnfuse_decode_paged(q, k_cache, v_cache, block_table, cache_lens=None, *, 
     _need(block_table, "block_table", (B, block_table.shape[1]), torch.int32, dev)
     if cache_lens is not None:
         _need(cache_lens, "cache_lens", (B,), torch.int32, dev)
-    if sinks:
-        _need_sinks(sinks, mask, window, alibi_slopes)
     out = _opt(out, "out", (B, H, D), q.dtype, dev)
     lse = _opt(lse, "lse", (B, H), torch.float32, dev)
     r, th, m, w, sc = _variant(rope, theta, mask, window, alibi_slopes, scale, D, H, dev)

@@ -21,6 +21,7 @@
 
 #include <ATen/core/Tensor.h>
 #include <ATen/ops/empty.h>
+#include <ATen/ops/empty_like.h>
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
@@ -29,6 +30,7 @@
 #include <cmath>
 
 #include "attnfuse.h"
+#include "attnfuse_llm.h"
 #include "binding.h"
 
 namespace {
@@ -411,6 +413,313 @@ PyObject* rope(Args a) {
   return rc ? PyLong_FromLong(rc) : tuple_of({&y0, &y1});
 }
 
+// ---------------------------------------------------------------- include/attnfuse_llm.h
+// A tensor of rows that may lie apart: exactly that shape, type and device, each
+// row contiguous and 16-byte aligned; s: the strides of its other dimensions in
+// elements, 0 for one of a single row.
+struct Rows {
+  long long s[3] = {0, 0, 0};
+  Rows(const Tensor& t, at::IntArrayRef shape, at::ScalarType type, c10::Device dev) {
+    if (t.device() != dev || t.scalar_type() != type || t.sizes() != shape) throw NotPlain{};
+    const int64_t last = t.dim() - 1;
+    if ((t.stride(last) != 1 && t.size(last) > 1) || reinterpret_cast<uintptr_t>(t.const_data_ptr()) % 16) throw NotPlain{};
+    for (int64_t i = 0; i < last; ++i) {
+      s[i] = t.size(i) > 1 ? t.stride(i) : 0;
+      if (s[i] * (long long)t.element_size() % 16) throw NotPlain{};
+    }
+  }
+  Rows() = default;
+};
+
+// The norm weights: both [D], fp32 or the rows' type, the same for both.
+struct Weights {
+  const void *q = nullptr, *k = nullptr;
+  int type = AF_DTYPE_FP32;
+  at::ScalarType scalar = at::kFloat;
+  Weights(const Tensor* qw, const Tensor* kw, int64_t D, at::ScalarType rows, c10::Device dev) {
+    if (const Tensor* w = qw ? qw : kw) scalar = w->scalar_type();
+    if (scalar != at::kFloat && scalar != rows) throw NotPlain{};
+    type = scalar == at::kFloat ? AF_DTYPE_FP32 : AF_DTYPE_BF16;
+    for (const Tensor* w : {qw, kw}) {
+      if (!w) continue;
+      same(*w, {D}, scalar, dev);
+      if (reinterpret_cast<uintptr_t>(w->const_data_ptr()) % 16) throw NotPlain{};
+    }
+    q = qw ? qw->const_data_ptr() : nullptr;
+    k = kw ? kw->const_data_ptr() : nullptr;
+  }
+};
+
+// Positions and the table of their angles; args: positions, then (at `late`) the
+// table and the binding's tables; n rows at 0..n-1 without positions.
+struct Placed {
+  const int* positions = nullptr;
+  Table table;
+  Placed(const Tensor* pos, Args late, int rope, double theta, int64_t D, int64_t n, at::IntArrayRef shape,
+         long long max_positions, c10::Device dev) {
+    if (rope == AF_ROPE_NONE) return;
+    if (pos) {
+      same(*pos, shape, at::kInt, dev);
+      positions = static_cast<const int*>(pos->const_data_ptr());
+      Args peek = late;
+      if (max_positions <= 0 && !peek.tensor()) throw NotPlain{};
+      n = max_positions > 0 ? max_positions : 1;
+    }
+    table = table_of(late, rope, theta, D, n, dev);
+  }
+};
+
+Tensor workspace_or(const Tensor* given, size_t bytes, c10::Device dev) {
+  if (given) {
+    if (given->device() != dev || !given->is_contiguous()) throw NotPlain{};
+    return *given;
+  }
+  return at::empty({(int64_t)bytes}, at::TensorOptions().dtype(at::kByte).device(dev));
+}
+
+size_t bytes_of(const Tensor& t) { return (size_t)t.numel() * t.element_size(); }
+
+// q [B, H, S, D] and k [B, H_kv, S, D] or None, rows apart.
+struct Qk {
+  const Tensor& q;
+  const Tensor* k;
+  c10::Device dev;
+  int dtype;
+  at::ScalarType type;
+  int64_t B, H, S, D, Hkv = 0;
+  Rows qs, ks;
+  explicit Qk(Args& a) : q(a.need()), k(a.tensor()), dev(q.device()), dtype(dtype_of(q)), type(q.scalar_type()) {
+    if (q.dim() != 4 || (k && k->dim() != 4)) throw NotPlain{};
+    B = q.size(0); H = q.size(1); S = q.size(2); D = q.size(3);
+    if (k) Hkv = k->size(1);
+    for (int64_t x : {B, H, S, D, Hkv}) if (x > INT_MAX) throw NotPlain{};
+    qs = Rows(q, q.sizes(), type, dev);
+    if (k) ks = Rows(*k, {B, Hkv, S, D}, type, dev);
+  }
+};
+
+// qknorm(q, k, q_weight, k_weight, out_q, out_k, positions, table, tables, eps, rope, theta, max_positions) -> (Qr, Kr)
+PyObject* qknorm(Args a) {
+  Qk x(a);
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *ok_ = a.tensor(), *pos = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const float eps = (float)a.number();
+  const int rope = a.index();
+  const double theta = a.number();
+  const long long most = a.whole();
+  if (!x.k && (kw || ok_)) throw NotPlain{};
+  const Weights w(qw, kw, x.D, x.type, x.dev);
+  const Placed at_(pos, late, rope, theta, x.D, x.S, {x.B, x.S}, most, x.dev);
+  const Tensor oq = out_or(oq_, x.q.sizes(), x.type, x.dev);
+  Tensor ok;
+  if (x.k) ok = out_or(ok_, x.k->sizes(), x.type, x.dev);
+  const int rc = enqueue(x.dev, [&](void* st) {
+    return attnfuse_qknorm_rope(in(x.q), x.k ? in(*x.k) : nullptr, out(oq), x.k ? out(ok) : nullptr, w.q, w.k, w.type, eps,
+                                x.qs.s[0], x.qs.s[1], x.qs.s[2], x.ks.s[0], x.ks.s[1], x.ks.s[2], (int)x.B, (int)x.H,
+                                (int)x.Hkv, (int)x.S, (int)x.D, x.dtype, rope, (float)theta, at_.table.ptr, at_.table.rows,
+                                at_.positions, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&oq, &ok});
+}
+
+// qknorm_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, table, tables, eps, rope, theta,
+//            max_positions, weight_grads) -> (dQ, dK, dq_weight, dk_weight)
+PyObject* qknorm_bwd(Args a) {
+  Qk x(a);
+  const Tensor& dqr = a.need();
+  const Tensor *dkr = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *dq_ = a.tensor(), *dk_ = a.tensor(), *ws_ = a.tensor(),
+               *pos = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const float eps = (float)a.number();
+  const int rope = a.index();
+  const double theta = a.number();
+  const long long most = a.whole();
+  const bool grads = a.whole() != 0;
+  if (!x.k != !dkr || (!x.k && (kw || dk_))) throw NotPlain{};
+  const Weights w(qw, kw, x.D, x.type, x.dev);
+  const Placed at_(pos, late, rope, theta, x.D, x.S, {x.B, x.S}, most, x.dev);
+  same(dqr, x.q.sizes(), x.type, x.dev);
+  if (dkr) same(*dkr, x.k->sizes(), x.type, x.dev);
+  const Tensor dq = dq_ ? *dq_ : at::empty_like(x.q);
+  Tensor dk, dqw, dkw, ws;
+  if (x.k) dk = dk_ ? *dk_ : at::empty_like(*x.k);
+  const Rows dqs(dq, x.q.sizes(), x.type, x.dev);
+  Rows dks;
+  if (x.k) dks = Rows(dk, x.k->sizes(), x.type, x.dev);
+  if (grads) {
+    const auto options = at::TensorOptions().dtype(w.scalar).device(x.dev);
+    dqw = at::empty({x.D}, options);
+    if (x.k) dkw = at::empty({x.D}, options);
+    ws = workspace_or(ws_, attnfuse_qknorm_rope_bwd_workspace_bytes((int)x.B, (int)x.H, (int)x.Hkv, (int)x.S, (int)x.D,
+                                                                    x.dtype), x.dev);
+  }
+  const int rc = enqueue(x.dev, [&](void* st) {
+    return attnfuse_qknorm_rope_bwd(
+        in(x.q), x.k ? in(*x.k) : nullptr, in(dqr), dkr ? in(*dkr) : nullptr, out(dq), x.k ? out(dk) : nullptr,
+        grads ? out(dqw) : nullptr, grads && x.k ? out(dkw) : nullptr, w.q, w.k, w.type, eps, x.qs.s[0], x.qs.s[1], x.qs.s[2],
+        x.ks.s[0], x.ks.s[1], x.ks.s[2], dqs.s[0], dqs.s[1], dqs.s[2], dks.s[0], dks.s[1], dks.s[2],
+        grads ? out(ws) : nullptr, grads ? bytes_of(ws) : 0, (int)x.B, (int)x.H, (int)x.Hkv, (int)x.S, (int)x.D, x.dtype,
+        rope, (float)theta, at_.table.ptr, at_.table.rows, at_.positions, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dqw, &dkw});
+}
+
+// append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, table, tables, norm, eps, rope, theta,
+//        max_positions) -> (Qr,)
+PyObject* append(Args a) {
+  const Tensor &q = a.need(), &k = a.need(), &v = a.need(), &kc = a.need(), &vc = a.need(), &slots = a.need();
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *pos = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const bool norm = a.whole() != 0;
+  const float eps = (float)a.number();
+  const int rope = a.index();
+  const double theta = a.number();
+  const long long most = a.whole();
+  const int dtype = dtype_of(q);
+  const c10::Device dev = q.device();
+  const at::ScalarType type = q.scalar_type();
+  if (q.dim() != 3 || k.dim() != 3 || kc.dim() != 4 || (rope != AF_ROPE_NONE && !pos)) throw NotPlain{};
+  const int64_t T = q.size(0), H = q.size(1), D = q.size(2), Hkv = k.size(1), pages = kc.size(0), page = kc.size(2);
+  for (int64_t n : {T, H, D, Hkv, pages, page}) if (n > INT_MAX) throw NotPlain{};
+  const Rows qs(q, {T, H, D}, type, dev), ks(k, {T, Hkv, D}, type, dev), vs(v, {T, Hkv, D}, type, dev),
+      kcs(kc, {pages, Hkv, page, D}, type, dev), vcs(vc, {pages, Hkv, page, D}, type, dev);
+  same(slots, {T}, at::kLong, dev);
+  const Weights w(qw, kw, D, type, dev);
+  const Placed at_(pos, late, rope, theta, D, 1, {T}, most, dev);
+  const Tensor oq = out_or(oq_, q.sizes(), type, dev);
+  const int rc = enqueue(dev, [&](void* st) {
+    return attnfuse_qknorm_rope_append(
+        in(q), in(k), in(v), out(oq), out(kc), out(vc), reinterpret_cast<const long long*>(slots.const_data_ptr()), w.q, w.k,
+        w.type, norm, eps, qs.s[0], qs.s[1], ks.s[0], ks.s[1], vs.s[0], vs.s[1], kcs.s[0], kcs.s[1], kcs.s[2], vcs.s[0],
+        vcs.s[1], vcs.s[2], (int)T, (int)H, (int)Hkv, (int)D, (int)pages, (int)page, dtype, rope, (float)theta,
+        at_.table.ptr, at_.table.rows, at_.positions, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&oq});
+}
+
+// decode_paged(q, k_cache, v_cache, block_table, lens, out, lse, workspace, slopes, table, tables, rope, theta, mask, window,
+//              sinks, scale) -> (O, LSE)
+PyObject* decode_paged(Args a) {
+  const Tensor &q = a.need(), &kc = a.need(), &vc = a.need(), &table = a.need();
+  const Tensor *lens = a.tensor(), *out_ = a.tensor(), *lse = a.tensor(), *ws_ = a.tensor(), *slopes = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const int rope = a.index();
+  const double theta = a.number();
+  const int mask = a.index(), window = a.size(), sinks = a.size();
+  const c10::Device dev = q.device();
+  const at::ScalarType type = q.scalar_type();
+  if (dtype_of(q) != AF_DTYPE_BF16 || q.dim() != 3 || kc.dim() != 4 || table.dim() != 2) throw NotPlain{};
+  const int64_t B = q.size(0), H = q.size(1), D = q.size(2), pages = kc.size(0), Hkv = kc.size(1), page = kc.size(2),
+                most = table.size(1);
+  for (int64_t n : {B, H, D, Hkv, pages, page, most}) if (n > (1 << 28)) throw NotPlain{};
+  const int64_t S = most * page;
+  if (S > INT_MAX) throw NotPlain{};
+  const float scale = a.scale(D);
+  same(q, q.sizes(), type, dev);
+  const Rows ks(kc, {pages, Hkv, page, D}, type, dev), vs(vc, {pages, Hkv, page, D}, type, dev);
+  same(table, {B, most}, at::kInt, dev);
+  if (lens) same(*lens, {B}, at::kInt, dev);
+  const Table tab = table_of(late, rope, theta, D, S, dev);
+  const float* sl = slopes_of(slopes, H, dev);
+  const Tensor o = out_or(out_, q.sizes(), type, dev), l = out_or(lse, {B, H}, at::kFloat, dev);
+  const Tensor ws = workspace_or(ws_, attnfuse_decode_paged_workspace_bytes((int)B, (int)H, (int)Hkv, (int)S, (int)D,
+                                                                            mask == AF_MASK_SLIDING_WINDOW ? window : 0,
+                                                                            sinks), dev);
+  const int rc = enqueue(dev, [&](void* st) {
+    return attnfuse_decode_paged(in(q), in(kc), in(vc), static_cast<const int*>(table.const_data_ptr()),
+                                 lens ? static_cast<const int*>(lens->const_data_ptr()) : nullptr, out(o),
+                                 static_cast<float*>(out(l)), out(ws), bytes_of(ws), ks.s[0], ks.s[1], ks.s[2], vs.s[0],
+                                 vs.s[1], vs.s[2], (int)B, (int)H, (int)Hkv, (int)D, (int)pages, (int)page, (int)most, rope,
+                                 (float)theta, tab.ptr, tab.rows, mask, window, sinks, sl, scale, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
+}
+
+// decode_sinks(q, k, v, lens, out, lse, workspace, table, tables, rope, theta, window, sinks, scale) -> (O, LSE)
+PyObject* decode_sinks(Args a) {
+  const Tensor &q = a.need(), &k = a.need(), &v = a.need();
+  const Tensor *lens = a.tensor(), *out_ = a.tensor(), *lse = a.tensor(), *ws_ = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const int rope = a.index();
+  const double theta = a.number();
+  const int window = a.size(), sinks = a.size();
+  const c10::Device dev = q.device();
+  const at::ScalarType type = q.scalar_type();
+  if (dtype_of(q) != AF_DTYPE_BF16 || q.dim() != 3 || k.dim() != 4) throw NotPlain{};
+  const int64_t B = q.size(0), H = q.size(1), D = q.size(2), Hkv = k.size(1), S = k.size(2);
+  for (int64_t n : {B, H, D, Hkv, S}) if (n > INT_MAX) throw NotPlain{};
+  const float scale = a.scale(D);
+  same(q, q.sizes(), type, dev);
+  same(k, {B, Hkv, S, D}, type, dev);
+  same(v, {B, Hkv, S, D}, type, dev);
+  if (lens) same(*lens, {B}, at::kInt, dev);
+  const Table tab = table_of(late, rope, theta, D, S, dev);
+  const Tensor o = out_or(out_, q.sizes(), type, dev), l = out_or(lse, {B, H}, at::kFloat, dev);
+  const Tensor ws = workspace_or(ws_, attnfuse_decode_paged_workspace_bytes((int)B, (int)H, (int)Hkv, (int)S, (int)D, window,
+                                                                            sinks), dev);
+  const int rc = enqueue(dev, [&](void* st) {
+    return attnfuse_decode_sinks(in(q), in(k), in(v), lens ? static_cast<const int*>(lens->const_data_ptr()) : nullptr,
+                                 out(o), static_cast<float*>(out(l)), out(ws), bytes_of(ws), (int)B, (int)H, (int)Hkv, (int)S,
+                                 (int)D, rope, (float)theta, tab.ptr, tab.rows, window, sinks, scale, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
+}
+
+// fwd_sinks(q, k, v, out, lse, table, tables, rope, theta, window, sinks, scale) -> (O, LSE)
+PyObject* fwd_sinks(Args a) {
+  Qkv x(a);
+  const Tensor *out_ = a.tensor(), *lse = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const int rope = a.index();
+  const double theta = a.number();
+  const int window = a.size(), sinks = a.size();
+  const float scale = a.scale(x.D);
+  const Table tab = table_of(late, rope, theta, x.D, x.S, x.dev);
+  const Tensor o = out_or(out_, x.q.sizes(), x.type, x.dev), l = out_or(lse, {x.B, x.H, x.S}, at::kFloat, x.dev);
+  const int B = (int)x.B, H = (int)x.H, Hkv = (int)x.Hkv, S = (int)x.S, D = (int)x.D;
+  Tensor ws;
+  const size_t n = attnfuse_fwd_sinks_workspace_bytes(B, Hkv, S, D, x.dtype, rope);
+  if (n) ws = workspace_or(nullptr, n, x.dev);
+  const int rc = enqueue(x.dev, [&](void* st) {
+    return attnfuse_fwd_sinks(in(x.q), in(x.k), in(x.v), out(o), static_cast<float*>(out(l)), n ? out(ws) : nullptr, n, B, H,
+                              Hkv, S, D, x.dtype, rope, (float)theta, tab.ptr, tab.rows, window, sinks, scale, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
+}
+
+// bwd_sinks(q, k, v, o, do, lse, dq, dk, dv, workspace, table, tables, rope, theta, window, sinks, scale) -> (dQ, dK, dV)
+PyObject* bwd_sinks(Args a) {
+  Qkv x(a);
+  const Tensor &o = a.need(), &dout = a.need(), &lse = a.need();
+  const Tensor *dq_ = a.tensor(), *dk_ = a.tensor(), *dv_ = a.tensor(), *ws_ = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const int rope = a.index();
+  const double theta = a.number();
+  const int window = a.size(), sinks = a.size();
+  const float scale = a.scale(x.D);
+  const Table tab = table_of(late, rope, theta, x.D, x.S, x.dev);
+  same(o, x.q.sizes(), x.type, x.dev);
+  same(dout, x.q.sizes(), x.type, x.dev);
+  same(lse, {x.B, x.H, x.S}, at::kFloat, x.dev);
+  const Tensor dq = out_or(dq_, x.q.sizes(), x.type, x.dev), dk = out_or(dk_, x.k.sizes(), x.type, x.dev),
+               dv = out_or(dv_, x.k.sizes(), x.type, x.dev);
+  const int B = (int)x.B, H = (int)x.H, Hkv = (int)x.Hkv, S = (int)x.S, D = (int)x.D;
+  const Tensor ws = workspace_or(ws_, attnfuse_bwd_sinks_workspace_bytes(B, H, Hkv, S, D, rope, window, sinks), x.dev);
+  const int rc = enqueue(x.dev, [&](void* st) {
+    return attnfuse_bwd_sinks(in(x.q), in(x.k), in(x.v), in(o), in(dout), static_cast<const float*>(lse.const_data_ptr()),
+                              out(dq), out(dk), out(dv), out(ws), bytes_of(ws), B, H, Hkv, S, D, x.dtype, rope, (float)theta,
+                              tab.ptr, tab.rows, window, sinks, scale, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dv});
+}
+
 template <PyObject* (*F)(Args)>
 PyObject* entry(PyObject*, PyObject* const* v, Py_ssize_t n) {
   HANDLE_TH_ERRORS
@@ -428,6 +737,9 @@ constexpr PyMethodDef method(const char* name) {
 }
 
 PyMethodDef methods[] = {method<fwd>("fwd"), method<bwd>("bwd"), method<decode>("decode"), method<rope>("rope"),
+                         method<qknorm>("qknorm"), method<qknorm_bwd>("qknorm_bwd"), method<append>("append"),
+                         method<decode_paged>("decode_paged"), method<decode_sinks>("decode_sinks"),
+                         method<fwd_sinks>("fwd_sinks"), method<bwd_sinks>("bwd_sinks"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
