@@ -194,8 +194,8 @@ size_t attnfuse_decode_paged_workspace_bytes(int B, int H, int H_kv, int S_kv, i
  *                                 to fp16: keys may have any bf16 value, and the
  *                                 LSE is that of the cached keys to 2^-16 of the
  *                                 scores' magnitudes.
- *   D in {64, 128}; any H a multiple of H_kv (a group of more than 32 query heads
- *   reads the cache once for each 32)
+ *   D in {64, 128}; B < 2^16; any H <= 16384 that is a multiple of H_kv (a group of
+ *   more than 32 query heads reads the cache once for each 32)
  *
  * A sequence's result depends on its own keys and length only, not on the other
  * sequences.  What lies in places that are not visible is never used, whatever

@@ -81,12 +81,19 @@ int page_shift_of(int page_size) {
 
 // ---------------------------------------------------------------- decode
 struct PagedLayout {
-  int hgroups, chunk, nsplit;
+  int hgroups, nsplit;
   size_t ml, acc, total;
 };
 
-// Visible 32-key tiles per workgroup: a power of two from 4 (one for each of its
-// waves) that leaves at most about 1024 workgroups.
+// Workgroups that share a sequence's visible 32-key tiles for a head group: one for
+// each CU over the whole batch, while every wave of theirs has a tile; then twice
+// as many, while a share keeps 32 tiles (eight for each wave) and there are fewer
+// than 1024, so that CUs with short sequences take more of the long ones.  A round of
+// tiles takes a lone wave 1.4 us, 124 workgroups saturate the memory, and the
+// second launch costs 5 us.  us with 1 / 2 / 4 / 8 / 16 / 32 shares, and those taken:
+//   B1 H32/8 D128 4096 keys: 50 / 31 / 21 / 16 / 13.5 / 12.6, 32;  B8 H32/8 8192: 102 / 63 / 54 / 56 / 57 / 65, 8
+//   B8 H64/8 lengths 8k to 32k: 357 / 198 / 139 / 132 / 136 / 136, 16;  B32 H32/8 window 1024: 28 / 33 / 36 / 54, 1
+//   B48 H12 D64 3500 keys: 114 / 108 / 102 / 106, 2;  B70 H32/8 lengths to 1500: 64 / 71 / 78 / 100, 1
 PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int sinks) {
   PagedLayout L{};
   L.hgroups = (H / H_kv + 31) / 32;
@@ -96,9 +103,10 @@ PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int s
     tiles = tiles < most ? tiles : most;
   }
   const long long units = (long long)B * H_kv * L.hgroups;
-  L.chunk = 4;
-  while (L.chunk < tiles && units * ((tiles + L.chunk - 1) / L.chunk) > 1024) L.chunk *= 2;
-  L.nsplit = (int)((tiles + L.chunk - 1) / L.chunk);
+  long long n = units < 256 ? (256 + units - 1) / units : 1;
+  while (n > 1 && tiles < 4 * n) --n;
+  while (units * n < 1024 && tiles >= 64 * n) n *= 2;
+  L.nsplit = (int)n;
   const size_t parts = (size_t)B * H * L.nsplit;
   L.ml = 0;
   L.acc = align256(parts * 2 * sizeof(float));
@@ -107,7 +115,7 @@ PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int s
 }
 
 bool decode_sizes(int B, int H, int H_kv, int S, int D) {
-  return B >= 1 && H >= 1 && H_kv >= 1 && H % H_kv == 0 && S >= 1 && S <= kMaxS && D >= 2 && D % 2 == 0 &&
+  return B >= 1 && B < (1 << 16) && H >= 1 && H <= kMaxHeads && H_kv >= 1 && H % H_kv == 0 && S >= 1 && S <= kMaxS && D >= 2 && D % 2 == 0 &&
          (long long)B * H * ((S + 63) / 64) < (1LL << 31);
 }
 
@@ -141,7 +149,7 @@ int decode_impl(af::PagedParams& p, const void* Q, const void* K, const void* V,
   p.part_acc = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.acc);
   p.B = B; p.H = H; p.Hkv = H_kv; p.S = S;
   p.window = window; p.sinks = sinks;
-  p.chunk = L.chunk; p.nsplit = L.nsplit; p.hgroups = L.hgroups;
+  p.nsplit = L.nsplit; p.G = H / H_kv; p.hgroups = L.hgroups;
   p.slopes = alibi_slopes;
   p.scale = softmax_scale;
   p.rope = reinterpret_cast<const float2*>(rope_table);

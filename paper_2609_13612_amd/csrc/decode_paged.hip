@@ -7,10 +7,11 @@
 // bound by reading the visible part of the cache once.
 //
 // The visible 32-key tiles of a sequence are numbered from 0: first the tiles
-// that hold sinks, then those of the window.  Workgroup = 4 waves = `chunk` of
-// those tiles of one (sequence, K/V head, up to 32 query heads), the waves taking
-// tiles in turn; which tiles depends on the sequence's own length alone, so its
-// result does too.  The four waves' (max, sum, O) are joined through LDS and
+// that hold sinks, then those of the window.  Workgroup = 4 waves = one of nsplit
+// shares of those tiles for one (sequence, K/V head, up to 32 query heads): wave w of
+// share s takes tiles 4 s + w, 4 (s + nsplit) + w, ..., so shares are even whatever
+// the length, the first tile's page is looked up before the length is known, and a
+// sequence's result depends on its own length alone.  The four waves' (max, sum, O) are joined through LDS and
 // leave as one partial per workgroup, or as the result where a sequence is
 // one workgroup's; a second kernel joins the partials.
 //
@@ -44,12 +45,18 @@ struct PagedCfg {
   static constexpr int SMEM = NW * VT * 2 > XCH ? NW * VT * 2 : XCH;
 };
 
+// A value that no kernel writes while this one runs, at a wave-uniform address: a
+// scalar load.  (A vector load would be waited for with vmcnt, behind every load of
+// the tiles in flight.)
+__device__ __forceinline__ int uniform_load(const int* p) {
+  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
+}
+
 // The visible tiles of a sequence with L keys: tiles [0, ns), then [t0, t0 + n - ns).
 struct Visible {
   int L, lo, sinks, ns, t0, n;
-  __device__ __forceinline__ Visible(const PagedParams& p, int b) {
-    L = p.lens ? min(p.lens[b], p.S) : p.S;
-    L = max(L, 0);
+  __device__ __forceinline__ Visible(const PagedParams& p, int len) {
+    L = max(min(len, p.S), 0);
     lo = p.window > 0 ? max(0, L - p.window) : 0;
     sinks = min(p.sinks, lo);                     // (those still in the window are the window's)
     t0 = lo >> 5;
@@ -71,24 +78,13 @@ void paged_split_kernel(PagedParams p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, lg = lane >> 5;
-  const int split = (int)(blockIdx.x % p.nsplit);
-  const int unit = (int)(blockIdx.x / p.nsplit);
-  const int hg = unit % p.hgroups, bg = unit / p.hgroups;
-  const int b = bg / p.Hkv, g = bg % p.Hkv;
-  const int G = p.H / p.Hkv, h0 = hg * 32, nh = min(32, G - h0);   // this workgroup's heads of the group
-  const Visible vis(p, b);
-  const int i_end = min((split + 1) * p.chunk, vis.n);
-  const int i_begin = split * p.chunk;
-  if (i_begin >= i_end) {                         // (workgroup-uniform)
-    if (p.nsplit == 1) {                          // an empty sequence: nothing else writes its rows
-      for (int j = tid; j < nh * (D / 8); j += 256)
-        st16(static_cast<uint16_t*>(p.o) + ((size_t)b * p.H + g * G + h0) * D + 8 * j, u32x4{0, 0, 0, 0});
-      if (tid < nh) p.lse[(size_t)b * p.H + g * G + h0 + tid] = -INFINITY;
-    }
-    return;
+  const int split = blockIdx.x, b = blockIdx.z;
+  int g = blockIdx.y, hg = 0;
+  if (p.hgroups > 1) {
+    hg = g % p.hgroups;
+    g /= p.hgroups;
   }
-  const int L = vis.L, pos = L - 1;
-
+  const int G = p.G, h0 = hg * 32, nh = min(32, G - h0);   // this workgroup's heads of the group
   const int h = g * G + h0 + lq % nh;             // head of this lane's column
   const float c2 = p.scale * kLog2e;
   const float slope2 = ALIBI ? p.slopes[h] * kLog2e : 0.f;
@@ -110,13 +106,38 @@ void paged_split_kernel(PagedParams p) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       if constexpr (PAGED) {
-        const int e = table[min((n0 + 16 * u) >> p.page_shift, p.max_pages - 1)];
+        const int e = uniform_load(table + min((n0 + 16 * u) >> p.page_shift, p.max_pages - 1));
         pg[u] = (unsigned)e < (unsigned)p.num_pages ? e : -1;
       } else {
         pg[u] = b;
       }
     }
   };
+  int pg[2] = {-1, -1}, pn[2] = {-1, -1};         // pages of the tile in flight, of the one after it
+  int i = C::NW * split + wave;                   // this wave's tile
+  const int step = C::NW * p.nsplit;
+  const bool early = PAGED && p.window <= 0;      // its place does not depend on the length
+  if (early) pages_of(32 * i, pg);
+  // Query rows (B operand of S^T = K Q'^T): lane holds column lq's head, dims 16s + 8lg .. +7.
+  u32x4 qreg[NQ][C::KS];
+  {
+    const uint16_t* Qh = static_cast<const uint16_t*>(p.q) + ((size_t)b * p.H + h) * D;
+#pragma unroll
+    for (int s = 0; s < C::KS; ++s) qreg[0][s] = ld16(Qh + 16 * s + 8 * lg);
+  }
+  const int len = p.lens ? uniform_load(p.lens + b) : p.S;
+  const Visible vis(p, len);
+  const int n_tiles = vis.n;
+  if (C::NW * split >= n_tiles) {                 // (workgroup-uniform)
+    if (p.nsplit == 1) {                          // an empty sequence: nothing else writes its rows
+      for (int j = tid; j < nh * (D / 8); j += 256)
+        st16(static_cast<uint16_t*>(p.o) + ((size_t)b * p.H + g * G + h0) * D + 8 * j, u32x4{0, 0, 0, 0});
+      if (tid < nh) p.lse[(size_t)b * p.H + g * G + h0 + tid] = -INFINITY;
+    }
+    return;
+  }
+  const int L = vis.L, pos = L - 1;
+
   u32x4 kreg[C::KS], vreg[C::VPL];
   // Rows that are not there (no page; past a contiguous cache) read another
   // row's finite memory: page 0, or the last row.  Their keys are masked and
@@ -153,21 +174,14 @@ void paged_split_kernel(PagedParams p) {
     }
   };
 
-  int i = i_begin + wave;
-  int pg[2] = {-1, -1}, pn[2] = {-1, -1};         // pages of the tile in flight, of the one after it
-  if (i < i_end) {
-    pages_of(32 * vis.tile(i), pg);
+  if (i < n_tiles) {
+    if (!early) pages_of(32 * vis.tile(i), pg);
     load_tile(32 * vis.tile(i), pg);
-    if (i + C::NW < i_end) pages_of(32 * vis.tile(i + C::NW), pn);
+    if (i + step < n_tiles) pages_of(32 * vis.tile(i + step), pn);
   }
 
-  // Query operand (B of S^T = K Q'^T): lane holds column lq's head, dims 16s + 8lg .. +7.
-  u32x4 qreg[NQ][C::KS];
   {
-    const uint16_t* Qh = static_cast<const uint16_t*>(p.q) + ((size_t)b * p.H + h) * D;
-#pragma unroll
-    for (int s = 0; s < C::KS; ++s) qreg[0][s] = ld16(Qh + 16 * s + 8 * lg);
-    if constexpr (ROPE != ROPE_NONE) {
+    if constexpr (ROPE != ROPE_NONE) {   // rotate the query and split it
       const float2* t = p.rope + (size_t)pos * (D / 2);
       auto split2 = [&](int s, int w, float x0, float x1) {
         const uint32_t hi = pack_bf16(x0, x1);
@@ -205,7 +219,7 @@ void paged_split_kernel(PagedParams p) {
     }
   }
 
-  for (; i < i_end; i += C::NW) {
+  for (; i < n_tiles; i += step) {
     const int n0 = 32 * vis.tile(i);
     // some key of the tile is not visible: past the end, before the window, or without a page
     const bool edge = n0 + 32 > L || (n0 < vis.lo && n0 + 32 > vis.sinks) || pg[0] < 0 || pg[1] < 0;   // (wave-uniform)
@@ -228,11 +242,11 @@ void paged_split_kernel(PagedParams p) {
 #pragma unroll
       for (int r = 0; r < 16; ++r) hidden |= (uint32_t)!seen(8 * (r >> 2) + 4 * lg + (r & 3)) << r;
     }
-    if (i + C::NW < i_end) {
+    if (i + step < n_tiles) {
       pg[0] = pn[0];
       pg[1] = pn[1];
-      load_tile(32 * vis.tile(i + C::NW), pg);
-      if (i + 2 * C::NW < i_end) pages_of(32 * vis.tile(i + 2 * C::NW), pn);
+      load_tile(32 * vis.tile(i + step), pg);
+      if (i + 2 * step < n_tiles) pages_of(32 * vis.tile(i + 2 * step), pn);
     }
 
     // element r: key n0 + 8 (r/4) + 4 lg + r%4 of column lq
@@ -343,21 +357,36 @@ void paged_split_kernel(PagedParams p) {
 }
 
 // Join the partials of one (sequence, query head), none of an empty sequence: D /
-// 4 lanes hold the dims, the groups of lanes take every NG-th partial.
-template <int D>
+// 4 lanes hold the dims, the groups of lanes take every NG-th partial.  The first
+// PF of a group and the statistics are on their way before the length, which says
+// how many there are, is known: one round trip to memory where they are all.
+template <int D, int PF>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
   constexpr int LPR = D / 4, NG = 256 / LPR;
   __shared__ float4 red[NG][LPR];
   __shared__ float wml[2][4];
   const int t = threadIdx.x, c = t % LPR, grp = t / LPR;
-  const size_t bh = blockIdx.x;
-  const Visible vis(p, (int)(bh / p.H));
-  const int n = (vis.n + p.chunk - 1) / p.chunk;   // partials
-  uint16_t* O = static_cast<uint16_t*>(p.o) + bh * D + 4 * c;
+  const int b = blockIdx.y;
+  const size_t bh = (size_t)b * p.H + blockIdx.x;
   const float* ml = p.part_ml + 2 * bh * p.nsplit;
   const float* acc = p.part_acc + bh * p.nsplit * D + 4 * c;
+  float4 x[PF];
+  float mx[PF];
+#pragma unroll
+  for (int j = 0; j < PF; ++j) {
+    const int i = min(grp + NG * j, p.nsplit - 1);
+    x[j] = *reinterpret_cast<const float4*>(acc + (size_t)i * D);
+    mx[j] = ml[2 * i];
+  }
+  float2 own = *reinterpret_cast<const float2*>(ml + 2 * min(t, p.nsplit - 1));
+  const Visible vis(p, p.lens ? uniform_load(p.lens + b) : p.S);
+  const int n = min(p.nsplit, (vis.n + 3) / 4);   // partials: the shares that have tiles
   float m = -INFINITY, l = 0.f;
-  for (int i = t; i < n; i += 256) {
+  if (t < n) {
+    m = own.x;
+    l = own.y;
+  }
+  for (int i = t + 256; i < n; i += 256) {
     const float2 v = *reinterpret_cast<const float2*>(ml + 2 * i);
     const float M = fmaxf(m, v.x);
     if (M != -INFINITY) {
@@ -386,28 +415,32 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
   for (int w = 0; w < 4; ++w)
     if (wml[0][w] != -INFINITY) l += wml[1][w] * fast_exp2(wml[0][w] - M);
   float4 sum = {0.f, 0.f, 0.f, 0.f};
-  for (int i = grp; i < n; i += NG) {
-    const float mi = ml[2 * i];
-    const float w = mi == -INFINITY ? 0.f : fast_exp2(mi - M);
-    const float4 x = *reinterpret_cast<const float4*>(acc + (size_t)i * D);
-    sum.x = __builtin_fmaf(w, x.x, sum.x);
-    sum.y = __builtin_fmaf(w, x.y, sum.y);
-    sum.z = __builtin_fmaf(w, x.z, sum.z);
-    sum.w = __builtin_fmaf(w, x.w, sum.w);
-  }
+  auto fold = [&](float mi, const float4& y) {
+    if (mi == -INFINITY) return;
+    const float w = fast_exp2(mi - M);
+    sum.x = __builtin_fmaf(w, y.x, sum.x);
+    sum.y = __builtin_fmaf(w, y.y, sum.y);
+    sum.z = __builtin_fmaf(w, y.z, sum.z);
+    sum.w = __builtin_fmaf(w, y.w, sum.w);
+  };
+#pragma unroll
+  for (int j = 0; j < PF; ++j)
+    if (grp + NG * j < n) fold(mx[j], x[j]);
+  for (int i = grp + NG * PF; i < n; i += NG) fold(ml[2 * i], *reinterpret_cast<const float4*>(acc + (size_t)i * D));
   red[grp][c] = sum;
   __syncthreads();
   if (grp == 0) {
 #pragma unroll
     for (int i = 1; i < NG; ++i) {
-      const float4 x = red[i][c];
-      sum.x += x.x;
-      sum.y += x.y;
-      sum.z += x.z;
-      sum.w += x.w;
+      const float4 y = red[i][c];
+      sum.x += y.x;
+      sum.y += y.y;
+      sum.z += y.z;
+      sum.w += y.w;
     }
     const float inv = l == 0.f ? 0.f : 1.f / l;
-    *reinterpret_cast<u32x2*>(O) = u32x2{pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv)};
+    *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o) + bh * D + 4 * c) =
+        u32x2{pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv)};
     if (t == 0) p.lse[bh] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
   }
 }
@@ -415,10 +448,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
 // ---------------------------------------------------------------- launch
 template <int D, int ROPE, bool ALIBI>
 static int launch_one(const PagedParams& p, hipStream_t st) {
-  const dim3 grid((unsigned)((long long)p.nsplit * p.hgroups * p.B * p.Hkv));
+  const dim3 grid((unsigned)p.nsplit, (unsigned)(p.Hkv * p.hgroups), (unsigned)p.B);
   if (p.table) hipLaunchKernelGGL((paged_split_kernel<D, ROPE, ALIBI, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((paged_split_kernel<D, ROPE, ALIBI, false>), grid, dim3(256), 0, st, p);
-  if (p.nsplit > 1) hipLaunchKernelGGL((paged_join_kernel<D>), dim3((unsigned)(p.B * p.H)), dim3(256), 0, st, p);
+  if (p.nsplit > 1) hipLaunchKernelGGL((paged_join_kernel<D, 4>), dim3((unsigned)p.H, (unsigned)p.B), dim3(256), 0, st, p);
   return hipGetLastError() == hipSuccess ? 0 : -3;
 }
 

@@ -133,8 +133,8 @@ struct PagedParams {
   float* part_acc;        // workspace [B, H, nsplit, D]
   int B, H, Hkv, S;       // S: the most keys a sequence may have
   int window, sinks;      // window 0: every cached key; sinks: first keys that stay visible
-  int chunk, nsplit;      // visible 32-key tiles per workgroup; workgroups per sequence and head group
-  int hgroups;            // groups of up to 32 query heads of a K/V head
+  int nsplit;             // workgroups that share a sequence's tiles for a head group
+  int G, hgroups;         // query heads of a K/V head, and their groups of up to 32
   const float* slopes;
   float scale;
   const float2* rope;     // [rows >= S][D/2] (cos, sin)

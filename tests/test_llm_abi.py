@@ -148,9 +148,9 @@ def test_qknorm_workspace_bytes():
 def test_decode_workspace_bytes():
     f = _lib.load().attnfuse_decode_paged_workspace_bytes
     assert f(1, 4, 2, 128, 64, 0, 0) == 256 + 4 * 64 * 4              # one part: four tiles
-    assert f(1, 4, 2, 129, 64, 0, 0) == 256 + 4 * 2 * 64 * 4          # two
+    assert f(1, 4, 2, 256, 64, 0, 0) == 256 + 4 * 2 * 64 * 4          # two, of four tiles each
     assert f(1, 4, 2, 1 << 20, 64, 32, 4) == 256 + 4 * 64 * 4         # a window's two tiles and the sinks'
-    assert f(1, 4, 2, 1 << 20, 64, 97, 4) == 256 + 4 * 2 * 64 * 4
+    assert f(1, 4, 2, 1 << 20, 64, 193, 4) == 256 + 4 * 2 * 64 * 4    # its seven, and the sinks'
     for bad in ((0, 4, 2, 128, 64, 0, 0), (1, 3, 2, 128, 64, 0, 0), (1, 4, 2, 0, 64, 0, 0), (1, 4, 2, 128, 64, -1, 0),
                 (1, 4, 2, 128, 64, 0, -1)):
         assert f(*bad) == 0
