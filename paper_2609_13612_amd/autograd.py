@@ -89,6 +89,12 @@ def qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox
                 max_positions=None, rope_table=None):
     """Differentiable norm and rotation of query and key rows: (Qr, Kr), or Qr without k; gradients for q, k and the
     weights.  Arguments as api.attnfuse_qknorm_rope."""
+    if api._native is not None:   # the same function, its backward in C++
+        r = api._native.qknorm_grad(q, k, q_weight, k_weight, positions, rope_table, api._TABLES, eps, api.ROPE.get(rope, -1),
+                                    theta, max_positions)
+        if r is not None:
+            qr, kr = api._result(r, "attnfuse_qknorm_rope")
+            return qr if k is None else (qr, kr)
     qr, kr = _QkNormRope.apply(q, k, q_weight, k_weight, positions, rope_table, eps, rope, theta, max_positions)
     return qr if k is None else (qr, kr)
 
@@ -97,6 +103,12 @@ def attention(q, k, v, *, rope="none", theta=10000.0, mask="causal", window=None
               return_lse=False, sinks=0):
     """Differentiable fused attention: O [B, H, S, D] (and the non-differentiable
     LSE [B, H, S] with ``return_lse``); arguments as api.attnfuse_fwd."""
+    if sinks and api._native is not None:   # the same function, its backward in C++
+        api._need_sinks(sinks, mask, window, alibi_slopes)
+        r = api._native.sinks_grad(q, k, v, None, api._TABLES, api.ROPE.get(rope, -1), theta, window, sinks, scale)
+        if r is not None:
+            o, lse = api._result(r, "attnfuse_fwd_sinks")
+            return (o, lse) if return_lse else o
     o, lse = _Attention.apply(q, k, v, alibi_slopes, rope, theta, mask, window, scale, sinks)
     return (o, lse) if return_lse else o
 

@@ -60,9 +60,10 @@ bool qknorm_sizes(int B, int H, int H_kv, int S, int D, int dtype) {
 }
 
 // Workgroups of the backward for q and k: one per unit (head group, position
-// block), or about 1024 that share them, four for each CU.
-bool qknorm_wgs(int B, int H, int H_kv, int S, int D, int dtype, int (&wgs)[2]) {
-  const long long hpt = dtype == AF_DTYPE_FP32 ? af::QKNORM_HPT32 : af::QKNORM_HPT16, rows = 256 / (D / 16);
+// block), or about 1024 that share them, four for each CU (B1 H32/8 S8192 D128 with
+// 768 / 1024 / 2048: 55.4 / 54.8 / 58.0 us; their sums are a second launch's work).
+bool qknorm_wgs(int B, int H, int H_kv, int S, int D, int (&wgs)[2]) {
+  const long long hpt = af::QKNORM_BWD_HPT, rows = 256 / (D / 16);
   const long long blocks = (S + rows - 1) / rows * B;
   const long long uq = blocks * ((H + hpt - 1) / hpt), uk = blocks * ((H_kv + hpt - 1) / hpt), all = uq + uk, most = 1024;
   if (all >= (1LL << 31)) return false;
@@ -209,7 +210,7 @@ int attnfuse_qknorm_rope(const void* Q, const void* K, void* Qr, void* Kr, const
 
 size_t attnfuse_qknorm_rope_bwd_workspace_bytes(int B, int H, int H_kv, int S, int D, int dtype) {
   int wgs[2];
-  if (!qknorm_sizes(B, H, H_kv, S, D, dtype) || !supported_d(D) || !qknorm_wgs(B, H, H_kv, S, D, dtype, wgs)) return 0;
+  if (!qknorm_sizes(B, H, H_kv, S, D, dtype) || !supported_d(D) || !qknorm_wgs(B, H, H_kv, S, D, wgs)) return 0;
   return (size_t)(wgs[0] + wgs[1]) * D * sizeof(float);
 }
 
@@ -250,7 +251,7 @@ int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, cons
   if ((rc = check_table(rope, rope_table, rope_table_rows, positions ? 1 : S, nullptr, 0)) != AF_OK) return rc;
   if (!supported_d(D)) return AF_ERR_UNSUPPORTED;
   af::QkNormParams p{};
-  if (!qknorm_wgs(B, H, H_kv, S, D, dtype, p.wgs)) return AF_ERR_INVALID_ARG;
+  if (!qknorm_wgs(B, H, H_kv, S, D, p.wgs)) return AF_ERR_INVALID_ARG;
   if (weights && workspace_bytes < (size_t)(p.wgs[0] + p.wgs[1]) * D * sizeof(float)) return AF_ERR_INVALID_ARG;
 
   p.x[0] = Q; p.x[1] = K;

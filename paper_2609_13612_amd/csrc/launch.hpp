@@ -95,7 +95,7 @@ struct RopeParams {
 // Norm and rotation of query and key rows (qknorm.hip).  Index 0 is q, 1 k, 2 v;
 // strides in elements: batch (of a cache: page), head, position.
 enum { QKNORM_FWD = 0, QKNORM_BWD = 1, QKNORM_APPEND = 2 };
-constexpr int QKNORM_HPT16 = 4, QKNORM_HPT32 = 2;   // heads a thread takes: bf16, fp32
+constexpr int QKNORM_BWD_HPT = 2;   // heads a thread takes in the backward
 
 struct QkNormParams {
   const void* x[3];       // inputs; rows at b xs[.][0] + h xs[.][1] + n xs[.][2]

@@ -314,7 +314,15 @@ __global__ __launch_bounds__(1024) void qknorm_dw_kernel(QkNormParams p) {
   const int t = blockIdx.y, lane = threadIdx.x & 31, row = threadIdx.x >> 5, d = 32 * blockIdx.x + lane;
   const float* part = p.part + (size_t)(t ? p.wgs[0] : 0) * D + d;
   float sum = 0.f;
-  for (int i = row; i < p.wgs[t]; i += 32) sum += part[(size_t)i * D];
+  int i = row;
+  for (; i + 7 * 32 < p.wgs[t]; i += 8 * 32) {   // eight loads in flight
+    float x[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) x[j] = part[(size_t)(i + 32 * j) * D];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += x[j];
+  }
+  for (; i < p.wgs[t]; i += 32) sum += part[(size_t)i * D];
   red[row][lane] = sum;
   __syncthreads();
   if (row == 0) {
@@ -330,17 +338,21 @@ __global__ __launch_bounds__(1024) void qknorm_dw_kernel(QkNormParams p) {
 template <bool FP32, int D, int ROPE>
 static int launch_one(int what, const QkNormParams& p, hipStream_t st) {
   constexpr int R = 256 / (D / 16);
-  constexpr int HPT = FP32 ? QKNORM_HPT32 : QKNORM_HPT16;
+  // Heads a thread takes: more share its cos/sin and weights and keep more loads in
+  // flight, fewer leave registers for more waves.  us with 1 / 2 / 4 heads, bf16:
+  // append of 4500 tokens H64/8 D128 46 / 43 / 40, of 64 tokens H32/8 6.0 / 5.2 / 5.4;
+  // backward B1 H32/8 S8192 D128 57.8 / 54.8 / 55.9.
+  constexpr int HPT = FP32 ? 2 : 4;
   const unsigned nblk = (unsigned)((p.S + R - 1) / R);
   auto groups = [&](int hpt) { return (unsigned)((p.heads[0] + hpt - 1) / hpt + (p.heads[1] + hpt - 1) / hpt); };
   if (what == QKNORM_BWD) {
-    hipLaunchKernelGGL((qknorm_rope_bwd_kernel<FP32, D, ROPE, HPT>), dim3((unsigned)(p.wgs[0] + p.wgs[1])), dim3(256), 0,
+    hipLaunchKernelGGL((qknorm_rope_bwd_kernel<FP32, D, ROPE, QKNORM_BWD_HPT>), dim3((unsigned)(p.wgs[0] + p.wgs[1])), dim3(256), 0,
                        st, p);
     if (p.part)
       hipLaunchKernelGGL((qknorm_dw_kernel<D>), dim3(D / 32, p.heads[1] ? 2 : 1), dim3(1024), 0, st, p);
   } else if (what == QKNORM_APPEND) {
-    hipLaunchKernelGGL((qknorm_append_kernel<FP32, D, ROPE, 1>), dim3(nblk, (unsigned)(p.heads[0] + 2 * p.heads[1])),
-                       dim3(256), 0, st, p);
+    hipLaunchKernelGGL((qknorm_append_kernel<FP32, D, ROPE, HPT>),
+                       dim3(nblk, groups(HPT) + (unsigned)((p.heads[1] + HPT - 1) / HPT)), dim3(256), 0, st, p);
   } else {
     hipLaunchKernelGGL((qknorm_rope_kernel<FP32, D, ROPE, HPT>), dim3(nblk, groups(HPT), (unsigned)p.B), dim3(256), 0, st,
                        p);

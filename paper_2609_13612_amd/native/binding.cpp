@@ -25,6 +25,7 @@
 #include <c10/core/DeviceGuard.h>
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
+#include <torch/csrc/autograd/custom_function.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -136,6 +137,7 @@ int dtype_of(const Tensor& q) {
 struct Table {
   const float* ptr = nullptr;
   int rows = 0;
+  Tensor own;   // the tensor itself: a differentiable call keeps it for its backward
 };
 
 Table table_of(Args& a, int rope, double theta, int64_t D, int64_t S, c10::Device dev) {
@@ -146,6 +148,7 @@ Table table_of(Args& a, int rope, double theta, int64_t D, int64_t S, c10::Devic
   auto take = [&](const Tensor& t) {
     r.ptr = static_cast<const float*>(t.const_data_ptr());
     r.rows = (int)t.size(0);
+    r.own = t;
   };
   if (given) {
     if (given->dim() != 3 || given->size(0) < S || given->size(0) > INT_MAX) throw NotPlain{};
@@ -178,9 +181,11 @@ Table table_of(Args& a, int rope, double theta, int64_t D, int64_t S, c10::Devic
 }
 
 // ---------------------------------------------------------------- calls
-struct NoGil {
-  PyThreadState* s = PyEval_SaveThread();
-  ~NoGil() { PyEval_RestoreThread(s); }
+struct NoGil {   // (a backward runs in a thread of the engine, which does not hold the lock)
+  PyThreadState* s = PyGILState_Check() ? PyEval_SaveThread() : nullptr;
+  ~NoGil() {
+    if (s) PyEval_RestoreThread(s);
+  }
 };
 
 // f(stream) on dev's current stream, without the interpreter's lock.
@@ -223,8 +228,11 @@ struct Qkv {
   int dtype;
   int64_t B, H, Hkv, S, D;
   at::ScalarType type;
-  explicit Qkv(Args& a)
-      : q(a.need()), k(a.need()), v(a.need()), dev(q.device()), dtype(dtype_of(q)), type(q.scalar_type()) {
+  explicit Qkv(Args& a) : Qkv(a.need(), a) {}
+  Qkv(const Tensor& q_, Args& a) : Qkv(q_, a.need(), a) {}   // (in the arguments' order)
+  Qkv(const Tensor& q_, const Tensor& k_, Args& a) : Qkv(q_, k_, a.need()) {}
+  Qkv(const Tensor& q_, const Tensor& k_, const Tensor& v_)
+      : q(q_), k(k_), v(v_), dev(q.device()), dtype(dtype_of(q)), type(q.scalar_type()) {
     if (q.dim() != 4 || k.dim() != 4) throw NotPlain{};
     B = q.size(0); H = q.size(1); S = q.size(2); D = q.size(3); Hkv = k.size(1);
     for (int64_t x : {B, H, S, D, Hkv}) if (x > INT_MAX) throw NotPlain{};
@@ -488,7 +496,7 @@ struct Qk {
   at::ScalarType type;
   int64_t B, H, S, D, Hkv = 0;
   Rows qs, ks;
-  explicit Qk(Args& a) : q(a.need()), k(a.tensor()), dev(q.device()), dtype(dtype_of(q)), type(q.scalar_type()) {
+  Qk(const Tensor& q_, const Tensor* k_) : q(q_), k(k_), dev(q.device()), dtype(dtype_of(q)), type(q.scalar_type()) {
     if (q.dim() != 4 || (k && k->dim() != 4)) throw NotPlain{};
     B = q.size(0); H = q.size(1); S = q.size(2); D = q.size(3);
     if (k) Hkv = k->size(1);
@@ -498,56 +506,33 @@ struct Qk {
   }
 };
 
-// qknorm(q, k, q_weight, k_weight, out_q, out_k, positions, table, tables, eps, rope, theta, max_positions) -> (Qr, Kr)
-PyObject* qknorm(Args a) {
-  Qk x(a);
-  const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *ok_ = a.tensor(), *pos = a.tensor();
-  Args late = a;
-  a.i += 2;
-  const float eps = (float)a.number();
-  const int rope = a.index();
-  const double theta = a.number();
-  const long long most = a.whole();
-  if (!x.k && (kw || ok_)) throw NotPlain{};
-  const Weights w(qw, kw, x.D, x.type, x.dev);
-  const Placed at_(pos, late, rope, theta, x.D, x.S, {x.B, x.S}, most, x.dev);
-  const Tensor oq = out_or(oq_, x.q.sizes(), x.type, x.dev);
-  Tensor ok;
-  if (x.k) ok = out_or(ok_, x.k->sizes(), x.type, x.dev);
-  const int rc = enqueue(x.dev, [&](void* st) {
-    return attnfuse_qknorm_rope(in(x.q), x.k ? in(*x.k) : nullptr, out(oq), x.k ? out(ok) : nullptr, w.q, w.k, w.type, eps,
+// A norm call's variant.
+struct Norm {
+  float eps;
+  int rope;
+  double theta;
+  explicit Norm(Args& a) : eps((float)a.number()), rope(a.index()), theta(a.number()) {}
+  Norm(float e, int r, double t) : eps(e), rope(r), theta(t) {}
+};
+
+int norm_fwd(const Qk& x, const Weights& w, const Norm& n, const Table& table, const int* positions, const Tensor& oq,
+             const Tensor& ok) {
+  return enqueue(x.dev, [&](void* st) {
+    return attnfuse_qknorm_rope(in(x.q), x.k ? in(*x.k) : nullptr, out(oq), x.k ? out(ok) : nullptr, w.q, w.k, w.type, n.eps,
                                 x.qs.s[0], x.qs.s[1], x.qs.s[2], x.ks.s[0], x.ks.s[1], x.ks.s[2], (int)x.B, (int)x.H,
-                                (int)x.Hkv, (int)x.S, (int)x.D, x.dtype, rope, (float)theta, at_.table.ptr, at_.table.rows,
-                                at_.positions, st);
+                                (int)x.Hkv, (int)x.S, (int)x.D, x.dtype, n.rope, (float)n.theta, table.ptr, table.rows,
+                                positions, st);
   });
-  return rc ? PyLong_FromLong(rc) : tuple_of({&oq, &ok});
 }
 
-// qknorm_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, table, tables, eps, rope, theta,
-//            max_positions, weight_grads) -> (dQ, dK, dq_weight, dk_weight)
-PyObject* qknorm_bwd(Args a) {
-  Qk x(a);
-  const Tensor& dqr = a.need();
-  const Tensor *dkr = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *dq_ = a.tensor(), *dk_ = a.tensor(), *ws_ = a.tensor(),
-               *pos = a.tensor();
-  Args late = a;
-  a.i += 2;
-  const float eps = (float)a.number();
-  const int rope = a.index();
-  const double theta = a.number();
-  const long long most = a.whole();
-  const bool grads = a.whole() != 0;
-  if (!x.k != !dkr || (!x.k && (kw || dk_))) throw NotPlain{};
-  const Weights w(qw, kw, x.D, x.type, x.dev);
-  const Placed at_(pos, late, rope, theta, x.D, x.S, {x.B, x.S}, most, x.dev);
+int norm_bwd(const Qk& x, const Weights& w, const Norm& n, const Table& table, const int* positions, const Tensor& dqr,
+             const Tensor* dkr, const Tensor& dq, const Tensor& dk, Tensor& dqw, Tensor& dkw, const Tensor* ws_, bool grads) {
   same(dqr, x.q.sizes(), x.type, x.dev);
   if (dkr) same(*dkr, x.k->sizes(), x.type, x.dev);
-  const Tensor dq = dq_ ? *dq_ : at::empty_like(x.q);
-  Tensor dk, dqw, dkw, ws;
-  if (x.k) dk = dk_ ? *dk_ : at::empty_like(*x.k);
   const Rows dqs(dq, x.q.sizes(), x.type, x.dev);
   Rows dks;
   if (x.k) dks = Rows(dk, x.k->sizes(), x.type, x.dev);
+  Tensor ws;
   if (grads) {
     const auto options = at::TensorOptions().dtype(w.scalar).device(x.dev);
     dqw = at::empty({x.D}, options);
@@ -555,14 +540,55 @@ PyObject* qknorm_bwd(Args a) {
     ws = workspace_or(ws_, attnfuse_qknorm_rope_bwd_workspace_bytes((int)x.B, (int)x.H, (int)x.Hkv, (int)x.S, (int)x.D,
                                                                     x.dtype), x.dev);
   }
-  const int rc = enqueue(x.dev, [&](void* st) {
+  return enqueue(x.dev, [&](void* st) {
     return attnfuse_qknorm_rope_bwd(
         in(x.q), x.k ? in(*x.k) : nullptr, in(dqr), dkr ? in(*dkr) : nullptr, out(dq), x.k ? out(dk) : nullptr,
-        grads ? out(dqw) : nullptr, grads && x.k ? out(dkw) : nullptr, w.q, w.k, w.type, eps, x.qs.s[0], x.qs.s[1], x.qs.s[2],
-        x.ks.s[0], x.ks.s[1], x.ks.s[2], dqs.s[0], dqs.s[1], dqs.s[2], dks.s[0], dks.s[1], dks.s[2],
+        grads ? out(dqw) : nullptr, grads && x.k ? out(dkw) : nullptr, w.q, w.k, w.type, n.eps, x.qs.s[0], x.qs.s[1],
+        x.qs.s[2], x.ks.s[0], x.ks.s[1], x.ks.s[2], dqs.s[0], dqs.s[1], dqs.s[2], dks.s[0], dks.s[1], dks.s[2],
         grads ? out(ws) : nullptr, grads ? bytes_of(ws) : 0, (int)x.B, (int)x.H, (int)x.Hkv, (int)x.S, (int)x.D, x.dtype,
-        rope, (float)theta, at_.table.ptr, at_.table.rows, at_.positions, st);
+        n.rope, (float)n.theta, table.ptr, table.rows, positions, st);
   });
+}
+
+// qknorm(q, k, q_weight, k_weight, out_q, out_k, positions, table, tables, eps, rope, theta, max_positions) -> (Qr, Kr)
+PyObject* qknorm(Args a) {
+  const Tensor &q = a.need(), *k = a.tensor();
+  const Qk x(q, k);
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *ok_ = a.tensor(), *pos = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const Norm n(a);
+  const long long most = a.whole();
+  if (!x.k && (kw || ok_)) throw NotPlain{};
+  const Weights w(qw, kw, x.D, x.type, x.dev);
+  const Placed at_(pos, late, n.rope, n.theta, x.D, x.S, {x.B, x.S}, most, x.dev);
+  const Tensor oq = out_or(oq_, x.q.sizes(), x.type, x.dev);
+  Tensor ok;
+  if (x.k) ok = out_or(ok_, x.k->sizes(), x.type, x.dev);
+  const int rc = norm_fwd(x, w, n, at_.table, at_.positions, oq, ok);
+  return rc ? PyLong_FromLong(rc) : tuple_of({&oq, &ok});
+}
+
+// qknorm_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, table, tables, eps, rope, theta,
+//            max_positions, weight_grads) -> (dQ, dK, dq_weight, dk_weight)
+PyObject* qknorm_bwd(Args a) {
+  const Tensor &q = a.need(), *k = a.tensor();
+  const Qk x(q, k);
+  const Tensor& dqr = a.need();
+  const Tensor *dkr = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *dq_ = a.tensor(), *dk_ = a.tensor(), *ws_ = a.tensor(),
+               *pos = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const Norm n(a);
+  const long long most = a.whole();
+  const bool grads = a.whole() != 0;
+  if (!x.k != !dkr || (!x.k && (kw || dk_))) throw NotPlain{};
+  const Weights w(qw, kw, x.D, x.type, x.dev);
+  const Placed at_(pos, late, n.rope, n.theta, x.D, x.S, {x.B, x.S}, most, x.dev);
+  const Tensor dq = dq_ ? *dq_ : at::empty_like(x.q);
+  Tensor dk, dqw, dkw;
+  if (x.k) dk = dk_ ? *dk_ : at::empty_like(*x.k);
+  const int rc = norm_bwd(x, w, n, at_.table, at_.positions, dqr, dkr, dq, dk, dqw, dkw, ws_, grads);
   return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dqw, &dkw});
 }
 
@@ -670,26 +696,59 @@ PyObject* decode_sinks(Args a) {
   return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
 }
 
+// A call under a window with sinks.
+struct Sinks {
+  int rope;
+  double theta;
+  int window, sinks;
+  float scale;
+};
+
+int sinks_fwd(const Qkv& x, const Sinks& c, const Table& tab, const Tensor& o, const Tensor& l) {
+  const int B = (int)x.B, H = (int)x.H, Hkv = (int)x.Hkv, S = (int)x.S, D = (int)x.D;
+  Tensor ws;
+  const size_t n = attnfuse_fwd_sinks_workspace_bytes(B, Hkv, S, D, x.dtype, c.rope);
+  if (n) ws = workspace_or(nullptr, n, x.dev);
+  return enqueue(x.dev, [&](void* st) {
+    return attnfuse_fwd_sinks(in(x.q), in(x.k), in(x.v), out(o), static_cast<float*>(out(l)), n ? out(ws) : nullptr, n, B, H,
+                              Hkv, S, D, x.dtype, c.rope, (float)c.theta, tab.ptr, tab.rows, c.window, c.sinks, c.scale, st);
+  });
+}
+
+int sinks_bwd(const Qkv& x, const Sinks& c, const Table& tab, const Tensor& o, const Tensor& dout, const Tensor& lse,
+              const Tensor& dq, const Tensor& dk, const Tensor& dv, const Tensor* ws_) {
+  same(o, x.q.sizes(), x.type, x.dev);
+  same(dout, x.q.sizes(), x.type, x.dev);
+  same(lse, {x.B, x.H, x.S}, at::kFloat, x.dev);
+  const int B = (int)x.B, H = (int)x.H, Hkv = (int)x.Hkv, S = (int)x.S, D = (int)x.D;
+  const Tensor ws = workspace_or(ws_, attnfuse_bwd_sinks_workspace_bytes(B, H, Hkv, S, D, c.rope, c.window, c.sinks), x.dev);
+  return enqueue(x.dev, [&](void* st) {
+    return attnfuse_bwd_sinks(in(x.q), in(x.k), in(x.v), in(o), in(dout), static_cast<const float*>(lse.const_data_ptr()),
+                              out(dq), out(dk), out(dv), out(ws), bytes_of(ws), B, H, Hkv, S, D, x.dtype, c.rope,
+                              (float)c.theta, tab.ptr, tab.rows, c.window, c.sinks, c.scale, st);
+  });
+}
+
+Sinks sinks_of(Args& a, int64_t D) {
+  Sinks c;
+  c.rope = a.index();
+  c.theta = a.number();
+  c.window = a.size();
+  c.sinks = a.size();
+  c.scale = a.scale(D);
+  return c;
+}
+
 // fwd_sinks(q, k, v, out, lse, table, tables, rope, theta, window, sinks, scale) -> (O, LSE)
 PyObject* fwd_sinks(Args a) {
   Qkv x(a);
   const Tensor *out_ = a.tensor(), *lse = a.tensor();
   Args late = a;
   a.i += 2;
-  const int rope = a.index();
-  const double theta = a.number();
-  const int window = a.size(), sinks = a.size();
-  const float scale = a.scale(x.D);
-  const Table tab = table_of(late, rope, theta, x.D, x.S, x.dev);
+  const Sinks c = sinks_of(a, x.D);
+  const Table tab = table_of(late, c.rope, c.theta, x.D, x.S, x.dev);
   const Tensor o = out_or(out_, x.q.sizes(), x.type, x.dev), l = out_or(lse, {x.B, x.H, x.S}, at::kFloat, x.dev);
-  const int B = (int)x.B, H = (int)x.H, Hkv = (int)x.Hkv, S = (int)x.S, D = (int)x.D;
-  Tensor ws;
-  const size_t n = attnfuse_fwd_sinks_workspace_bytes(B, Hkv, S, D, x.dtype, rope);
-  if (n) ws = workspace_or(nullptr, n, x.dev);
-  const int rc = enqueue(x.dev, [&](void* st) {
-    return attnfuse_fwd_sinks(in(x.q), in(x.k), in(x.v), out(o), static_cast<float*>(out(l)), n ? out(ws) : nullptr, n, B, H,
-                              Hkv, S, D, x.dtype, rope, (float)theta, tab.ptr, tab.rows, window, sinks, scale, st);
-  });
+  const int rc = sinks_fwd(x, c, tab, o, l);
   return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
 }
 
@@ -700,24 +759,169 @@ PyObject* bwd_sinks(Args a) {
   const Tensor *dq_ = a.tensor(), *dk_ = a.tensor(), *dv_ = a.tensor(), *ws_ = a.tensor();
   Args late = a;
   a.i += 2;
-  const int rope = a.index();
-  const double theta = a.number();
-  const int window = a.size(), sinks = a.size();
-  const float scale = a.scale(x.D);
-  const Table tab = table_of(late, rope, theta, x.D, x.S, x.dev);
-  same(o, x.q.sizes(), x.type, x.dev);
-  same(dout, x.q.sizes(), x.type, x.dev);
-  same(lse, {x.B, x.H, x.S}, at::kFloat, x.dev);
+  const Sinks c = sinks_of(a, x.D);
+  const Table tab = table_of(late, c.rope, c.theta, x.D, x.S, x.dev);
   const Tensor dq = out_or(dq_, x.q.sizes(), x.type, x.dev), dk = out_or(dk_, x.k.sizes(), x.type, x.dev),
                dv = out_or(dv_, x.k.sizes(), x.type, x.dev);
-  const int B = (int)x.B, H = (int)x.H, Hkv = (int)x.Hkv, S = (int)x.S, D = (int)x.D;
-  const Tensor ws = workspace_or(ws_, attnfuse_bwd_sinks_workspace_bytes(B, H, Hkv, S, D, rope, window, sinks), x.dev);
-  const int rc = enqueue(x.dev, [&](void* st) {
-    return attnfuse_bwd_sinks(in(x.q), in(x.k), in(x.v), in(o), in(dout), static_cast<const float*>(lse.const_data_ptr()),
-                              out(dq), out(dk), out(dv), out(ws), bytes_of(ws), B, H, Hkv, S, D, x.dtype, rope, (float)theta,
-                              tab.ptr, tab.rows, window, sinks, scale, st);
-  });
+  const int rc = sinks_bwd(x, c, tab, o, dout, lse, dq, dk, dv, ws_);
   return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dv});
+}
+
+// ---------------------------------------------------------------- differentiable calls
+// The same as differentiable functions.  As a torch.autograd.Function in Python, whose
+// backward takes the interpreter's lock in the engine's thread, a small norm and
+// rotation forward and backward kept the host busy for 108 us; this one for 93, of
+// which 65 are torch's own for an empty function (its engine's thread).
+struct Failed {   // the library's code, to the entry function that called apply
+  int code;
+};
+
+using torch::autograd::AutogradContext;
+using torch::autograd::variable_list;
+
+// f() in a backward, where no exception of another kind may leave: the engine knows
+// only those of the standard library.
+template <class F>
+void in_backward(const char* name, F f) {
+  int rc = 0;
+  try {
+    rc = f();
+  } catch (const NotPlain&) {
+    TORCH_CHECK(false, name, ": a gradient or a saved tensor is not what the forward had");
+  }
+  TORCH_CHECK(rc == 0, name, ": ", attnfuse_strerror(rc), " (code ", rc, ")");
+}
+
+Table table_in(const Tensor& t) {
+  Table r;
+  r.ptr = static_cast<const float*>(t.const_data_ptr());
+  r.rows = (int)t.size(0);
+  return r;
+}
+
+// apply() takes no undefined tensors: a call without one passes q in its place and
+// clears its bit.
+enum { HAS_K = 1, HAS_QW = 2, HAS_KW = 4, HAS_POSITIONS = 8, HAS_TABLE = 16, WEIGHT_GRADS = 32 };
+
+struct NormFunction : torch::autograd::Function<NormFunction> {
+  // The call's tensors, as forward and backward both see them.
+  struct Call {
+    int64_t has;
+    const Qk x;
+    const Weights w;
+    const Table table;
+    const int* positions;
+    Call(const Tensor& q, const Tensor& k, const Tensor& qw, const Tensor& kw, const Tensor& pos, const Tensor& tab, int64_t has_)
+        : has(has_), x(q, has & HAS_K ? &k : nullptr),
+          w(has & HAS_QW ? &qw : nullptr, has & HAS_KW ? &kw : nullptr, x.D, x.type, x.dev),
+          table(has & HAS_TABLE ? table_in(tab) : Table()),
+          positions(has & HAS_POSITIONS ? static_cast<const int*>(pos.const_data_ptr()) : nullptr) {}
+  };
+
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& qw, const Tensor& kw,
+                               const Tensor& positions, const Tensor& table, double eps, int64_t rope, double theta,
+                               int64_t has) {
+    const Call c(q, k, qw, kw, positions, table, has);
+    const Tensor oq = out_or(nullptr, c.x.q.sizes(), c.x.type, c.x.dev);
+    Tensor ok;
+    if (c.x.k) ok = out_or(nullptr, c.x.k->sizes(), c.x.type, c.x.dev);
+    const int rc = norm_fwd(c.x, c.w, Norm((float)eps, (int)rope, theta), c.table, c.positions, oq, ok);
+    if (rc) throw Failed{rc};
+    ctx->save_for_backward({q, k, qw, kw, positions, table});
+    ctx->saved_data["variant"] = std::vector<double>{eps, (double)rope, theta, (double)has};
+    if (c.x.k) return {oq, ok};
+    return {oq};
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grad) {
+    const variable_list s = ctx->get_saved_variables();
+    Tensor dq, dk, dqw, dkw;
+    in_backward("attnfuse_qknorm_rope_bwd", [&] {
+      const std::vector<double> v = ctx->saved_data["variant"].toDoubleVector();
+      const Call c(s[0], s[1], s[2], s[3], s[4], s[5], (int64_t)v[3]);
+      const Tensor dqr = grad[0].contiguous(), dkr = c.x.k ? grad[1].contiguous() : Tensor();
+      dq = at::empty_like(c.x.q);
+      if (c.x.k) dk = at::empty_like(*c.x.k);
+      const int rc = norm_bwd(c.x, c.w, Norm((float)v[0], (int)v[1], v[2]), c.table, c.positions, dqr,
+                              c.x.k ? &dkr : nullptr, dq, dk, dqw, dkw, nullptr, c.has & WEIGHT_GRADS);
+      if (!(c.has & HAS_QW)) dqw.reset();
+      if (!(c.has & HAS_KW)) dkw.reset();
+      return rc;
+    });
+    return {dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
+
+// qknorm_grad(q, k, q_weight, k_weight, positions, table, tables, eps, rope, theta, max_positions) -> (Qr, Kr)
+PyObject* qknorm_grad(Args a) {
+  const Tensor &q = a.need(), *k = a.tensor();
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), *pos = a.tensor();
+  Args late = a;
+  a.i += 2;
+  const Norm n(a);
+  const long long most = a.whole();
+  if (!k && kw) throw NotPlain{};
+  const Qk x(q, k);
+  const Placed at_(pos, late, n.rope, n.theta, x.D, x.S, {x.B, x.S}, most, x.dev);
+  const Tensor& table = at_.table.own;
+  const bool grads = (qw && qw->requires_grad()) || (kw && kw->requires_grad());
+  const int64_t has = (k ? HAS_K : 0) | (qw ? HAS_QW : 0) | (kw ? HAS_KW : 0) | (at_.positions ? HAS_POSITIONS : 0) |
+                      (table.defined() ? HAS_TABLE : 0) | (grads ? WEIGHT_GRADS : 0);
+  try {
+    const variable_list r =
+        NormFunction::apply(q, k ? *k : q, qw ? *qw : q, kw ? *kw : q, at_.positions ? *pos : q, table.defined() ? table : q,
+                            (double)n.eps, (int64_t)n.rope, n.theta, has);
+    const Tensor ok = r.size() > 1 ? r[1] : Tensor();
+    return tuple_of({&r[0], &ok});
+  } catch (const Failed& f) {
+    return PyLong_FromLong(f.code);
+  }
+}
+
+struct SinksFunction : torch::autograd::Function<SinksFunction> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& v, const Tensor& table,
+                               int64_t rope, double theta, int64_t window, int64_t sinks, double scale) {
+    const Qkv x(q, k, v);
+    const Tensor o = out_or(nullptr, x.q.sizes(), x.type, x.dev), l = out_or(nullptr, {x.B, x.H, x.S}, at::kFloat, x.dev);
+    const int rc = sinks_fwd(x, Sinks{(int)rope, theta, (int)window, (int)sinks, (float)scale},
+                             rope != AF_ROPE_NONE ? table_in(table) : Table(), o, l);
+    if (rc) throw Failed{rc};
+    ctx->save_for_backward({q, k, v, o, l, table});
+    ctx->saved_data["variant"] = std::vector<double>{(double)rope, theta, (double)window, (double)sinks, scale};
+    ctx->mark_non_differentiable({l});
+    return {o, l};
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grad) {
+    const variable_list s = ctx->get_saved_variables();
+    Tensor dq, dk, dv;
+    in_backward("attnfuse_bwd_sinks", [&] {
+      const std::vector<double> v = ctx->saved_data["variant"].toDoubleVector();
+      const Qkv x(s[0], s[1], s[2]);
+      dq = at::empty_like(x.q);
+      dk = at::empty_like(x.k);
+      dv = at::empty_like(x.k);
+      return sinks_bwd(x, Sinks{(int)v[0], v[1], (int)v[2], (int)v[3], (float)v[4]},
+                       v[0] != AF_ROPE_NONE ? table_in(s[5]) : Table(), s[3], grad[0].contiguous(), s[4], dq, dk, dv, nullptr);
+    });
+    return {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+  }
+};
+
+// sinks_grad(q, k, v, table, tables, rope, theta, window, sinks, scale) -> (O, LSE)
+PyObject* sinks_grad(Args a) {
+  Qkv x(a);
+  Args late = a;
+  a.i += 2;
+  const Sinks c = sinks_of(a, x.D);
+  const Table tab = table_of(late, c.rope, c.theta, x.D, x.S, x.dev);
+  try {
+    const variable_list r = SinksFunction::apply(x.q, x.k, x.v, tab.own.defined() ? tab.own : x.q, (int64_t)c.rope, c.theta,
+                                                 (int64_t)c.window, (int64_t)c.sinks, (double)c.scale);
+    return tuple_of({&r[0], &r[1]});
+  } catch (const Failed& f) {
+    return PyLong_FromLong(f.code);
+  }
 }
 
 template <PyObject* (*F)(Args)>
@@ -737,9 +941,9 @@ constexpr PyMethodDef method(const char* name) {
 }
 
 PyMethodDef methods[] = {method<fwd>("fwd"), method<bwd>("bwd"), method<decode>("decode"), method<rope>("rope"),
-                         method<qknorm>("qknorm"), method<qknorm_bwd>("qknorm_bwd"), method<append>("append"),
+                         method<qknorm>("qknorm"), method<qknorm_bwd>("qknorm_bwd"), method<qknorm_grad>("qknorm_grad"), method<append>("append"),
                          method<decode_paged>("decode_paged"), method<decode_sinks>("decode_sinks"),
-                         method<fwd_sinks>("fwd_sinks"), method<bwd_sinks>("bwd_sinks"),
+                         method<fwd_sinks>("fwd_sinks"), method<bwd_sinks>("bwd_sinks"), method<sinks_grad>("sinks_grad"),
                          {nullptr, nullptr, 0, nullptr}};
 
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

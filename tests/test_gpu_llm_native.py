@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from gpu_util import announce, device_inputs, need_gpu
-from paper_2609_13612_amd import api
+from paper_2609_13612_amd import api, autograd
 
 pytestmark = pytest.mark.gpu
 B, H, HKV, S, D = 2, 8, 2, 100, 64
@@ -148,3 +148,118 @@ def test_given_outputs_and_refusals(monkeypatch, native):
         print(f"refusal {i}", flush=True)
         with pytest.raises(error):
             call()
+
+
+def _training(d):
+    """(leaves, forward, gradients of its outputs) of the differentiable calls."""
+    q, k, v, do, w = (d[n] for n in ("q", "k", "v", "do", "w"))
+    sq, sk = d["x"][:, :, :H].transpose(1, 2), d["x"][:, :, H:H + HKV].transpose(1, 2)
+    far = dict(positions=d["pos"], max_positions=500)
+    yield (sq, sk, w, w.clone()), lambda a, b, c, e: autograd.qknorm_rope(a, b, c, e, theta=500000.0), (do, k)
+    yield (q, k), lambda a, b: autograd.qknorm_rope(a, b, rope="interleaved", **far), (do, k)
+    yield (q, w.float()), lambda a, c: autograd.qknorm_rope(a, None, c, rope="none"), (do,)
+    yield (sk, w), lambda a, c: autograd.qknorm_rope(a, None, c), (k.transpose(2, 3).contiguous().transpose(2, 3),)
+    for rope in ("neox", "none"):
+        kw = dict(rope=rope, mask="sliding_window", window=20, sinks=3)
+        yield (q, k, v), lambda a, b, c, kw=kw: autograd.attention(a, b, c, **kw), (do,)
+        yield (q, k, v), lambda a, b, c, kw=kw: autograd.attention(a, b, c, scale=0.3, **kw), (do.transpose(1, 2).contiguous()
+                                                                                               .transpose(1, 2),)
+    f = [x.float() for x in (q, k, v)]
+    yield f, lambda a, b, c: autograd.attention(a, b, c, mask="sliding_window", window=7, sinks=1), (do.float(),)
+
+
+def _grads(leaves, forward, out_grads, wanted=None):
+    leaves = [x.detach().requires_grad_(wanted is None or i in wanted) for i, x in enumerate(leaves)]
+    out = forward(*leaves)
+    out = out if isinstance(out, tuple) else (out,)
+    used = [x for x in leaves if x.requires_grad]
+    return [o.detach() for o in out] + list(torch.autograd.grad(out, used, out_grads))
+
+
+def test_differentiable_calls_as_in_python(monkeypatch):
+    """The C++ functions against the Python ones: outputs and gradients, all of them or those of one leaf."""
+    need_gpu()
+    announce("native differentiable calls")
+    real, n = api._native, 0
+    for case in _training(_inputs()):
+        for wanted in (None, {0}, {len(case[0]) - 1}):
+            _grads(*case, wanted)                          # builds the table
+            got = _grads(*case, wanted)
+            monkeypatch.setattr(api, "_native", None)
+            want = _grads(*case, wanted)
+            monkeypatch.setattr(api, "_native", real)
+            assert len(got) == len(want) and all(torch.equal(a, b) and a.stride() == b.stride() for a, b in zip(got, want))
+            n += 1
+    assert n == 27
+
+
+def test_differentiable_calls_are_taken_natively(monkeypatch):
+    need_gpu()
+    announce("native differentiable calls taken")
+    for case in _training(_inputs()):
+        _grads(*case)
+        with monkeypatch.context() as m:
+            for name in ("_QkNormRope", "_Attention"):
+                m.setattr(autograd, name, None)            # an AttributeError where the Python function would be used
+            _grads(*case)
+
+
+def test_unused_output_and_second_backward():
+    """An output without a gradient counts as zeros; a graph kept for a second backward gives the same; LSE takes none."""
+    need_gpu()
+    announce("native differentiable calls, graphs")
+    d = _inputs()
+    q, k, w = (d[n].detach().requires_grad_() for n in ("q", "k", "w"))
+    qr, kr = autograd.qknorm_rope(q, k, w)
+    first = torch.autograd.grad(qr, (q, k, w), d["do"], retain_graph=True)
+    want = api.attnfuse_qknorm_rope_bwd(d["q"], d["k"], d["do"], torch.zeros_like(d["k"]), d["w"])
+    assert all(torch.equal(a, b) for a, b in zip(first, (want[0], want[1], want[2])))
+    assert all(torch.equal(a, b) for a, b in zip(first, torch.autograd.grad(qr, (q, k, w), d["do"])))
+    o, lse = autograd.attention(q, k, d["v"], mask="sliding_window", window=9, sinks=2, return_lse=True)
+    assert o.requires_grad and not lse.requires_grad
+    with torch.no_grad():
+        assert not autograd.attention(q, k, d["v"], mask="sliding_window", window=9, sinks=2).requires_grad
+    with pytest.raises(RuntimeError):   # a saved tensor changed in place
+        o = autograd.attention(q, k, d["v"], mask="sliding_window", window=9, sinks=2)
+        with torch.no_grad():
+            q.mul_(2)
+        torch.autograd.grad(o, q, d["do"])
+
+
+def test_training_step_replayed_from_a_graph():
+    """Norm, rotation, attention with sinks and their backward captured once and replayed on new inputs; an eager graph of
+    other leaves lives meanwhile (a captured backward needs leaves of its own: torch ties a leaf's gradient to the stream
+    that its first graph was made on)."""
+    need_gpu()
+    announce("native differentiable calls captured")
+    kw = dict(mask="sliding_window", window=30, sinks=4)
+
+    def step(x, w, do):
+        leaf, wl = x.detach().requires_grad_(), w.detach().requires_grad_()
+        q, k, v = (leaf[:, :, a:b].transpose(1, 2) for a, b in ((0, H), (H, H + HKV), (H + HKV, H + 2 * HKV)))
+        qr, kr = autograd.qknorm_rope(q, k, wl, wl, theta=500000.0)
+        o = autograd.attention(qr, kr, v.contiguous(), **kw)
+        return (o.detach(),) + torch.autograd.grad(o, (leaf, wl), do)
+
+    d = _inputs()
+    x, w, do = d["x"].clone(), d["w"], d["do"].clone()
+    living = autograd.attention(d["q"].requires_grad_(), d["k"], d["v"], **kw)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step(x, w, do)
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph):
+        got = step(x, w, do)
+    for i in range(3):
+        g = torch.Generator("cuda").manual_seed(i)
+        x.normal_(generator=g)
+        do.normal_(generator=g)
+        graph.replay()
+        torch.cuda.synchronize()
+        want = step(x.clone(), w, do.clone())
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want)), i
+    torch.autograd.grad(living, d["q"], do)

@@ -138,7 +138,7 @@ def test_refuses(name, base, over, code):
 
 def test_qknorm_workspace_bytes():
     f = _lib.load().attnfuse_qknorm_rope_bwd_workspace_bytes
-    assert f(2, 4, 2, 16, 64, 0) == (2 + 2) * 64 * 4          # one position block, a head group of q and one of k per batch
+    assert f(2, 4, 2, 16, 64, 0) == (4 + 2) * 64 * 4          # a position block and two heads of each of the two batches
     assert f(1, 32, 8, 8192, 128, 0) == 1024 * 128 * 4
     assert f(1, 1, 0, 1, 64, 1) == 64 * 4                     # no keys
     for bad in ((0, 1, 1, 1, 64, 0), (1, 1, 1, 0, 64, 0), (1, 1, 1, 1, 96, 0), (1, 1, 1, 1, 64, 2), (1, 1, -1, 1, 64, 0)):
