@@ -19,15 +19,18 @@ struct FarCfg {
   static constexpr int NW = 4;
   static constexpr int KS = D / 16, MT = D / 32;
   static constexpr int KP = D + 8;                       // pitch of the resident K' and V rows (16-byte reads)
-  using Tile = AsyncTile<D, 1, 32>;                      // a wave's own 32 query rows
-  static constexpr int TILES = NW * 2 * Tile::ELEMS;     // Q' and dO of each wave
+  static constexpr int TILE = 32 * D;                    // a wave's own 32 query rows, swizzled
+  static constexpr int IPT = 32 * (D / 8) / 64;          // 16-byte chunks of a tile per lane
+  static constexpr int TILES = NW * 2 * TILE;            // Q' and dO of each wave
   static constexpr int SMEM = TILES + 2 * 32 * KP;
   static_assert(SMEM * 2 >= NW * MT * 16 * 64 * 4, "the waves' sums go through the same memory");
 };
 
 // Workgroup = 4 waves, one part of the steps of 32 sinks of one (batch, K/V
-// head).  A wave takes every fourth 32-row query tile of its part, copied to its
-// own LDS: no barriers.  K' and V rows (fp16) are shared.
+// head).  A wave takes every fourth 32-row query tile of its part, through its
+// own LDS: no barriers; the next tile is on its way, in registers, while one is
+// worked on.  K' and V rows (fp16) are shared.  Bound by reading Q' and dO, which the
+// dQ pass has just written.
 template <int D, int ROPE>
 __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
   using C = FarCfg<D>;
@@ -69,33 +72,49 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
   const long long steps = (long long)G * nq;
   const int s_begin = (int)(steps * part / p.far_parts), s_end = (int)(steps * (part + 1) / p.far_parts);
 
-  const typename C::Tile at(lane, 0);
-  uint16_t* Qs = smem + wave * 2 * C::Tile::ELEMS;
-  uint16_t* Os = Qs + C::Tile::ELEMS;
+  uint16_t* Qs = smem + wave * 2 * C::TILE;
+  uint16_t* Os = Qs + C::TILE;
   float (*st)[32] = stat[wave];
-  for (int s = s_begin + wave; s < s_end; s += C::NW) {
+  const SwzLane<D> z(lane);
+  u32x4 qt[C::IPT], ot[C::IPT];   // the tile in flight
+  float stat_t;
+  auto load = [&](int s) {
     const size_t bh = (size_t)b * p.H + g * G + s / nq;
     const int mq = 32 * (tq + s % nq);
-    at.load(static_cast<const uint16_t*>(ROT ? p.qr16 : p.q) + bh * S * D, mq, S, Qs);
-    at.load(static_cast<const uint16_t*>(p.do16) + bh * S * D, mq, S, Os);
-    const int m_own = min(mq + lq, S - 1);
-    st[lg][lq] = (lg ? p.delta : p.lse2)[bh * S + m_own];
-    async_wait();
-    // a query row as an fp16 operand: Q is bf16 without RoPE (exact in fp16's range)
-    auto f16_of = [&](u32x4 x) {
-      if constexpr (!ROT) {
+    const uint16_t* Q = static_cast<const uint16_t*>(ROT ? p.qr16 : p.q) + bh * S * D;
+    const uint16_t* dO = static_cast<const uint16_t*>(p.do16) + bh * S * D;
 #pragma unroll
-        for (int w = 0; w < 4; ++w) x[w] = pack_f16(bf_lo(x[w]), bf_hi(x[w]));
+    for (int i = 0; i < C::IPT; ++i) {
+      const int it = lane + 64 * i;
+      const size_t off = (size_t)min(mq + it / (D / 8), S - 1) * D + 8 * (it % (D / 8));
+      qt[i] = ld16(Q + off);
+      ot[i] = ld16(dO + off);
+    }
+    stat_t = (lg ? p.delta : p.lse2)[bh * S + min(mq + lq, S - 1)];
+  };
+  if (s_begin + wave < s_end) load(s_begin + wave);
+  for (int s = s_begin + wave; s < s_end; s += C::NW) {
+    const int mq = 32 * (tq + s % nq);
+#pragma unroll
+    for (int i = 0; i < C::IPT; ++i) {   // (this wave's earlier reads are done: LDS is in order per wave)
+      const int it = lane + 64 * i, at = swz_at<D>(it / (D / 8), 8 * (it % (D / 8)));
+      u32x4 q = qt[i];
+      if constexpr (!ROT) {              // Q is bf16 without RoPE (exact in fp16's range)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) q[w] = pack_f16(bf_lo(q[w]), bf_hi(q[w]));
       }
-      return x;
-    };
+      *reinterpret_cast<u32x4*>(Qs + at) = q;
+      *reinterpret_cast<u32x4*>(Os + at) = ot[i];
+    }
+    st[lg][lq] = stat_t;
+    if (s + C::NW < s_end) load(s + C::NW);
     f32x16 sc = f32x16{}, dp = f32x16{};
 #pragma unroll
     for (int k = 0; k < C::KS; ++k) {
       const u32x4 bk = *reinterpret_cast<const u32x4*>(Ks + lq * C::KP + 16 * k + 8 * lg);
       const u32x4 bv = *reinterpret_cast<const u32x4*>(Vs + lq * C::KP + 16 * k + 8 * lg);
-      sc = mfma32<true>(f16_of(at.row(Qs, 0, k)), bk, sc);
-      dp = mfma32<true>(at.row(Os, 0, k), bv, dp);
+      sc = mfma32<true>(row_operand_swz<D>(Qs, z, 0, k), bk, sc);
+      dp = mfma32<true>(row_operand_swz<D>(Os, z, 0, k), bv, dp);
     }
     // element r: query mq + 8 (r/4) + 4 lg + r%4, key n
     u32x4 pb[2], db[2];
@@ -121,11 +140,9 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
     for (int hf = 0; hf < 2; ++hf)
 #pragma unroll
       for (int mt = 0; mt < C::MT; ++mt) {
-        dv[mt] = mfma32<true>(at.tr(Os, 16 * hf, mt), pb[hf], dv[mt]);
-        dk[mt] = mfma32<true>(f16_of(at.tr(Qs, 16 * hf, mt)), db[hf], dk[mt]);
+        dv[mt] = mfma32<true>(tr_operand_swz<D>(Os, z, 16 * hf, mt), pb[hf], dv[mt]);
+        dk[mt] = mfma32<true>(tr_operand_swz<D>(Qs, z, 16 * hf, mt), db[hf], dk[mt]);
       }
-    // the next tile's copies must not overtake these reads
-    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
   }
 
   // Sum the waves, 32 dims of dK' and dV each; [wave][tile][element][lane] in the tiles' memory.
