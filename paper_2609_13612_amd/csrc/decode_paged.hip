@@ -39,6 +39,7 @@ struct PagedCfg {
   static constexpr int KS = D / 16;               // MFMA k-steps over the head dimension
   static constexpr int MT = D / 32;               // 32-row output tiles over the head dimension
   static constexpr int VP = D + 16;               // V tile pitch (transpose reads)
+  static constexpr int QP = D + 8;                // pitch of the rotated heads' rows (16-byte reads)
   static constexpr int VT = 32 * VP;              // one wave's V tile (elements)
   static constexpr int VPL = 32 * (D / 8) / 64;   // 16-byte V chunks per lane per tile
   static constexpr int XCH = MT * (NW - 1) * 16 * 64 * 4;   // bytes of the waves' exchange of O: every tile but the own
@@ -74,6 +75,7 @@ void paged_split_kernel(PagedParams p) {
   constexpr int NQ = ROPE == ROPE_NONE ? 1 : 2;   // bf16 parts of the query
   __shared__ __attribute__((aligned(16))) unsigned char smem[C::SMEM];
   __shared__ float xml[2][C::NW][32];             // the waves' max and sum per column
+  __shared__ __attribute__((aligned(16))) uint16_t qs[ROPE == ROPE_NONE ? 8 : NQ * 32 * C::QP];   // the rotated heads
 
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -118,12 +120,23 @@ void paged_split_kernel(PagedParams p) {
   const int step = C::NW * p.nsplit;
   const bool early = PAGED && p.window <= 0;      // its place does not depend on the length
   if (early) pages_of(32 * i, pg);
-  // Query rows (B operand of S^T = K Q'^T): lane holds column lq's head, dims 16s + 8lg .. +7.
+  // Query operand (B of S^T = K Q'^T): lane holds column lq's head, dims 16s + 8lg .. +7.
+  // With RoPE the workgroup rotates its heads once, a thread two pairs of a head (words
+  // qa and qb of the row), and hands them out through LDS.
   u32x4 qreg[NQ][C::KS];
-  {
-    const uint16_t* Qh = static_cast<const uint16_t*>(p.q) + ((size_t)b * p.H + h) * D;
+  const uint32_t* qrows = reinterpret_cast<const uint32_t*>(static_cast<const uint16_t*>(p.q) +
+                                                            ((size_t)b * p.H + g * G + h0) * D);
+  auto word_a = [&](int j) { return (j / (D / 4)) * (D / 2) + (ROPE == ROPE_NEOX ? j % (D / 4) : 2 * (j % (D / 4))); };
+  auto word_b = [&](int j) { return word_a(j) + (ROPE == ROPE_NEOX ? D / 4 : 1); };
+  const int items = nh * (D / 4);
+  uint32_t qa = 0, qb = 0;
+  if constexpr (ROPE == ROPE_NONE) {
+    const uint16_t* Qh = reinterpret_cast<const uint16_t*>(qrows) + (lq % nh) * D;
 #pragma unroll
     for (int s = 0; s < C::KS; ++s) qreg[0][s] = ld16(Qh + 16 * s + 8 * lg);
+  } else {
+    qa = qrows[word_a(min(tid, items - 1))];
+    qb = qrows[word_b(min(tid, items - 1))];
   }
   const int len = p.lens ? uniform_load(p.lens + b) : p.S;
   const Visible vis(p, len);
@@ -174,49 +187,44 @@ void paged_split_kernel(PagedParams p) {
     }
   };
 
+  [[maybe_unused]] float4 cs;                     // cos and sin of a thread's pairs, ahead of the tile's loads
+  [[maybe_unused]] const float2* angles = p.rope + (size_t)pos * (D / 2);
+  if constexpr (ROPE != ROPE_NONE) cs = *reinterpret_cast<const float4*>(angles + 2 * (tid % (D / 4)));
   if (i < n_tiles) {
     if (!early) pages_of(32 * vis.tile(i), pg);
     load_tile(32 * vis.tile(i), pg);
     if (i + step < n_tiles) pages_of(32 * vis.tile(i + step), pn);
   }
 
-  {
-    if constexpr (ROPE != ROPE_NONE) {   // rotate the query and split it
-      const float2* t = p.rope + (size_t)pos * (D / 2);
-      auto split2 = [&](int s, int w, float x0, float x1) {
-        const uint32_t hi = pack_bf16(x0, x1);
-        qreg[0][s][w] = hi;
-        qreg[1][s][w] = pack_bf16(x0 - bf_lo(hi), x1 - bf_hi(hi));
-      };
-      if constexpr (ROPE == ROPE_NEOX) {
-#pragma unroll
-        for (int s = 0; s < C::KS / 2; ++s) {
-          float4 cs[4];
-          load_cs(cs, t + 16 * s + 8 * lg);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            float a0 = bf_lo(qreg[0][s][w]), a1 = bf_hi(qreg[0][s][w]);
-            float b0 = bf_lo(qreg[0][s + C::KS / 2][w]), b1 = bf_hi(qreg[0][s + C::KS / 2][w]);
-            rotate_pair<false>(a0, b0, cs[w].x, cs[w].y);
-            rotate_pair<false>(a1, b1, cs[w].z, cs[w].w);
-            split2(s, w, a0, a1);
-            split2(s + C::KS / 2, w, b0, b1);
-          }
-        }
-      } else {
-#pragma unroll
-        for (int s = 0; s < C::KS; ++s) {
-          float4 cs[2];
-          load_cs(cs, t + 8 * s + 4 * lg);
-#pragma unroll
-          for (int w = 0; w < 4; ++w) {
-            float x0 = bf_lo(qreg[0][s][w]), x1 = bf_hi(qreg[0][s][w]);
-            rotate_pair<false>(x0, x1, (w & 1) ? cs[w >> 1].z : cs[w >> 1].x, (w & 1) ? cs[w >> 1].w : cs[w >> 1].y);
-            split2(s, w, x0, x1);
-          }
-        }
+  if constexpr (ROPE != ROPE_NONE) {
+    for (int j = tid; j < items; j += 256) {      // (256 is a multiple of D / 4: the same pairs of other heads)
+      if (j != tid) {
+        qa = qrows[word_a(j)];
+        qb = qrows[word_b(j)];
       }
+      float x[4] = {bf_lo(qa), bf_hi(qa), bf_lo(qb), bf_hi(qb)};
+      if constexpr (ROPE == ROPE_NEOX) {
+        rotate_pair<false>(x[0], x[2], cs.x, cs.y);
+        rotate_pair<false>(x[1], x[3], cs.z, cs.w);
+      } else {
+        rotate_pair<false>(x[0], x[1], cs.x, cs.y);
+        rotate_pair<false>(x[2], x[3], cs.z, cs.w);
+      }
+      const uint32_t ha = pack_bf16(x[0], x[1]), hb = pack_bf16(x[2], x[3]);
+      const int head = j / (D / 4), a = word_a(j) - head * (D / 2), w = word_b(j) - head * (D / 2);
+      uint32_t* row = reinterpret_cast<uint32_t*>(qs) + head * (C::QP / 2);
+      row[a] = ha;
+      row[w] = hb;
+      row += 32 * C::QP / 2;
+      row[a] = pack_bf16(x[0] - bf_lo(ha), x[1] - bf_hi(ha));
+      row[w] = pack_bf16(x[2] - bf_lo(hb), x[3] - bf_hi(hb));
     }
+    __syncthreads();
+#pragma unroll
+    for (int q = 0; q < NQ; ++q)
+#pragma unroll
+      for (int s = 0; s < C::KS; ++s)
+        qreg[q][s] = *reinterpret_cast<const u32x4*>(qs + (32 * q + lq % nh) * C::QP + 16 * s + 8 * lg);
   }
 
   for (; i < n_tiles; i += step) {
