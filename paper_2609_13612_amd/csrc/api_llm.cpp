@@ -83,6 +83,7 @@ int page_shift_of(int page_size) {
 // ---------------------------------------------------------------- decode
 struct PagedLayout {
   int hgroups, nsplit;
+  bool by_length;
   size_t ml, acc, total;
 };
 
@@ -108,6 +109,12 @@ PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int s
   while (n > 1 && tiles < 4 * n) --n;
   while (units * n < 1024 && tiles >= 64 * n) n *= 2;
   L.nsplit = (int)n;
+  // The longest sequences first, where more workgroups run than are resident (two to a
+  // CU) and each is long enough to pay for the ranking (1 to 2 us of its start).  us
+  // without / with, lengths from a quarter on: B32 H32/8 to 8192 147 / 138, B8 H64/8 to
+  // 32768 141 / 129, B20 H16/16 to 3000 74 / 69, B64 H32/8 to 4000 137 / 128; not
+  // taken: B70 H32/8 to 1500 65 / 70, B48 H12 D64 to 3500 74 / 77, B100 D64 153 / 165.
+  L.by_length = B > 1 && B <= 64 && units * n > 512 && tiles * D >= 4096 * n;
   const size_t parts = (size_t)B * H * L.nsplit;
   L.ml = 0;
   L.acc = align256(parts * 2 * sizeof(float));
@@ -150,6 +157,7 @@ int decode_impl(af::PagedParams& p, const void* Q, const void* K, const void* V,
   p.part_acc = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.acc);
   p.B = B; p.H = H; p.Hkv = H_kv; p.S = S;
   p.window = window; p.sinks = sinks;
+  p.by_length = cache_lens && L.by_length;
   p.nsplit = L.nsplit; p.G = H / H_kv; p.hgroups = L.hgroups;
   p.slopes = alibi_slopes;
   p.scale = softmax_scale;

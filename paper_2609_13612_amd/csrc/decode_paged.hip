@@ -68,6 +68,16 @@ struct Visible {
   __device__ __forceinline__ bool key(int n_) const { return n_ < L && (n_ >= lo || n_ < sinks); }
 };
 
+// The sequence with the r-th most cached keys (the lower index first), of up to 64:
+// where workgroups wait for others to end, the longest start first and the short ones
+// fill the end.  One length a lane, ranked by counting the larger ones.
+__device__ __forceinline__ int nth_longest(const PagedParams& p, int r, int lane) {
+  const int key = lane < p.B ? max(min(p.lens[lane], p.S), 0) * 64 + (63 - lane) : -1;   // (S <= 2^20)
+  int above = 0;
+  for (int j = 0; j < p.B; ++j) above += __builtin_amdgcn_readlane(key, j) > key;
+  return __ffsll((long long)__ballot(key >= 0 && above == r)) - 1;
+}
+
 template <int D, int ROPE, bool ALIBI, bool PAGED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_split_kernel(PagedParams p) {
@@ -80,7 +90,8 @@ void paged_split_kernel(PagedParams p) {
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int lq = lane & 31, lg = lane >> 5;
-  const int split = blockIdx.x, b = blockIdx.z;
+  const int split = blockIdx.x;
+  const int b = p.by_length ? __builtin_amdgcn_readfirstlane(nth_longest(p, blockIdx.z, lane)) : (int)blockIdx.z;
   int g = blockIdx.y, hg = 0;
   if (p.hgroups > 1) {
     hg = g % p.hgroups;

@@ -134,6 +134,7 @@ struct PagedParams {
   int B, H, Hkv, S;       // S: the most keys a sequence may have
   int window, sinks;      // window 0: every cached key; sinks: first keys that stay visible
   int nsplit;             // workgroups that share a sequence's tiles for a head group
+  bool by_length;         // the longest sequences' workgroups first (B <= 64, lens given)
   int G, hgroups;         // query heads of a K/V head, and their groups of up to 32
   const float* slopes;
   float scale;

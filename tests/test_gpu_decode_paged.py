@@ -254,3 +254,21 @@ def test_on_two_streams():
                 got[i] = api.attnfuse_decode_paged(qs[i], *sets[i], rope="neox")
     torch.cuda.synchronize()
     assert all(torch.equal(got[i][j], want[i][j]) for i in range(2) for j in range(2))
+
+
+def test_the_longest_first():
+    """More workgroups than are resident, each with a long share: the sequences are taken by length.  Equal, empty, negative
+    and over-long ones among them; each result is that of the sequence alone."""
+    need_gpu()
+    announce("paged by length")
+    g = torch.Generator().manual_seed(11)
+    B, H, Hkv, S, D, page = 37, 32, 16, 1100, 128, 16
+    lens = torch.randint(1, S + 1, (B,), generator=g).to(torch.int32)
+    lens[3], lens[4], lens[5], lens[6], lens[20], lens[21], lens[36] = 0, -5, 5000, 700, 700, 700, 1
+    k, v, table, flat = cache(B, Hkv, S, D, page, g)
+    q = torch.randn(B, H, D, generator=g).bfloat16().cuda()
+    most = table.shape[1] * page
+    o, lse = api.attnfuse_decode_paged(q, k, v, table, lens.cuda(), rope="neox")
+    for b in range(B):
+        want = decode(q[b], *flat[b], seen_of(int(lens[b]), most, 0, 0), min(int(lens[b]), most) - 1, rope="neox")
+        check(o[b:b + 1], lse[b:b + 1], [want], f"sequence {b}")
