@@ -305,7 +305,8 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
   const FarLayout far = sinks > 0 ? far_layout(B, H, H_kv, S, D, window, sinks) : FarLayout{};   // in front of the rest
   if (workspace_bytes < far.bytes) return AF_ERR_INVALID_ARG;
   workspace_bytes -= far.bytes;
-  if (workspace_bytes < bwd_workspace(B, H, H_kv, S, D, rope).part) return AF_ERR_INVALID_ARG;
+  const int rows16 = sinks > 0 ? AF_ROPE_NEOX : rope;   // with sinks the fp16 rows have their place without RoPE too
+  if (workspace_bytes < bwd_workspace(B, H, H_kv, S, D, rows16).part) return AF_ERR_INVALID_ARG;
   if (!supported_d(D)) return AF_ERR_UNSUPPORTED;
   if (sparse && dtype == AF_DTYPE_FP32) return AF_ERR_UNSUPPORTED;        // block-sparse: bf16 kernels only
   if (ext.kind() != af::EXT_NONE && (dtype == AF_DTYPE_FP32 || alibi_slopes || sparse)) return AF_ERR_UNSUPPORTED;
@@ -314,7 +315,7 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
   af::BwdParams p{};
   p.q = Q; p.k = K; p.v = V; p.o = O; p.dout = dO; p.lse = LSE;
   p.dq = dQ; p.dk = dK; p.dv = dV;
-  const BwdWorkspace ws = bwd_workspace(B, H, H_kv, S, D, rope);
+  const BwdWorkspace ws = bwd_workspace(B, H, H_kv, S, D, rows16);
   char* wb = static_cast<char*>(workspace) + far.bytes;
   p.sinks = sinks;
   p.far = static_cast<float*>(workspace);
@@ -332,8 +333,8 @@ int bwd_impl(const void* Q, const void* K, const void* V, const void* O, const v
     p.part = reinterpret_cast<float*>(wb + ws.part);
   }
   p.dmax_chunks = ws.dmax_chunks < af::DMAX_PARTS ? ws.dmax_chunks : af::DMAX_PARTS;
-  p.qr16 = (rope != AF_ROPE_NONE) ? wb + ws.qr16 : nullptr;
-  p.kr16 = (rope != AF_ROPE_NONE) ? wb + ws.kr16 : nullptr;
+  p.qr16 = (rows16 != AF_ROPE_NONE) ? wb + ws.qr16 : nullptr;
+  p.kr16 = (rows16 != AF_ROPE_NONE) ? wb + ws.kr16 : nullptr;
   p.B = B; p.H = H; p.Hkv = H_kv; p.S = S;
   // a window of S or more keys is the causal mask; clamping keeps n + window in int range
   p.window = (mask == AF_MASK_SLIDING_WINDOW) ? (window < S ? window : S) : 0;
@@ -478,7 +479,8 @@ int attnfuse_fwd_sinks(const void* Q, const void* K, const void* V, void* O, flo
 size_t attnfuse_bwd_sinks_workspace_bytes(int B, int H, int H_kv, int S, int D, int rope, int window, int sinks) {
   const size_t base = attnfuse_bwd_workspace_bytes(B, H, H_kv, S, D, rope);
   if (base == 0 || window < 1 || sinks < 1) return 0;
-  return base + (all_visible(S, window, sinks) ? 0 : far_layout(B, H, H_kv, S, D, window, sinks).bytes);
+  if (all_visible(S, window, sinks)) return base;
+  return attnfuse_bwd_workspace_bytes(B, H, H_kv, S, D, AF_ROPE_NEOX) + far_layout(B, H, H_kv, S, D, window, sinks).bytes;
 }
 
 int attnfuse_bwd_sinks(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,

@@ -9,8 +9,8 @@
 namespace af {
 
 // Load one lane's row of a bf16 matrix as the MFMA B operand (dims 16s + 8lg..+7),
-// RoPE-rotated in-lane (rotated values rounded to fp16) or, with TO_F16,
-// converted to fp16 unrotated.  Rows >= S give zeros.
+// RoPE-rotated in-lane (rotated values rounded to fp16) or, with TO_F16 or
+// ROPE_F16, converted to fp16 unrotated.  Rows >= S give zeros.
 template <int D, int ROPE, bool TO_F16 = false>
 __device__ __forceinline__ void load_row_operand(u32x4 (&reg)[D / 16], const uint16_t* __restrict__ src,
                                                  const float2* __restrict__ table, int n, int S, int lg) {
@@ -27,7 +27,7 @@ __device__ __forceinline__ void load_row_operand(u32x4 (&reg)[D / 16], const uin
       for (int s = 0; s < KS; ++s) rotate_interleaved8<false, true>(reg[s], table + (size_t)n * (D / 2) + 8 * s + 4 * lg);
     }
   }
-  if constexpr (TO_F16 && ROPE == ROPE_NONE) {
+  if constexpr ((TO_F16 && ROPE == ROPE_NONE) || ROPE == ROPE_F16) {
 #pragma unroll
     for (int s = 0; s < KS; ++s)
 #pragma unroll

@@ -21,7 +21,7 @@ static int launch_one(const BwdParams& p, hipStream_t st) {
 template <int D>
 static int dispatch_rope(int rope, const BwdParams& p, hipStream_t st) {
   switch (rope) {
-    case ROPE_NONE: return launch_one<D, ROPE_NONE>(p, st);
+    case ROPE_F16: return launch_one<D, ROPE_F16>(p, st);
     case ROPE_NEOX: return launch_one<D, ROPE_NEOX>(p, st);
     case ROPE_INTERLEAVED: return launch_one<D, ROPE_INTERLEAVED>(p, st);
   }

@@ -10,6 +10,11 @@
 // split over the queries: the workgroups of 32 sinks share their (query head,
 // query tile) steps and leave fp32 partial sums, which the dK/dV pass adds in
 // their order (no atomics) before it rotates and rounds dK and dV once.
+//
+// Without RoPE K and Q go through the workspace in fp16 too (ROPE_F16), so that the
+// passes copy their tiles straight to LDS in workgroups of four waves: converted as
+// they were staged, by eight, B4 H12 S2001 D64 window 256 took the dQ pass 61 us
+// against 46.
 #include "dq_kernel.hpp"
 
 namespace af {
@@ -31,10 +36,9 @@ struct FarCfg {
 // own LDS: no barriers; the next tile is on its way, in registers, while one is
 // worked on.  K' and V rows (fp16) are shared.  Bound by reading Q' and dO, which the
 // dQ pass has just written.
-template <int D, int ROPE>
+template <int D>
 __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
   using C = FarCfg<D>;
-  constexpr bool ROT = ROPE != ROPE_NONE;    // Q' and K' come rotated (fp16) from the workspace
   __shared__ __attribute__((aligned(16))) uint16_t smem[C::SMEM];
   __shared__ __attribute__((aligned(16))) float stat[C::NW][2][32];   // the tile's LSE (log2 units) and delta
   const int tid = threadIdx.x, lane = tid & 63, lq = lane & 31, lg = lane >> 5;
@@ -48,17 +52,14 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
 
   uint16_t* Ks = smem + C::TILES;
   uint16_t* Vs = Ks + 32 * C::KP;
-  const uint16_t* Kg = static_cast<const uint16_t*>(ROT ? p.kr16 : p.k) + (size_t)bg * S * D;
+  const uint16_t* Kg = static_cast<const uint16_t*>(p.kr16) + (size_t)bg * S * D;
   const uint16_t* Vg = static_cast<const uint16_t*>(p.v) + (size_t)bg * S * D;
   for (int it = tid; it < 32 * (D / 8); it += 256) {
     const int r = it / (D / 8), c = it % (D / 8);
     const size_t off = (size_t)min(nw + r, S - 1) * D + 8 * c;
     u32x4 v = ld16(Vg + off), k = ld16(Kg + off);
 #pragma unroll
-    for (int w = 0; w < 4; ++w) {
-      v[w] = pack_f16(bf_lo(v[w]), bf_hi(v[w]));
-      if constexpr (!ROT) k[w] = pack_f16(bf_lo(k[w]), bf_hi(k[w]));
-    }
+    for (int w = 0; w < 4; ++w) v[w] = pack_f16(bf_lo(v[w]), bf_hi(v[w]));
     *reinterpret_cast<u32x4*>(Vs + r * C::KP + 8 * c) = v;
     *reinterpret_cast<u32x4*>(Ks + r * C::KP + 8 * c) = k;
   }
@@ -81,7 +82,7 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
   auto load = [&](int s) {
     const size_t bh = (size_t)b * p.H + g * G + s / nq;
     const int mq = 32 * (tq + s % nq);
-    const uint16_t* Q = static_cast<const uint16_t*>(ROT ? p.qr16 : p.q) + bh * S * D;
+    const uint16_t* Q = static_cast<const uint16_t*>(p.qr16) + bh * S * D;
     const uint16_t* dO = static_cast<const uint16_t*>(p.do16) + bh * S * D;
 #pragma unroll
     for (int i = 0; i < C::IPT; ++i) {
@@ -98,12 +99,7 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
 #pragma unroll
     for (int i = 0; i < C::IPT; ++i) {   // (this wave's earlier reads are done: LDS is in order per wave)
       const int it = lane + 64 * i, at = swz_at<D>(it / (D / 8), 8 * (it % (D / 8)));
-      u32x4 q = qt[i];
-      if constexpr (!ROT) {              // Q is bf16 without RoPE (exact in fp16's range)
-#pragma unroll
-        for (int w = 0; w < 4; ++w) q[w] = pack_f16(bf_lo(q[w]), bf_hi(q[w]));
-      }
-      *reinterpret_cast<u32x4*>(Qs + at) = q;
+      *reinterpret_cast<u32x4*>(Qs + at) = qt[i];
       *reinterpret_cast<u32x4*>(Os + at) = ot[i];
     }
     st[lg][lq] = stat_t;
@@ -178,7 +174,7 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
 template <int D, int ROPE>
 static int launch_one(const BwdParams& p, hipStream_t st) {
   constexpr int RPB = 256 / (D / 16);
-  const long long rows = (ROPE != ROPE_NONE) ? (long long)p.B * p.Hkv * p.S : 0;
+  const long long rows = (long long)p.B * p.Hkv * p.S;
   const int d_blocks = p.B * p.Hkv * p.dmax_chunks;
   hipLaunchKernelGGL((bwd_pre_kernel<D, ROPE>), dim3((unsigned)(d_blocks + (rows + RPB - 1) / RPB)), dim3(256), 0, st, p,
                      d_blocks);
@@ -191,7 +187,7 @@ static int launch_one(const BwdParams& p, hipStream_t st) {
   hipLaunchKernelGGL((bwd_dq_kernel<D, ROPE, MASK_SINKS, false, false, EXT_NONE>), dim3((unsigned)qblocks), dim3(64 * NW),
                      0, st, pq);
   const long long far = (long long)p.B * p.Hkv * ((p.sinks + 31) / 32) * p.far_parts;
-  hipLaunchKernelGGL((bwd_far_kernel<D, ROPE>), dim3((unsigned)far), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((bwd_far_kernel<D>), dim3((unsigned)far), dim3(256), 0, st, p);
   if (hipGetLastError() != hipSuccess) return -3;
   return launch_bwd_dkdv_sinks(D, ROPE, p, st);
 }
@@ -199,7 +195,7 @@ static int launch_one(const BwdParams& p, hipStream_t st) {
 template <int D>
 static int dispatch_rope(int rope, const BwdParams& p, hipStream_t st) {
   switch (rope) {
-    case ROPE_NONE: return launch_one<D, ROPE_NONE>(p, st);
+    case ROPE_NONE: return launch_one<D, ROPE_F16>(p, st);
     case ROPE_NEOX: return launch_one<D, ROPE_NEOX>(p, st);
     case ROPE_INTERLEAVED: return launch_one<D, ROPE_INTERLEAVED>(p, st);
   }

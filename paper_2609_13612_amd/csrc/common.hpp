@@ -27,7 +27,9 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kLn2 = 0.6931471805599453f;
 
-enum RopeKind { ROPE_NONE = 0, ROPE_NEOX = 1, ROPE_INTERLEAVED = 2 };
+// ROPE_F16: no rotation, but rows pass through the workspace in fp16 as rotated ones do
+// (the backward with sinks; entry points take it as no RoPE).
+enum RopeKind { ROPE_NONE = 0, ROPE_NEOX = 1, ROPE_INTERLEAVED = 2, ROPE_F16 = 3 };
 // MASK_SINKS: a sliding window whose first `sinks` keys stay visible; entry points
 // take it as a window and a number of sinks.
 enum MaskKind { MASK_NONE = 0, MASK_CAUSAL = 1, MASK_SLIDING_WINDOW = 2, MASK_SINKS = 3 };

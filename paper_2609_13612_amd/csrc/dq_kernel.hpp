@@ -71,6 +71,12 @@ __global__ __launch_bounds__(256) void bwd_pre_kernel(BwdParams p, int dmax_bloc
       u32x4 k0 = ld16(Kr + d0), k1 = ld16(Kr + d1);
       if constexpr (ROPE == ROPE_NEOX) {
         rotate_neox8<false, true>(k0, k1, p.table + (size_t)pos * (D / 2) + 8 * c);
+      } else if constexpr (ROPE == ROPE_F16) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          k0[w] = pack_f16(bf_lo(k0[w]), bf_hi(k0[w]));
+          k1[w] = pack_f16(bf_lo(k1[w]), bf_hi(k1[w]));
+        }
       } else {
         rotate_interleaved8<false, true>(k0, p.table + (size_t)pos * (D / 2) + 4 * c);
         rotate_interleaved8<false, true>(k1, p.table + (size_t)pos * (D / 2) + D / 4 + 4 * c);

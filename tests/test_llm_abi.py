@@ -163,7 +163,8 @@ def test_sinks_workspace_bytes():
     assert f(2, 2, 100, 64, 0, 0) == f(2, 2, 100, 64, 1, 1) == f(0, 2, 100, 64, 0, 1) == f(2, 2, 100, 96, 0, 1) == 0
     g, base = lib.attnfuse_bwd_sinks_workspace_bytes, lib.attnfuse_bwd_workspace_bytes
     # 32 sinks of 2 heads: a part for each four steps, of 2 query heads x 4 tiles
-    assert g(1, 4, 2, 128, 64, 0, 10, 32) == base(1, 4, 2, 128, 64, 0) + 2 * 2 * 2 * 32 * 64 * 4
+    # (without RoPE too Q and K pass through the workspace in fp16)
+    assert g(1, 4, 2, 128, 64, 0, 10, 32) == g(1, 4, 2, 128, 64, 1, 10, 32) == base(1, 4, 2, 128, 64, 1) + 2 * 2 * 2 * 32 * 64 * 4
     assert g(1, 4, 2, 128, 64, 0, 100, 28) == base(1, 4, 2, 128, 64, 0)     # every key is visible
     for bad in ((0, 4, 2, 128, 64, 0, 10, 4), (1, 4, 2, 128, 64, 0, 0, 4), (1, 4, 2, 128, 64, 0, 10, 0), (1, 3, 2, 128, 64, 0, 10, 4)):
         assert g(*bad) == 0
