@@ -339,23 +339,29 @@ template <bool FP32, int D, int ROPE>
 static int launch_one(int what, const QkNormParams& p, hipStream_t st) {
   constexpr int R = 256 / (D / 16);
   // Heads a thread takes: more share its cos/sin and weights and keep more loads in
-  // flight, fewer leave registers for more waves.  us with 1 / 2 / 4 heads, bf16:
-  // append of 4500 tokens H64/8 D128 46 / 43 / 40, of 64 tokens H32/8 6.0 / 5.2 / 5.4;
-  // backward B1 H32/8 S8192 D128 57.8 / 54.8 / 55.9.
+  // flight, one is done sooner.  us with 1 / 2 / 4 heads, bf16: append of 4500 tokens
+  // H64/8 D128 46 / 43 / 40 (3384 workgroups with 4); backward B1 H32/8 S8192 D128 57.8 /
+  // 54.8 / 55.9; captured in a graph, append H32/8 D128 with 1 / 4 heads of 1 token 2.5 /
+  // 3.8, 128 2.9 / 4.0, 512 4.1 / 4.7, 1000 5.8 / 6.4 (384 workgroups with 4).
   constexpr int HPT = FP32 ? 2 : 4;
   const unsigned nblk = (unsigned)((p.S + R - 1) / R);
-  auto groups = [&](int hpt) { return (unsigned)((p.heads[0] + hpt - 1) / hpt + (p.heads[1] + hpt - 1) / hpt); };
   if (what == QKNORM_BWD) {
     hipLaunchKernelGGL((qknorm_rope_bwd_kernel<FP32, D, ROPE, QKNORM_BWD_HPT>), dim3((unsigned)(p.wgs[0] + p.wgs[1])), dim3(256), 0,
                        st, p);
     if (p.part)
       hipLaunchKernelGGL((qknorm_dw_kernel<D>), dim3(D / 32, p.heads[1] ? 2 : 1), dim3(1024), 0, st, p);
-  } else if (what == QKNORM_APPEND) {
-    hipLaunchKernelGGL((qknorm_append_kernel<FP32, D, ROPE, HPT>),
-                       dim3(nblk, groups(HPT) + (unsigned)((p.heads[1] + HPT - 1) / HPT)), dim3(256), 0, st, p);
   } else {
-    hipLaunchKernelGGL((qknorm_rope_kernel<FP32, D, ROPE, HPT>), dim3(nblk, groups(HPT), (unsigned)p.B), dim3(256), 0, st,
-                       p);
+    const int nk = what == QKNORM_APPEND ? 2 : 1;   // key tensors: the values go the keys' way
+    auto groups = [&](int hpt) { return (unsigned)((p.heads[0] + hpt - 1) / hpt + nk * ((p.heads[1] + hpt - 1) / hpt)); };
+    const bool one = (long long)nblk * groups(HPT) * p.B < 512;
+    const dim3 grid(nblk, groups(one ? 1 : HPT), (unsigned)p.B);
+    if (what == QKNORM_APPEND) {
+      if (one) hipLaunchKernelGGL((qknorm_append_kernel<FP32, D, ROPE, 1>), grid, dim3(256), 0, st, p);
+      else hipLaunchKernelGGL((qknorm_append_kernel<FP32, D, ROPE, HPT>), grid, dim3(256), 0, st, p);
+    } else {
+      if (one) hipLaunchKernelGGL((qknorm_rope_kernel<FP32, D, ROPE, 1>), grid, dim3(256), 0, st, p);
+      else hipLaunchKernelGGL((qknorm_rope_kernel<FP32, D, ROPE, HPT>), grid, dim3(256), 0, st, p);
+    }
   }
   return hipGetLastError() == hipSuccess ? 0 : -3;
 }

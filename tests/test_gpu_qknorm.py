@@ -46,6 +46,9 @@ CASES = [
     (2, 6, 0, 40, 128, torch.bfloat16, "interleaved", "slice", "rows", False),   # no keys
     (4, 16, 4, 1000, 128, torch.bfloat16, "none", "bhsd", "rows", False),
     (1, 64, 8, 700, 64, torch.bfloat16, "neox", "slice", "rows", True),          # more units than workgroups
+    # several heads a thread, not all of them there for the last
+    (2, 9, 3, 2000, 128, torch.float32, "neox", "slice", "fp32", False),
+    (12, 7, 3, 900, 64, torch.bfloat16, "interleaved", "bshd", "rows", True),
 ]
 
 
@@ -159,6 +162,9 @@ APPENDS = [
     (77, 12, 12, 64, 3, 128, torch.float32, "neox", False, False),
     (1000, 64, 8, 128, 70, 32, torch.bfloat16, "none", True, True),
     (33, 1, 1, 128, 5, 64, torch.float32, "none", False, False),
+    (2000, 11, 5, 128, 130, 16, torch.float32, "neox", True, True),
+    (3000, 13, 3, 64, 50, 64, torch.bfloat16, "neox", True, False),
+    (3000, 25, 7, 64, 50, 64, torch.bfloat16, "interleaved", False, True),
 ]
 
 
