@@ -11,9 +11,9 @@
 // shares of those tiles for one (sequence, K/V head, up to 32 query heads): wave w of
 // share s takes tiles 4 s + w, 4 (s + nsplit) + w, ..., so shares are even whatever
 // the length, the first tile's page is looked up before the length is known, and a
-// sequence's result depends on its own length alone.  The four waves' (max, sum, O) are joined through LDS and
-// leave as one partial per workgroup, or as the result where a sequence is
-// one workgroup's; a second kernel joins the partials.
+// sequence's result depends on its own length alone.  The four waves' (max, sum, O)
+// are joined through LDS and leave as one partial per workgroup, or as the result
+// where a sequence is one workgroup's; a second kernel joins the partials.
 //
 // A tile is two units of 16 keys.  Pages hold a multiple of 16, so a unit lies in
 // one page and its address is wave-uniform: the page numbers are scalar loads,
@@ -28,6 +28,12 @@
 // time, and neither range nor the LSE suffers from a 16-bit query.  P is rounded to
 // bf16 (2^-8 of each weight at most, as the bf16 O is); sums, maxima and O stay
 // fp32 to the end.
+//
+// Measured (K and V bytes of the visible keys over the whole time, D 128, H 32 of 8):
+// 32 sequences of 8192 keys 187 us, 5.7 TB/s; the same with lengths from 2048 to 8192
+// 131 us; one sequence of 4096 keys 8.7 us in a replayed graph and one of 16 keys 5.0,
+// of which a launch is 1.7: there the chain length and page -> K and V -> products ->
+// join -> second kernel is what lasts.
 #include "common.hpp"
 #include "launch.hpp"
 
@@ -42,9 +48,11 @@ struct PagedCfg {
   static constexpr int QP = D + 8;                // pitch of the rotated heads' rows (16-byte reads)
   static constexpr int VT = 32 * VP;              // one wave's V tile (elements)
   static constexpr int VPL = 32 * (D / 8) / 64;   // 16-byte V chunks per lane per tile
-  static constexpr int XCH = MT * (NW - 1) * 16 * 64 * 4;   // bytes of the waves' exchange of O: every tile but the own
-  static constexpr int SMEM = NW * VT * 2 > XCH ? NW * VT * 2 : XCH;
+  static_assert(VT * 2 >= MT * 4 * 32 * 16, "16 columns of a wave's O go through its V tile's memory");
 };
+
+// The bits below bit n.
+__device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
 // A value that no kernel writes while this one runs, at a wave-uniform address: a
 // scalar load.  (A vector load would be waited for with vmcnt, behind every load of
@@ -65,7 +73,6 @@ struct Visible {
     n = ns + ((L + 31) >> 5) - t0;
   }
   __device__ __forceinline__ int tile(int i) const { return i < ns ? i : t0 + i - ns; }
-  __device__ __forceinline__ bool key(int n_) const { return n_ < L && (n_ >= lo || n_ < sinks); }
 };
 
 // The sequence with the r-th most cached keys (the lower index first), of up to 64:
@@ -83,7 +90,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_split_kernel(PagedParams p) {
   using C = PagedCfg<D>;
   constexpr int NQ = ROPE == ROPE_NONE ? 1 : 2;   // bf16 parts of the query
-  __shared__ __attribute__((aligned(16))) unsigned char smem[C::SMEM];
+  __shared__ __attribute__((aligned(16))) uint16_t smem[C::NW * C::VT];
   __shared__ float xml[2][C::NW][32];             // the waves' max and sum per column
   __shared__ __attribute__((aligned(16))) uint16_t qs[ROPE == ROPE_NONE ? 8 : NQ * 32 * C::QP];   // the rotated heads
 
@@ -105,7 +112,7 @@ void paged_split_kernel(PagedParams p) {
   const uint16_t* __restrict__ V = static_cast<const uint16_t*>(p.v) + g * p.vs[1];
   const int* __restrict__ table = PAGED ? p.table + (size_t)b * p.max_pages : nullptr;
 
-  uint16_t* Vw = reinterpret_cast<uint16_t*>(smem) + wave * C::VT;
+  uint16_t* Vw = smem + wave * C::VT;
   const int tr_key = 4 * lg + ((lane & 15) >> 2);
   const int tr_col = 16 * ((lane >> 4) & 1) + 4 * (lane & 3);
 
@@ -242,11 +249,18 @@ void paged_split_kernel(PagedParams p) {
     const int n0 = 32 * vis.tile(i);
     // some key of the tile is not visible: past the end, before the window, or without a page
     const bool edge = n0 + 32 > L || (n0 < vis.lo && n0 + 32 > vis.sinks) || pg[0] < 0 || pg[1] < 0;   // (wave-uniform)
-    auto seen = [&](int r) { return vis.key(n0 + r) && (r < 16 ? pg[0] : pg[1]) >= 0; };
-    if (edge) {   // what lies in rows that are not visible may be anything: 0 x NaN is NaN
+    // Bit k: key n0 + k is visible.  (One wave-uniform mask for V's rows and for S; a test
+    // of each key held registers that the loads in flight want: 8192 keys of 32 sequences,
+    // H 32 of 8, D 128, all in 194 us against 187.)
+    uint32_t seen = ~0u;
+    if (edge) {
+      seen = below(L - n0) & (~below(vis.lo - n0) | below(vis.sinks - n0));
+      if (pg[0] < 0) seen &= 0xffff0000u;
+      if (pg[1] < 0) seen &= 0x0000ffffu;
+      // what lies in rows that are not visible may be anything: 0 x NaN is NaN
 #pragma unroll
       for (int k = 0; k < C::VPL; ++k)
-        if (!seen(k * (512 / D) + lane / (D / 8))) vreg[k] = u32x4{0, 0, 0, 0};
+        if (!(seen >> (k * (512 / D) + lane / (D / 8)) & 1)) vreg[k] = u32x4{0, 0, 0, 0};
     }
 #pragma unroll
     for (int k = 0; k < C::VPL; ++k)   // (this wave's earlier transpose reads are done: LDS is in order per wave)
@@ -256,11 +270,6 @@ void paged_split_kernel(PagedParams p) {
     for (int s = 0; s < C::KS; ++s)
 #pragma unroll
       for (int q = 0; q < NQ; ++q) st = mfma32(kreg[s], qreg[q][s], st);
-    uint32_t hidden = 0;   // bit r: element r's key is not visible
-    if (edge) {
-#pragma unroll
-      for (int r = 0; r < 16; ++r) hidden |= (uint32_t)!seen(8 * (r >> 2) + 4 * lg + (r & 3)) << r;
-    }
     if (i + step < n_tiles) {
       pg[0] = pn[0];
       pg[1] = pn[1];
@@ -276,7 +285,7 @@ void paged_split_kernel(PagedParams p) {
     }
     if (edge) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) st[r] = (hidden >> r) & 1 ? -INFINITY : st[r];
+      for (int r = 0; r < 16; ++r) st[r] = seen >> (4 * lg) >> (8 * (r >> 2) + (r & 3)) & 1 ? st[r] : -INFINITY;
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -314,64 +323,64 @@ void paged_split_kernel(PagedParams p) {
       }
   }
 
-  // Join the waves: each scales its O to the common max and hands the 32-dim
-  // tiles of the other waves over; wave w sums tile w.
+  // Join the waves, 16 columns at a time: each leaves its O of those columns, as 16-byte
+  // pieces [32-dim tile][piece][lane], in the memory of its own V tile, which no other
+  // wave reads; then wave w sums dims 32 w .. of all four, each weighted by 2^(its max
+  // - the common one).  (Sums of whole tiles over 48 KB of LDS, scaled before, took two
+  // barriers: 16 keys of one sequence 5.8 us against 5.5.)
   const float l_tot = pair_sum(l_run);
   if (lg == 0) {
     xml[0][wave][lq] = m_run;
     xml[1][wave][lq] = l_tot;
   }
-  __syncthreads();   // (and every wave is past its V tile: the exchange reuses it)
-  float M = -INFINITY, l = 0.f;
-#pragma unroll
-  for (int w = 0; w < C::NW; ++w) M = fmaxf(M, xml[0][w][lq]);
-#pragma unroll
-  for (int w = 0; w < C::NW; ++w) {
-    const float m = xml[0][w][lq];
-    if (m != -INFINITY) l += xml[1][w][lq] * fast_exp2(m - M);
-  }
-  const float a = (m_run == -INFINITY) ? 0.f : fast_exp2(m_run - M);
-  float* xch = reinterpret_cast<float*>(smem) + lane;
-  auto slot = [&](int from, int mt) { return ((from * (C::MT - 1) + mt - (mt > from)) * 16) * 64; };
-#pragma unroll
-  for (int mt = 0; mt < C::MT; ++mt) {
-    acc[mt] *= a;
-    if (mt != wave || wave >= C::MT) {
-      // (waves past the tiles, at D = 64, hand over every tile: two slots each)
-      const int at = wave < C::MT ? slot(wave, mt) : ((C::MT * (C::MT - 1) + (wave - C::MT) * C::MT + mt) * 16) * 64;
-#pragma unroll
-      for (int r = 0; r < 16; ++r) xch[at + r * 64] = acc[mt][r];
-    }
-  }
-  __syncthreads();
-  if (wave >= C::MT) return;
-  f32x16 o = f32x16{};
-#pragma unroll
-  for (int mt = 0; mt < C::MT; ++mt)
-    if (mt == wave) o = acc[mt];
-#pragma unroll
-  for (int w = 0; w < C::NW; ++w) {
-    if (w == wave) continue;
-    const int at = w < C::MT ? slot(w, wave) : ((C::MT * (C::MT - 1) + (w - C::MT) * C::MT + wave) * 16) * 64;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) o[r] += xch[at + r * 64];
-  }
-  if (lq >= nh) return;
   const size_t bh = (size_t)b * p.H + h;
-  if (p.nsplit == 1) {
-    const float inv = l == 0.f ? 0.f : 1.f / l;
-    uint16_t* O = static_cast<uint16_t*>(p.o) + bh * D + 32 * wave + 4 * lg;
+  for (int c0 = 0; c0 < nh; c0 += 16) {           // (one round for up to 16 heads of a group)
+    const bool mine = lq >= c0 && lq < c0 + 16;
+    const int at = 16 * lg + lq - c0;             // of 32 lanes
+    if (c0 > 0) __syncthreads();                  // the round before has been read
+    if (mine) {
+      float4* own = reinterpret_cast<float4*>(Vw);
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<u32x2*>(O + 8 * q) = u32x2{pack_bf16(o[4 * q] * inv, o[4 * q + 1] * inv),
-                                                   pack_bf16(o[4 * q + 2] * inv, o[4 * q + 3] * inv)};
-    if (wave == 0 && lg == 0) p.lse[bh] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
-  } else {
-    float* dst = p.part_acc + (bh * p.nsplit + split) * D + 32 * wave + 4 * lg;
+      for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
-    for (int q = 0; q < 4; ++q)
-      *reinterpret_cast<float4*>(dst + 8 * q) = float4{o[4 * q], o[4 * q + 1], o[4 * q + 2], o[4 * q + 3]};
-    if (wave == 0 && lg == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (bh * p.nsplit + split)) = float2{M, l};
+        for (int q = 0; q < 4; ++q)
+          own[(4 * mt + q) * 32 + at] = float4{acc[mt][4 * q], acc[mt][4 * q + 1], acc[mt][4 * q + 2], acc[mt][4 * q + 3]};
+    }
+    __syncthreads();
+    if (wave >= C::MT || !mine || lq >= nh) continue;
+    float M = -INFINITY, l = 0.f;
+    float4 o[4] = {};
+#pragma unroll
+    for (int w = 0; w < C::NW; ++w) M = fmaxf(M, xml[0][w][lq]);
+#pragma unroll
+    for (int w = 0; w < C::NW; ++w) {
+      const float m = xml[0][w][lq];
+      const float a = (m == -INFINITY) ? 0.f : fast_exp2(m - M);
+      l = __builtin_fmaf(xml[1][w][lq], a, l);
+      const float4* from = reinterpret_cast<const float4*>(smem + w * C::VT);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const float4 x = from[(4 * wave + q) * 32 + at];
+        o[q].x = __builtin_fmaf(x.x, a, o[q].x);
+        o[q].y = __builtin_fmaf(x.y, a, o[q].y);
+        o[q].z = __builtin_fmaf(x.z, a, o[q].z);
+        o[q].w = __builtin_fmaf(x.w, a, o[q].w);
+      }
+    }
+    if (p.nsplit == 1) {
+      const float inv = l == 0.f ? 0.f : 1.f / l;
+      uint16_t* O = static_cast<uint16_t*>(p.o) + bh * D + 32 * wave + 4 * lg;
+#pragma unroll
+      for (int q = 0; q < 4; ++q)
+        *reinterpret_cast<u32x2*>(O + 8 * q) =
+            u32x2{pack_bf16(o[q].x * inv, o[q].y * inv), pack_bf16(o[q].z * inv, o[q].w * inv)};
+      if (wave == 0 && lg == 0) p.lse[bh] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+    } else {
+      float* dst = p.part_acc + (bh * p.nsplit + split) * D + 32 * wave + 4 * lg;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(dst + 8 * q) = o[q];
+      if (wave == 0 && lg == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * (bh * p.nsplit + split)) = float2{M, l};
+    }
   }
 }
 
