@@ -150,9 +150,10 @@ int splits_that_fit(int n, const BwdWorkspace& w, size_t bytes, size_t kv_elems)
 bool all_visible(int S, int window, int sinks) { return (long long)window + sinks >= S; }
 
 // The pass over the sinks' queries past the window: workgroups that share 32
-// sinks' (query head, 32-row query tile) steps, as many as are resident at once (by
-// their LDS, one to a CU at D = 128, three at D = 64) while each of their waves has a
-// step; and their fp32 partial dK' and dV.
+// sinks' (query head, 32-row query tile) steps, as many as are resident at once (one to
+// a CU by their LDS at D = 128, two by their registers at D = 64) while each of their
+// waves has a step; and their fp32 partial dK' and dV.  B4 H12 S2001 D64 window 256, us
+// for 512 / 768 workgroups: 4 sinks 10.9 / 14.6, 37 sinks 14.6 / 17.0.
 struct FarLayout {
   int parts = 0;
   size_t bytes = 0;
@@ -162,7 +163,7 @@ FarLayout far_layout(int B, int H, int H_kv, int S, int D, int window, int sinks
   FarLayout f;
   const long long blocks = (long long)B * H_kv * ((sinks + 31) / 32);
   const long long steps = (long long)(H / H_kv) * ((S + 31) / 32 - window / 32);
-  long long n = (D == 64 ? 768 : 256) / blocks;
+  long long n = (D == 64 ? 512 : 256) / blocks;
   n = n < steps / 4 ? n : steps / 4;
   f.parts = n < 1 ? 1 : (int)n;
   f.bytes = align256((size_t)blocks * f.parts * 2 * 32 * D * sizeof(float));

@@ -92,10 +92,10 @@ struct PagedLayout {
 // as many, while a share keeps 32 tiles (eight for each wave) and there are fewer
 // than 1024, so that CUs with short sequences take more of the long ones.  A round of
 // tiles takes a lone wave 1.4 us, 124 workgroups saturate the memory, and the
-// second launch costs 5 us.  us with 1 / 2 / 4 / 8 / 16 / 32 shares, and those taken:
-//   B1 H32/8 D128 4096 keys: 50 / 31 / 21 / 16 / 13.5 / 12.6, 32;  B8 H32/8 8192: 102 / 63 / 54 / 56 / 57 / 65, 8
-//   B8 H64/8 lengths 8k to 32k: 357 / 198 / 139 / 132 / 136 / 136, 16;  B32 H32/8 window 1024: 28 / 33 / 36 / 54, 1
-//   B48 H12 D64 3500 keys: 114 / 108 / 102 / 106, 2;  B70 H32/8 lengths to 1500: 64 / 71 / 78 / 100, 1
+// second launch costs 4 us.  us with 1 / 2 / 4 / 8 / 16 / 32 shares, and those taken:
+//   B1 H32/8 D128 4096 keys: 49 / 32 / 21 / 15.5 / 12.2 / 11.1, 32;  B8 H32/8 8192: 102 / 64 / 53 / 52 / 54 / 59, 8
+//   B8 H64/8 lengths 8k to 32k: 356 / 198 / 137 / 129 / 123 / 129, 16;  B32 H32/8 window 1024: 26 / 29 / 32 / 42, 1
+//   B48 H12 D64 3500 keys: 117 / 106 / 100 / 106, 2;  B70 H32/8 lengths to 1500: 60 / 68 / 73 / 88, 1
 PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int sinks) {
   PagedLayout L{};
   L.hgroups = (H / H_kv + 31) / 32;
@@ -111,9 +111,9 @@ PagedLayout paged_layout(int B, int H, int H_kv, int S, int D, int window, int s
   L.nsplit = (int)n;
   // The longest sequences first, where more workgroups run than are resident (two to a
   // CU) and each is long enough to pay for the ranking (1 to 2 us of its start).  us
-  // without / with, lengths from a quarter on: B32 H32/8 to 8192 147 / 138, B8 H64/8 to
-  // 32768 141 / 129, B20 H16/16 to 3000 74 / 69, B64 H32/8 to 4000 137 / 128; not
-  // taken: B70 H32/8 to 1500 65 / 70, B48 H12 D64 to 3500 74 / 77, B100 D64 153 / 165.
+  // without / with, lengths from a quarter on: B32 H32/8 to 8192 139 / 130, B8 H64/8 to
+  // 32768 133 / 122, B20 H16/16 to 3000 68 / 63, B64 H32/8 to 4000 134 / 125; not taken:
+  // B48 H12 D64 to 1000 25.5 / 25.7 and to 3500 73.3 / 73.4.  Even lengths: B32 184.5 / 185.7.
   L.by_length = B > 1 && B <= 64 && units * n > 512 && tiles * D >= 4096 * n;
   const size_t parts = (size_t)B * H * L.nsplit;
   L.ml = 0;

@@ -35,9 +35,12 @@ struct FarCfg {
 // head).  A wave takes every fourth 32-row query tile of its part, through its
 // own LDS: no barriers; the next tile is on its way, in registers, while one is
 // worked on.  K' and V rows (fp16) are shared.  Bound by reading Q' and dO, which the
-// dQ pass has just written.
+// dQ pass has just written: B1 H32/8 S8192 D128 window 1024, 4 sinks 33 us, 117 MB at
+// 3.6 TB/s; small calls by their chain, load -> products -> sums of the waves (B4 H12
+// S2001 D64 window 256, 4 sinks 10.4 us, of 21 MB).
 template <int D>
-__global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(D == 64 ? 2 : 1, D == 64 ? 2 : 1)))
+void bwd_far_kernel(BwdParams p) {
   using C = FarCfg<D>;
   __shared__ __attribute__((aligned(16))) uint16_t smem[C::SMEM];
   __shared__ __attribute__((aligned(16))) float stat[C::NW][2][32];   // the tile's LSE (log2 units) and delta
@@ -49,21 +52,6 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
   const int fb = rest % nfb, bg = rest / nfb;
   const int b = bg / p.Hkv, g = bg % p.Hkv;
   const int nw = 32 * fb, n = nw + lq;       // the block's first key, this lane's key
-
-  uint16_t* Ks = smem + C::TILES;
-  uint16_t* Vs = Ks + 32 * C::KP;
-  const uint16_t* Kg = static_cast<const uint16_t*>(p.kr16) + (size_t)bg * S * D;
-  const uint16_t* Vg = static_cast<const uint16_t*>(p.v) + (size_t)bg * S * D;
-  for (int it = tid; it < 32 * (D / 8); it += 256) {
-    const int r = it / (D / 8), c = it % (D / 8);
-    const size_t off = (size_t)min(nw + r, S - 1) * D + 8 * c;
-    u32x4 v = ld16(Vg + off), k = ld16(Kg + off);
-#pragma unroll
-    for (int w = 0; w < 4; ++w) v[w] = pack_f16(bf_lo(v[w]), bf_hi(v[w]));
-    *reinterpret_cast<u32x4*>(Vs + r * C::KP + 8 * c) = v;
-    *reinterpret_cast<u32x4*>(Ks + r * C::KP + 8 * c) = k;
-  }
-  __syncthreads();
 
   f32x16 dk[C::MT], dv[C::MT];
 #pragma unroll
@@ -94,6 +82,22 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
     stat_t = (lg ? p.delta : p.lse2)[bh * S + min(mq + lq, S - 1)];
   };
   if (s_begin + wave < s_end) load(s_begin + wave);
+
+  uint16_t* Ks = smem + C::TILES;
+  uint16_t* Vs = Ks + 32 * C::KP;
+  const uint16_t* Kg = static_cast<const uint16_t*>(p.kr16) + (size_t)bg * S * D;
+  const uint16_t* Vg = static_cast<const uint16_t*>(p.v) + (size_t)bg * S * D;
+  for (int it = tid; it < 32 * (D / 8); it += 256) {
+    const int r = it / (D / 8), c = it % (D / 8);
+    const size_t off = (size_t)min(nw + r, S - 1) * D + 8 * c;
+    u32x4 v = ld16(Vg + off), k = ld16(Kg + off);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) v[w] = pack_f16(bf_lo(v[w]), bf_hi(v[w]));
+    *reinterpret_cast<u32x4*>(Vs + r * C::KP + 8 * c) = v;
+    *reinterpret_cast<u32x4*>(Ks + r * C::KP + 8 * c) = k;
+  }
+  __syncthreads();
+
   for (int s = s_begin + wave; s < s_end; s += C::NW) {
     const int mq = 32 * (tq + s % nq);
 #pragma unroll
@@ -141,18 +145,21 @@ __global__ __launch_bounds__(256) void bwd_far_kernel(BwdParams p) {
       }
   }
 
-  // Sum the waves, 32 dims of dK' and dV each; [wave][tile][element][lane] in the tiles' memory.
+  // Sum the waves, 32 dims of dK' and dV each; [wave][tile][element][lane] in the tiles'
+  // memory.  Rows past the sinks are neither written here nor read.
   float* xch = reinterpret_cast<float*>(smem) + lane;
   float* dst = p.far + (((size_t)bg * nfb + fb) * p.far_parts + part) * 2 * 32 * D + lq * D + 4 * lg;
 #pragma unroll
   for (int what = 0; what < 2; ++what) {
     __syncthreads();   // every wave is past its tiles, or past the sums of dK'
+    if (n < p.sinks) {
 #pragma unroll
-    for (int mt = 0; mt < C::MT; ++mt)
+      for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
-      for (int r = 0; r < 16; ++r) xch[((wave * C::MT + mt) * 16 + r) * 64] = what ? dv[mt][r] : dk[mt][r];
+        for (int r = 0; r < 16; ++r) xch[((wave * C::MT + mt) * 16 + r) * 64] = what ? dv[mt][r] : dk[mt][r];
+    }
     __syncthreads();
-    if (wave < C::MT) {
+    if (wave < C::MT && n < p.sinks) {
 #pragma unroll
       for (int a = 0; a < 4; ++a) {
         float4 x = {0.f, 0.f, 0.f, 0.f};

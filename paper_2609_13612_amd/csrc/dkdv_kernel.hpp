@@ -176,11 +176,12 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
 #pragma unroll
   for (int i = 0; i < C::MT; ++i) { dk[i] = f32x16{}; dv[i] = f32x16{}; }
   if constexpr (MASK == MASK_SINKS) {   // this pass is the window's pairs: start from the sinks' others (bwd_sinks.hip)
-    if (sp == 0 && nw < p.sinks) {        // (wave-uniform)
+    if (sp == 0 && nw + lq < p.sinks) {   // (the other rows of the partials are not written)
       const int nfb = (p.sinks + 31) / 32;
       const float* src = p.far + ((((size_t)bg * nfb + nw / 32) * p.far_parts * 2 + qh) * 32 + lq) * D + 4 * lg;
       auto add_far = [&](f32x16 (&y)[C::MT]) {
-        for (int j = 0; j < p.far_parts; ++j, src += (size_t)2 * 32 * D)
+#pragma unroll 4
+        for (int j = 0; j < p.far_parts; ++j, src += (size_t)2 * 32 * D)   // (four parts' loads in flight)
 #pragma unroll
           for (int mt = 0; mt < C::MT; ++mt)
 #pragma unroll
