@@ -10,6 +10,9 @@
  *           stride for each dimension but the last, in elements.  The last
  *           dimension is contiguous, every stride is >= 0 and a multiple of 16
  *           bytes, and every pointer 16-byte aligned.
+ * Workspaces hold a call's intermediate results only: any memory will do from call
+ *           to call, but calls that may overlap (on different streams, or replays
+ *           of graphs) need one each.
  * Positions and slots are read on the device and cannot be refused by the
  *           call: each entry point says what one out of range does.
  */
