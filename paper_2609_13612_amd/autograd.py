@@ -8,6 +8,10 @@ attnfuse_bwd on the incoming gradient of O.  Argument marshalling only: every
 step of the computation runs in the HIP kernels, and the gradients are exactly
 those attnfuse_bwd returns.  ALiBi slopes, theta, the window and the scale get
 no gradient.
+
+A backward that is captured into a graph needs leaves of its own: torch keeps a
+leaf's accumulation on the stream that first used it for as long as any eager
+graph of that leaf lives, and work on that stream ends the capture.
 """
 import torch
 

@@ -139,6 +139,25 @@ def test_entries_outside_the_pool_hold_no_keys():
     check(o, lse, refs, "bad pages")
 
 
+def test_pages_that_sequences_share():
+    """A page in several places of the table: a prefix two sequences share, and one page twice in a sequence; 20 and 5 heads
+    a group."""
+    need_gpu()
+    announce("paged: shared pages")
+    g = torch.Generator().manual_seed(9)
+    page, D, most = 32, 128, 6
+    table = torch.tensor([[3, 1, 4, 0, 0, 2], [3, 1, 4, 5, 1, 3]])
+    lens = [180, 97]
+    for H, Hkv in ((20, 1), (10, 2)):
+        k, v = (torch.randn(7, Hkv, page, D, generator=g).bfloat16() for _ in "kv")
+        q = torch.randn(2, H, D, generator=g).bfloat16()
+        o, lse = api.attnfuse_decode_paged(q.cuda(), k.cuda(), v.cuda(), table.to(torch.int32).cuda(),
+                                           torch.tensor(lens, dtype=torch.int32).cuda(), rope="neox")
+        flat = [[x[table[b]].transpose(0, 1).reshape(Hkv, most * page, D) for x in (k, v)] for b in range(2)]
+        check(o, lse, [decode(q[b], *flat[b], seen_of(lens[b], most * page, 0, 0), lens[b] - 1, rope="neox", theta=10000.0,
+                              slopes=None) for b in range(2)], f"shared pages H={H}")
+
+
 def test_a_sequence_does_not_depend_on_the_others():
     need_gpu()
     announce("paged neighbours")
