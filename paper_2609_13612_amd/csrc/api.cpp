@@ -152,8 +152,10 @@ bool all_visible(int S, int window, int sinks) { return (long long)window + sink
 // The pass over the sinks' queries past the window: workgroups that share 32
 // sinks' (query head, 32-row query tile) steps, as many as are resident at once (one to
 // a CU by their LDS at D = 128, two by their registers at D = 64) while each of their
-// waves has a step; and their fp32 partial dK' and dV.  B4 H12 S2001 D64 window 256, us
-// for 512 / 768 workgroups: 4 sinks 10.9 / 14.6, 37 sinks 14.6 / 17.0.
+// waves has a step, 64 parts at most; and their fp32 partial dK' and dV.  B4 H12 S2001
+// D64 window 256, us for 512 / 768 workgroups: 4 sinks 10.9 / 14.6, 37 sinks 14.6 / 17.0.
+// This pass and the sum of its parts, H8/1 D64 window 256, for at most 32 / 64 / 256
+// parts: S3000 22.8 / 23.6 / 38.5, S16000 56.5 / 42.4 / 61.7; D128 S3000 29.8 / 26.6 / 38.3.
 struct FarLayout {
   int parts = 0;
   size_t bytes = 0;
@@ -165,7 +167,7 @@ FarLayout far_layout(int B, int H, int H_kv, int S, int D, int window, int sinks
   const long long steps = (long long)(H / H_kv) * ((S + 31) / 32 - window / 32);
   long long n = (D == 64 ? 512 : 256) / blocks;
   n = n < steps / 4 ? n : steps / 4;
-  f.parts = n < 1 ? 1 : (int)n;
+  f.parts = n < 1 ? 1 : n > 64 ? 64 : (int)n;
   f.bytes = align256((size_t)blocks * f.parts * 2 * 32 * D * sizeof(float));
   return f;
 }

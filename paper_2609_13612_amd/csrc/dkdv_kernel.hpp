@@ -175,8 +175,10 @@ __global__ __launch_bounds__(512) void bwd_dkdv_kernel(BwdParams p) {
   f32x16 dk[C::MT], dv[C::MT];
 #pragma unroll
   for (int i = 0; i < C::MT; ++i) { dk[i] = f32x16{}; dv[i] = f32x16{}; }
-  if constexpr (MASK == MASK_SINKS) {   // this pass is the window's pairs: start from the sinks' others (bwd_sinks.hip)
-    if (sp == 0 && nw + lq < p.sinks) {   // (the other rows of the partials are not written)
+  // With sinks this pass is the window's pairs: start from the sinks' others
+  // (bwd_sinks.hip), which with splits the reduction adds.
+  if constexpr (MASK == MASK_SINKS && !SPLIT) {
+    if (n < p.sinks) {   // (the other rows of the partials are not written)
       const int nfb = (p.sinks + 31) / 32;
       const float* src = p.far + ((((size_t)bg * nfb + nw / 32) * p.far_parts * 2 + qh) * 32 + lq) * D + 4 * lg;
       auto add_far = [&](f32x16 (&y)[C::MT]) {
