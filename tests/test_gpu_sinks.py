@@ -68,6 +68,7 @@ CASES = [
     (2, 2, 2, 1, 64, "bf16", "neox", 1, 1),
     (1, 16, 2, 2100, 128, "bf16", "interleaved", 1024, 16),
     (1, 8, 1, 3000, 64, "bf16", "neox", 256, 4),             # one K/V head: key blocks shared by workgroups
+    (2, 4, 4, 3181, 128, "bf16", "none", 102, 5),            # many parts of the sinks' sums, key blocks not shared
     (1, 4, 2, 300, 64, "fp32", "neox", 32, 3),
     (2, 2, 1, 201, 128, "fp32", "none", 50, 40),
     (1, 3, 3, 150, 64, "fp32", "interleaved", 1, 17),
