@@ -64,7 +64,7 @@ bool qknorm_sizes(int B, int H, int H_kv, int S, int D, int dtype) {
 // 768 / 1024 / 2048: 55.4 / 54.8 / 58.0 us; their sums are a second launch's work).
 bool qknorm_wgs(int B, int H, int H_kv, int S, int D, int (&wgs)[2]) {
   const long long hpt = af::QKNORM_BWD_HPT, rows = 256 / (D / 16);
-  const long long blocks = (S + rows - 1) / rows * B;
+  const long long per = af::qknorm_per(S, D), blocks = (S + rows - 1) / rows * ((B + per - 1) / per);
   const long long uq = blocks * ((H + hpt - 1) / hpt), uk = blocks * ((H_kv + hpt - 1) / hpt), all = uq + uk, most = 1024;
   if (all >= (1LL << 31)) return false;
   const long long q = all <= most ? uq : uq * most / all, k = all <= most ? uk : most - q;

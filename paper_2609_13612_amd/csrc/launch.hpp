@@ -96,6 +96,8 @@ struct RopeParams {
 // strides in elements: batch (of a cache: page), head, position.
 enum { QKNORM_FWD = 0, QKNORM_BWD = 1, QKNORM_APPEND = 2 };
 constexpr int QKNORM_BWD_HPT = 2;   // heads a thread takes in the backward
+// Batches whose rows share a workgroup of 256 / (D / 16) rows: several of them fit.
+inline int qknorm_per(int S, int D) { return 2 * S <= 4096 / D ? 4096 / D / S : 1; }
 
 struct QkNormParams {
   const void* x[3];       // inputs; rows at b xs[.][0] + h xs[.][1] + n xs[.][2]
@@ -106,6 +108,7 @@ struct QkNormParams {
   long long xs[3][3], ys[3][3];
   int heads[2];           // H, H_kv (0: no k)
   int B, S;               // append: 1, the tokens
+  int per;                // batches a workgroup takes the rows of (qknorm_per)
   bool w32, norm;         // weights are fp32; append: norm the rows
   float eps;
   const float2* table;    // [rows][D/2] (cos, sin)

@@ -46,6 +46,10 @@ CASES = [
     (2, 6, 0, 40, 128, torch.bfloat16, "interleaved", "slice", "rows", False),   # no keys
     (4, 16, 4, 1000, 128, torch.bfloat16, "none", "bhsd", "rows", False),
     (1, 64, 8, 700, 64, torch.bfloat16, "neox", "slice", "rows", True),          # more units than workgroups
+    # short sequences, several a workgroup: as many as fit, with rows to spare, and a last workgroup that is not full
+    (67, 5, 2, 1, 128, torch.bfloat16, "neox", "slice", "fp32", True),
+    (23, 6, 3, 3, 64, torch.bfloat16, "interleaved", "bhsd", "rows", False),
+    (5, 4, 4, 16, 128, torch.float32, "neox", "bshd", "rows", True),
     # several heads a thread, not all of them there for the last
     (2, 9, 3, 2000, 128, torch.float32, "neox", "slice", "fp32", False),
     (12, 7, 3, 900, 64, torch.bfloat16, "interleaved", "bshd", "rows", True),

@@ -62,7 +62,7 @@ BWD = dict(Q=A, K=A + 0x1000, dQr=A + 0x2000, dKr=A + 0x3000, dQ=A + 0x4000, dK=
            S=S, D=D, dtype=0, rope=1, theta=1e4, table=TABLE, rows=S, positions=None, stream=None)
 BWD_BAD = {
     INVALID: [dict(Q=None), dict(dQr=None), dict(dKr=None), dict(dQ=None), dict(dK=None), dict(dkw=None), dict(dqw=None),
-              dict(ws=None), dict(ws=ODD), dict(wbytes=(2 + 2) * D * 4 - 1), dict(dQ=A), dict(dK=A + 0x3000),
+              dict(ws=None), dict(ws=ODD), dict(wbytes=(2 + 1) * D * 4 - 1), dict(dQ=A), dict(dK=A + 0x3000),
               dict(dQ=A + 0x5000), dict(ws=A + 0x6000), dict(ws=TABLE), dict(dqs=D - 8), dict(dqh=0), dict(dkb=8),
               dict(qs=4), dict(dqs=D + 4), dict(eps=NAN), dict(wtype=-1), dict(H_kv=0), dict(rows=S - 1), dict(dqw=A + 0x6002)],
     UNSUPPORTED: [dict(D=96, dqs=96, dks=96), dict(D=96, dqs=96, K=None, dKr=None, dK=None, dkw=None),
@@ -138,7 +138,9 @@ def test_refuses(name, base, over, code):
 
 def test_qknorm_workspace_bytes():
     f = _lib.load().attnfuse_qknorm_rope_bwd_workspace_bytes
-    assert f(2, 4, 2, 16, 64, 0) == (4 + 2) * 64 * 4          # a position block and two heads of each of the two batches
+    assert f(2, 4, 2, 16, 64, 0) == (2 + 1) * 64 * 4          # two heads each; both batches in one workgroup's 64 rows
+    assert f(2, 4, 2, 33, 64, 0) == (4 + 2) * 64 * 4          # a workgroup for each batch
+    assert f(9, 4, 2, 16, 64, 0) == (6 + 3) * 64 * 4
     assert f(1, 32, 8, 8192, 128, 0) == 1024 * 128 * 4
     assert f(1, 1, 0, 1, 64, 1) == 64 * 4                     # no keys
     for bad in ((0, 1, 1, 1, 64, 0), (1, 1, 1, 0, 64, 0), (1, 1, 1, 1, 96, 0), (1, 1, 1, 1, 64, 2), (1, 1, -1, 1, 64, 0)):
