@@ -184,7 +184,7 @@ size_t attnfuse_decode_paged_workspace_bytes(int B, int H, int H_kv, int S_kv, i
  *                                 max_pages * page_size keys); larger values are
  *                                 clamped to that
  *   O [B,H,D] (bf16), LSE [B,H] fp32; a sequence with no visible key gets O = 0,
- *   LSE = -inf
+ *   LSE = -inf.  A NaN in a query, or in a key that it sees, gives a NaN O and LSE.
  *   workspace                     >= attnfuse_decode_paged_workspace_bytes(B, H,
  *                                 H_kv, max_pages * page_size, D, window, sinks)
  *   mask                          NONE, CAUSAL: every cached key; or

@@ -85,6 +85,18 @@ __device__ __forceinline__ int nth_longest(const PagedParams& p, int r, int lane
   return __ffsll((long long)__ballot(key >= 0 && above == r)) - 1;
 }
 
+// What a partial with maximum m counts in a sum of maximum M.  Scores that are all NaN
+// leave m at -inf, as no visible key does, and NaN in the sums: those are added, times
+// 0, and stay NaN.
+__device__ __forceinline__ float part_weight(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
+
+// Fold the (max, sum) pair (m2, l2) into (m, l).
+__device__ __forceinline__ void merge_stats(float& m, float& l, float m2, float l2) {
+  const float M = fmaxf(m, m2);
+  l = l * part_weight(m, M) + l2 * part_weight(m2, M);
+  m = M;
+}
+
 template <int D, int ROPE, bool ALIBI, bool PAGED>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2, 2)))
 void paged_split_kernel(PagedParams p) {
@@ -354,8 +366,7 @@ void paged_split_kernel(PagedParams p) {
     for (int w = 0; w < C::NW; ++w) M = fmaxf(M, xml[0][w][lq]);
 #pragma unroll
     for (int w = 0; w < C::NW; ++w) {
-      const float m = xml[0][w][lq];
-      const float a = (m == -INFINITY) ? 0.f : fast_exp2(m - M);
+      const float a = part_weight(xml[0][w][lq], M);
       l = __builtin_fmaf(xml[1][w][lq], a, l);
       const float4* from = reinterpret_cast<const float4*>(smem + w * C::VT);
 #pragma unroll
@@ -416,20 +427,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
   }
   for (int i = t + 256; i < n; i += 256) {
     const float2 v = *reinterpret_cast<const float2*>(ml + 2 * i);
-    const float M = fmaxf(m, v.x);
-    if (M != -INFINITY) {
-      l = l * fast_exp2(m - M) + v.y * fast_exp2(v.x - M);
-      m = M;
-    }
+    merge_stats(m, l, v.x, v.y);
   }
 #pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float m2 = __shfl_xor(m, o), l2 = __shfl_xor(l, o), M = fmaxf(m, m2);
-    if (M != -INFINITY) {
-      l = l * fast_exp2(m - M) + l2 * fast_exp2(m2 - M);
-      m = M;
-    }
-  }
+  for (int o = 32; o > 0; o >>= 1) merge_stats(m, l, __shfl_xor(m, o), __shfl_xor(l, o));
   if ((t & 63) == 0) {
     wml[0][t >> 6] = m;
     wml[1][t >> 6] = l;
@@ -440,12 +441,10 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedParams p) {
 #pragma unroll
   for (int w = 0; w < 4; ++w) M = fmaxf(M, wml[0][w]);
 #pragma unroll
-  for (int w = 0; w < 4; ++w)
-    if (wml[0][w] != -INFINITY) l += wml[1][w] * fast_exp2(wml[0][w] - M);
+  for (int w = 0; w < 4; ++w) l = __builtin_fmaf(wml[1][w], part_weight(wml[0][w], M), l);
   float4 sum = {0.f, 0.f, 0.f, 0.f};
   auto fold = [&](float mi, const float4& y) {
-    if (mi == -INFINITY) return;
-    const float w = fast_exp2(mi - M);
+    const float w = part_weight(mi, M);
     sum.x = __builtin_fmaf(w, y.x, sum.x);
     sum.y = __builtin_fmaf(w, y.y, sum.y);
     sum.z = __builtin_fmaf(w, y.z, sum.z);

@@ -291,3 +291,88 @@ def test_the_longest_first():
     for b in range(B):
         want = decode(q[b], *flat[b], seen_of(int(lens[b]), most, 0, 0), min(int(lens[b]), most) - 1, rope="neox")
         check(o[b:b + 1], lse[b:b + 1], [want], f"sequence {b}")
+
+
+# ---------------------------------------------------------------- NaN among what is visible
+def shares(nbytes, B, H, D):
+    """Workgroups that share a sequence, from the workspace: a (max, sum) and D values for each, rounded up."""
+    return nbytes // (B * H * (4 * D + 8))
+
+
+def check_nan(o, lse, ref, nan_heads, what):
+    """O and LSE of one sequence: NaN in every element of the given heads, the reference's values in the others."""
+    O, L, pv, mag = ref
+    bad = torch.zeros(o.shape[0], dtype=torch.bool)
+    bad[nan_heads] = True
+    assert torch.equal(o.cpu().isnan(), bad[:, None].expand(*o.shape)), f"{what}: O's NaN"
+    assert torch.equal(lse.cpu().isnan(), bad), f"{what}: LSE's NaN"
+    check(o[~bad.to(o.device)][None], lse[~bad.to(o.device)][None], [(O[~bad], L[~bad], pv[~bad], mag[~bad])], what)
+
+
+@pytest.mark.parametrize("rope", ["none", "neox"])
+@pytest.mark.parametrize("H,Hkv,D,S,L,split", [(8, 2, 128, 100, 97, 1), (8, 2, 64, 2048, 641, 16), (4, 1, 128, 4096, 4096, 32),
+                                               (6, 3, 64, 4096, 129, 32)])
+def test_a_nan_query_or_key_gives_nan(H, Hkv, D, S, L, split, rope):
+    """NaN scores come out as NaN whether one workgroup takes the sequence or several, which are joined, and never as the
+    result of a sequence without visible keys, which stays O = 0 and LSE = -inf beside them."""
+    need_gpu()
+    announce(f"paged NaN H={H}/{Hkv} D={D} S={S} L={L} {rope}")
+    g = torch.Generator().manual_seed(S + L)
+    G, page = H // Hkv, 16
+    k, v, table, flat = cache(1, Hkv, S, D, page, g)
+    nbytes = api.attnfuse_decode_paged_workspace_bytes(1, H, Hkv, table.shape[1] * page, D)
+    assert shares(nbytes, 1, H, D) == split
+    q = torch.randn(1, H, D, generator=g).bfloat16()
+    lens = torch.tensor([L], dtype=torch.int32).cuda()
+    ref = decode(q[0], *flat[0], torch.arange(L), L - 1, rope=rope)
+    bad = q.clone()
+    bad[0, 1] = float("nan")
+    o, lse = api.attnfuse_decode_paged(bad.cuda(), k, v, table, lens, rope=rope)
+    check_nan(o[0], lse[0], ref, [1], "a NaN query")
+    # one visible key, the last (alone in its tile where L is 32 n + 1), and every key, of the last K/V head
+    for n, what in ((slice(L - 1, L), "the last key NaN"), (slice(0, L), "every key NaN")):
+        kn = k.clone()
+        for i in range(*n.indices(L)):
+            kn[table[0, i // page].long(), Hkv - 1, i % page] = float("nan")
+        o, lse = api.attnfuse_decode_paged(q.cuda(), kn, v, table, lens, rope=rope)
+        check_nan(o[0], lse[0], ref, list(range(H - G, H)), what)
+    for pages, n in ((table, torch.zeros_like(lens)), (torch.full_like(table, -1), lens)):
+        o, lse = api.attnfuse_decode_paged(bad.cuda(), k, v, pages, n, rope=rope)
+        assert not o.any() and torch.isneginf(lse).all(), "no visible key"
+
+
+@pytest.mark.parametrize("S,L,window,sinks,split", [(70, 70, 40, 4, 1), (6000, 5001, 4096, 4, 32)])
+def test_a_nan_query_or_key_gives_nan_in_a_contiguous_cache(S, L, window, sinks, split):
+    need_gpu()
+    announce(f"stream NaN S={S} L={L} W={window} sinks={sinks}")
+    g = torch.Generator().manual_seed(S)
+    H, Hkv, D = 8, 2, 128
+    nbytes = api.attnfuse_decode_paged_workspace_bytes(2, H, Hkv, S, D, window, sinks)
+    assert shares(nbytes, 2, H, D) == split
+    q = torch.randn(2, H, D, generator=g).bfloat16()
+    k, v = (torch.randn(2, Hkv, S, D, generator=g).bfloat16() for _ in "kv")
+    lens = torch.tensor([L, 0], dtype=torch.int32).cuda()
+    ref = decode(q[0], k[0], v[0], seen_of(L, S, window, sinks), L - 1, rope="neox")
+    bad, kn = q.clone(), k.clone()
+    bad[:, 3] = float("nan")
+    kn[0, 0, 1] = float("nan")   # a sink
+    for a, b, heads in ((bad, k, [3]), (q, kn, [0, 1, 2, 3])):
+        o, lse = api.attnfuse_decode(a.cuda(), b.cuda(), v.cuda(), lens, rope="neox", mask="sliding_window", window=window,
+                                     sinks=sinks)
+        check_nan(o[0], lse[0], ref, heads, "stream")
+        assert not o[1].any() and torch.isneginf(lse[1]).all()
+
+
+@pytest.mark.parametrize("S", [100, 4096])
+def test_a_nan_value_gives_nan_in_its_element(S):
+    need_gpu()
+    announce(f"paged NaN value S={S}")
+    g = torch.Generator().manual_seed(S)
+    k, v, table, flat = cache(1, 2, S, 64, 16, g)
+    q = torch.randn(1, 4, 64, generator=g).bfloat16()
+    o, lse = api.attnfuse_decode_paged(q.cuda(), k, v, table)
+    v[table[0, 3].long(), 1, 5, 33] = float("nan")
+    on, ln = api.attnfuse_decode_paged(q.cuda(), k, v, table)
+    assert torch.equal(ln, lse) and on[0, 2:, 33].isnan().all()
+    on[0, 2:, 33] = o[0, 2:, 33]
+    assert torch.equal(on, o)
