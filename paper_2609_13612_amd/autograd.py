@@ -12,10 +12,43 @@ no gradient.
 A backward that is captured into a graph needs leaves of its own: torch keeps a
 leaf's accumulation on the stream that first used it for as long as any eager
 graph of that leaf lives, and work on that stream ends the capture.
+
+There are no second derivatives: under create_graph the gradients are the same,
+and a derivative of them raises a RuntimeError.
 """
+import functools
+
 import torch
 
 from . import api
+
+
+class _Once(torch.autograd.Function):
+    """The first n tensors, as functions of the others that have no derivative."""
+    @staticmethod
+    def forward(ctx, n, *tensors):
+        return tuple(t.data for t in tensors[:n])
+
+    @staticmethod
+    def backward(ctx, *_):
+        raise RuntimeError("the gradients of these operations cannot be differentiated twice")
+
+
+def _once(backward):
+    """A Function's backward whose gradients come from kernels: under create_graph they depend on what they were formed
+    from through _Once.  (torch's once_differentiable ties them to leaves of its own, and not at all where the incoming
+    gradient is a constant: a gradient penalty's term would be lost without a word.)"""
+    @functools.wraps(backward)
+    def run(ctx, *grads):
+        if not torch.is_grad_enabled():
+            return backward(ctx, *grads)
+        with torch.no_grad():
+            out = backward(ctx, *grads)
+        of = [t for t in (*grads, *ctx.saved_tensors) if t is not None and t.requires_grad]
+        given = [x for x in out if x is not None]
+        tied = iter(_Once.apply(len(given), *given, *of))
+        return tuple(None if x is None else next(tied) for x in out)
+    return run
 
 
 class _Attention(torch.autograd.Function):
@@ -29,6 +62,7 @@ class _Attention(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @_once
     def backward(ctx, do, _dlse):
         q, k, v, o, lse, slopes = ctx.saved_tensors
         dq, dk, dv = api.attnfuse_bwd(q, k, v, o, do.contiguous(), lse, alibi_slopes=slopes, **ctx.cfg)
@@ -47,6 +81,7 @@ class _BlockSparseAttention(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @_once
     def backward(ctx, do, _dlse):
         q, k, v, o, lse, slopes = ctx.saved_tensors
         dq, dk, dv = api.attnfuse_bwd_blocksparse(q, k, v, o, do.contiguous(), lse, ctx.block_mask,
@@ -66,6 +101,7 @@ class _BiasNormAttention(torch.autograd.Function):
         return o, lse
 
     @staticmethod
+    @_once
     def backward(ctx, do, _dlse):
         q, k, v, o, lse, bias = ctx.saved_tensors
         dq, dk, dv = api.attnfuse_bwd_bias_norm(q, k, v, o, do.contiguous(), lse, bias=bias, **ctx.cfg)
@@ -80,6 +116,7 @@ class _QkNormRope(torch.autograd.Function):
         return api.attnfuse_qknorm_rope(q, k, q_weight, k_weight, positions=positions, rope_table=rope_table, **ctx.cfg)
 
     @staticmethod
+    @_once
     def backward(ctx, dqr, dkr):
         q, k, qw, kw, positions, table = ctx.saved_tensors
         want = ctx.needs_input_grad

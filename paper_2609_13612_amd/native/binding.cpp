@@ -26,6 +26,8 @@
 #include <c10/hip/HIPStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/custom_function.h>
+#include <torch/csrc/autograd/functions/basic_ops.h>
+#include <torch/csrc/autograd/functions/utils.h>
 #include <torch/csrc/autograd/python_variable.h>
 
 #include <cmath>
@@ -792,6 +794,20 @@ void in_backward(const char* name, F f) {
   TORCH_CHECK(rc == 0, name, ": ", attnfuse_strerror(rc), " (code ", rc, ")");
 }
 
+// The gradients of a backward under create_graph: they come from kernels and have no
+// derivative, so they depend on what they were formed from (`of`, and the incoming
+// gradients) through an error.
+variable_list once(variable_list grads, const variable_list& of, const variable_list& incoming) {
+  if (!at::GradMode::is_enabled()) return grads;
+  const std::shared_ptr<torch::autograd::Node> error(
+      new torch::autograd::Error("the gradients of these operations cannot be differentiated twice",
+                                 torch::autograd::collect_next_edges(of, incoming)),
+      torch::autograd::deleteNode);
+  for (const Tensor& g : grads)
+    if (g.defined()) torch::autograd::set_history(g, error);
+  return grads;
+}
+
 Table table_in(const Tensor& t) {
   Table r;
   r.ptr = static_cast<const float*>(t.const_data_ptr());
@@ -848,7 +864,7 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
       if (!(c.has & HAS_KW)) dkw.reset();
       return rc;
     });
-    return {dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    return once({dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2], s[3]}, grad);
   }
 };
 
@@ -904,7 +920,7 @@ struct SinksFunction : torch::autograd::Function<SinksFunction> {
       return sinks_bwd(x, Sinks{(int)v[0], v[1], (int)v[2], (int)v[3], (float)v[4]},
                        v[0] != AF_ROPE_NONE ? table_in(s[5]) : Table(), s[3], grad[0].contiguous(), s[4], dq, dk, dv, nullptr);
     });
-    return {dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()};
+    return once({dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2]}, grad);
   }
 };
 

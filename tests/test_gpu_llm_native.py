@@ -4,7 +4,7 @@ import pytest
 import torch
 
 from gpu_util import announce, device_inputs, need_gpu
-from paper_2609_13612_amd import api, autograd
+from paper_2609_13612_amd import api, autograd, blockmask
 
 pytestmark = pytest.mark.gpu
 B, H, HKV, S, D = 2, 8, 2, 100, 64
@@ -263,3 +263,51 @@ def test_training_step_replayed_from_a_graph():
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want)), i
     torch.autograd.grad(living, d["q"], do)
+
+
+# ---------------------------------------------------------------- second derivatives
+def _twice(d):
+    """(leaves, forward) of every differentiable operation, the dense and block-sparse attention among them."""
+    q, k, v, w = (d[n] for n in ("q", "k", "v", "w"))
+    blocks = blockmask.block_mask_from_dense(torch.ones(2, 2, dtype=torch.bool), S, device="cuda")
+    bias = torch.zeros(B, 1, S, S, device="cuda")
+    yield (q, k, w, w.clone()), lambda a, b, c, e: autograd.qknorm_rope(a, b, c, e)
+    yield (q, w), lambda a, c: autograd.qknorm_rope(a, None, c, positions=d["pos"], max_positions=500)
+    yield (q, k, v), lambda a, b, c: autograd.attention(a, b, c, mask="sliding_window", window=20, sinks=3)
+    yield (q, k, v), lambda a, b, c: autograd.attention(a, b, c)
+    yield (q, k, v), lambda a, b, c: autograd.blocksparse_attention(a, b, c, blocks)
+    yield (q, k, v), lambda a, b, c: autograd.attention_bias_norm(a, b, c, bias=bias)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_second_derivatives_are_refused(monkeypatch, native):
+    """Under create_graph the gradients are those of a plain backward, and a derivative of them is an error, not a loss of
+    their part: through backward() and through grad() of one leaf, with a constant gradient and one that itself depends on
+    a leaf."""
+    need_gpu()
+    announce(f"second derivatives native={native}")
+    if not native:
+        monkeypatch.setattr(api, "_native", None)
+    for n, (leaves, forward) in enumerate(_twice(_inputs())):
+        print(f"operation {n}", flush=True)
+        leaves = [x.detach().requires_grad_() for x in leaves]
+
+        def loss(power):
+            out = forward(*leaves)
+            return sum((o.float() if power == 1 else o.float().square()).sum() for o in (out if isinstance(out, tuple) else (out,)))
+
+        for power in (1, 2):   # the outputs' gradient: a constant, or the outputs themselves
+            want = torch.autograd.grad(loss(power), leaves)
+            got = torch.autograd.grad(loss(power), leaves, create_graph=True)
+            assert all(torch.equal(a, b) for a, b in zip(got, want))
+            for i, x in enumerate(got):
+                assert x.requires_grad, f"gradient {i} has lost its graph"
+                penalised = x.float().square().sum() + sum(y.float().square().sum() for y in leaves)
+                with pytest.raises(RuntimeError, match="differentiated twice"):
+                    torch.autograd.grad(penalised, leaves[0], retain_graph=True)
+                with pytest.raises(RuntimeError, match="differentiated twice"):
+                    penalised.backward(retain_graph=True)
+        # what does not pass through the gradients is not affected
+        (g,) = torch.autograd.grad(sum(y.float().square().sum() for y in leaves), leaves[0], create_graph=True)
+        torch.autograd.grad(g.float().sum(), leaves[0])
+    assert n == 5
