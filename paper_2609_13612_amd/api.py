@@ -592,13 +592,18 @@ def _norm_weights(qw, kw, D, dtype, device):
 
 
 def _position_table(rope, theta, D, n, device, positions, shape, max_positions, rope_table):
-    """The table of a call whose rows are at `positions`, or at 0..n-1 without any."""
+    """The table of a call whose rows are at `positions`, or at 0..n-1 without any: its first max_positions rows, where
+    that is given, however many more it has."""
     if positions is None or ROPE[rope] == ROPE["none"]:
         return _table(rope, theta, D, n, device, rope_table)
     _need(positions, "positions", shape, torch.int32, device)
     if rope_table is None and max_positions is None:
         raise ValueError("positions need max_positions (every position is below it) or rope_table")
-    return _table(rope, theta, D, 1 if max_positions is None else int(max_positions), device, rope_table)
+    if max_positions is None:
+        return _table(rope, theta, D, 1, device, rope_table)
+    if int(max_positions) < 1:
+        raise ValueError(f"max_positions must be at least 1 (it is {max_positions})")
+    return _table(rope, theta, D, int(max_positions), device, rope_table)[:int(max_positions)]
 
 
 def _qknorm_shape(q, k):
@@ -615,8 +620,9 @@ def _qknorm_shape(q, k):
 def attnfuse_qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0, positions=None,
                          max_positions=None, out_q=None, out_k=None, rope_table=None):
     """Qr, Kr: the rows of q and k over their root mean square, times the weights, rotated at their positions (0..S-1, or
-    ``positions`` int32 [B, S], all below ``max_positions``); see attnfuse_qknorm_rope in include/attnfuse_llm.h.  q and k
-    may be slices whose rows lie apart; Qr and Kr are contiguous."""
+    ``positions`` int32 [B, S], all below ``max_positions``: a row at another one comes out as NaN); see
+    attnfuse_qknorm_rope in include/attnfuse_llm.h.  q and k may be slices whose rows lie apart; Qr and Kr are
+    contiguous."""
     if _native is not None:
         r = _native.qknorm(q, k, q_weight, k_weight, out_q, out_k, positions, rope_table, _TABLES, eps, ROPE.get(rope, -1),
                            theta, max_positions)
@@ -691,7 +697,7 @@ def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None,
                                 rope="neox", theta=10000.0, positions=None, max_positions=None, out_q=None,
                                 rope_table=None):
     """Qr [T, H, D]: the queries of T new tokens, normed (unless ``norm`` is False) and rotated at ``positions`` (int32
-    [T], all below ``max_positions``); their keys, likewise, and values are written to the pages [num_pages, H_kv,
+    [T], all below ``max_positions``, or NaN); their keys, likewise, and values are written to the pages [num_pages, H_kv,
     page_size, D] at ``slots`` (int64 [T]: page * page_size + place; -1: nowhere); see attnfuse_qknorm_rope_append in
     include/attnfuse_llm.h.  q, k, v and the pages may lie apart (a fused projection's slices, pages [num_pages, page_size,
     H_kv, D] transposed)."""

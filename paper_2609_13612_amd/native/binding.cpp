@@ -91,6 +91,12 @@ struct Args {
     }
     return x;
   }
+  long long positive() {   // 0 for None
+    if (i < n && v[i] == Py_None) return whole();
+    const long long x = whole();
+    if (x < 1) throw NotPlain{};
+    return x;
+  }
   int index() {   // an enum's value, or -1 for an unknown name
     const long long x = whole();
     if (x < 0 || x > 2) throw NotPlain{};
@@ -460,8 +466,9 @@ struct Weights {
   }
 };
 
-// Positions and the table of their angles; args: positions, then (at `late`) the
-// table and the binding's tables; n rows at 0..n-1 without positions.
+// Positions and the table of their angles (of its rows the first max_positions, where
+// that is given: not 0); args: positions, then (at `late`) the table and the binding's
+// tables; n rows at 0..n-1 without positions.
 struct Placed {
   const int* positions = nullptr;
   Table table;
@@ -476,6 +483,7 @@ struct Placed {
       n = max_positions > 0 ? max_positions : 1;
     }
     table = table_of(late, rope, theta, D, n, dev);
+    if (pos && max_positions > 0) table.rows = (int)max_positions;
   }
 };
 
@@ -560,7 +568,7 @@ PyObject* qknorm(Args a) {
   Args late = a;
   a.i += 2;
   const Norm n(a);
-  const long long most = a.whole();
+  const long long most = a.positive();
   if (!x.k && (kw || ok_)) throw NotPlain{};
   const Weights w(qw, kw, x.D, x.type, x.dev);
   const Placed at_(pos, late, n.rope, n.theta, x.D, x.S, {x.B, x.S}, most, x.dev);
@@ -582,7 +590,7 @@ PyObject* qknorm_bwd(Args a) {
   Args late = a;
   a.i += 2;
   const Norm n(a);
-  const long long most = a.whole();
+  const long long most = a.positive();
   const bool grads = a.whole() != 0;
   if (!x.k != !dkr || (!x.k && (kw || dk_))) throw NotPlain{};
   const Weights w(qw, kw, x.D, x.type, x.dev);
@@ -605,7 +613,7 @@ PyObject* append(Args a) {
   const float eps = (float)a.number();
   const int rope = a.index();
   const double theta = a.number();
-  const long long most = a.whole();
+  const long long most = a.positive();
   const int dtype = dtype_of(q);
   const c10::Device dev = q.device();
   const at::ScalarType type = q.scalar_type();
@@ -808,10 +816,10 @@ variable_list once(variable_list grads, const variable_list& of, const variable_
   return grads;
 }
 
-Table table_in(const Tensor& t) {
+Table table_in(const Tensor& t, int64_t rows) {
   Table r;
   r.ptr = static_cast<const float*>(t.const_data_ptr());
-  r.rows = (int)t.size(0);
+  r.rows = (int)rows;
   return r;
 }
 
@@ -827,24 +835,25 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
     const Weights w;
     const Table table;
     const int* positions;
-    Call(const Tensor& q, const Tensor& k, const Tensor& qw, const Tensor& kw, const Tensor& pos, const Tensor& tab, int64_t has_)
+    Call(const Tensor& q, const Tensor& k, const Tensor& qw, const Tensor& kw, const Tensor& pos, const Tensor& tab, int64_t rows,
+         int64_t has_)
         : has(has_), x(q, has & HAS_K ? &k : nullptr),
           w(has & HAS_QW ? &qw : nullptr, has & HAS_KW ? &kw : nullptr, x.D, x.type, x.dev),
-          table(has & HAS_TABLE ? table_in(tab) : Table()),
+          table(has & HAS_TABLE ? table_in(tab, rows) : Table()),
           positions(has & HAS_POSITIONS ? static_cast<const int*>(pos.const_data_ptr()) : nullptr) {}
   };
 
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& qw, const Tensor& kw,
-                               const Tensor& positions, const Tensor& table, double eps, int64_t rope, double theta,
-                               int64_t has) {
-    const Call c(q, k, qw, kw, positions, table, has);
+                               const Tensor& positions, const Tensor& table, int64_t rows, double eps, int64_t rope,
+                               double theta, int64_t has) {
+    const Call c(q, k, qw, kw, positions, table, rows, has);
     const Tensor oq = out_or(nullptr, c.x.q.sizes(), c.x.type, c.x.dev);
     Tensor ok;
     if (c.x.k) ok = out_or(nullptr, c.x.k->sizes(), c.x.type, c.x.dev);
     const int rc = norm_fwd(c.x, c.w, Norm((float)eps, (int)rope, theta), c.table, c.positions, oq, ok);
     if (rc) throw Failed{rc};
     ctx->save_for_backward({q, k, qw, kw, positions, table});
-    ctx->saved_data["variant"] = std::vector<double>{eps, (double)rope, theta, (double)has};
+    ctx->saved_data["variant"] = std::vector<double>{eps, (double)rope, theta, (double)has, (double)rows};
     if (c.x.k) return {oq, ok};
     return {oq};
   }
@@ -854,7 +863,7 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
     Tensor dq, dk, dqw, dkw;
     in_backward("attnfuse_qknorm_rope_bwd", [&] {
       const std::vector<double> v = ctx->saved_data["variant"].toDoubleVector();
-      const Call c(s[0], s[1], s[2], s[3], s[4], s[5], (int64_t)v[3]);
+      const Call c(s[0], s[1], s[2], s[3], s[4], s[5], (int64_t)v[4], (int64_t)v[3]);
       const Tensor dqr = grad[0].contiguous(), dkr = c.x.k ? grad[1].contiguous() : Tensor();
       dq = at::empty_like(c.x.q);
       if (c.x.k) dk = at::empty_like(*c.x.k);
@@ -864,7 +873,7 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
       if (!(c.has & HAS_KW)) dkw.reset();
       return rc;
     });
-    return once({dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2], s[3]}, grad);
+    return once({dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2], s[3]}, grad);
   }
 };
 
@@ -875,7 +884,7 @@ PyObject* qknorm_grad(Args a) {
   Args late = a;
   a.i += 2;
   const Norm n(a);
-  const long long most = a.whole();
+  const long long most = a.positive();
   if (!k && kw) throw NotPlain{};
   const Qk x(q, k);
   const Placed at_(pos, late, n.rope, n.theta, x.D, x.S, {x.B, x.S}, most, x.dev);
@@ -886,7 +895,7 @@ PyObject* qknorm_grad(Args a) {
   try {
     const variable_list r =
         NormFunction::apply(q, k ? *k : q, qw ? *qw : q, kw ? *kw : q, at_.positions ? *pos : q, table.defined() ? table : q,
-                            (double)n.eps, (int64_t)n.rope, n.theta, has);
+                            (int64_t)at_.table.rows, (double)n.eps, (int64_t)n.rope, n.theta, has);
     const Tensor ok = r.size() > 1 ? r[1] : Tensor();
     return tuple_of({&r[0], &ok});
   } catch (const Failed& f) {
@@ -900,7 +909,7 @@ struct SinksFunction : torch::autograd::Function<SinksFunction> {
     const Qkv x(q, k, v);
     const Tensor o = out_or(nullptr, x.q.sizes(), x.type, x.dev), l = out_or(nullptr, {x.B, x.H, x.S}, at::kFloat, x.dev);
     const int rc = sinks_fwd(x, Sinks{(int)rope, theta, (int)window, (int)sinks, (float)scale},
-                             rope != AF_ROPE_NONE ? table_in(table) : Table(), o, l);
+                             rope != AF_ROPE_NONE ? table_in(table, table.size(0)) : Table(), o, l);
     if (rc) throw Failed{rc};
     ctx->save_for_backward({q, k, v, o, l, table});
     ctx->saved_data["variant"] = std::vector<double>{(double)rope, theta, (double)window, (double)sinks, scale};
@@ -918,7 +927,7 @@ struct SinksFunction : torch::autograd::Function<SinksFunction> {
       dk = at::empty_like(x.k);
       dv = at::empty_like(x.k);
       return sinks_bwd(x, Sinks{(int)v[0], v[1], (int)v[2], (int)v[3], (float)v[4]},
-                       v[0] != AF_ROPE_NONE ? table_in(s[5]) : Table(), s[3], grad[0].contiguous(), s[4], dq, dk, dv, nullptr);
+                       v[0] != AF_ROPE_NONE ? table_in(s[5], s[5].size(0)) : Table(), s[3], grad[0].contiguous(), s[4], dq, dk, dv, nullptr);
     });
     return once({dq, dk, dv, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2]}, grad);
   }

@@ -311,3 +311,46 @@ def test_second_derivatives_are_refused(monkeypatch, native):
         (g,) = torch.autograd.grad(sum(y.float().square().sum() for y in leaves), leaves[0], create_graph=True)
         torch.autograd.grad(g.float().sum(), leaves[0])
     assert n == 5
+
+
+# ---------------------------------------------------------------- positions past max_positions
+@pytest.mark.parametrize("native", [True, False])
+@pytest.mark.parametrize("given", [False, True])
+def test_positions_from_max_positions_on_give_nan(monkeypatch, native, given):
+    """Whatever longer table an earlier call left, or the caller's table holds."""
+    need_gpu()
+    announce(f"max_positions native={native} given={given}")
+    if not native:
+        monkeypatch.setattr(api, "_native", None)
+    d = _inputs()
+    q, k, w = (d[n] for n in ("q", "k", "w"))
+    api.attnfuse_qknorm_rope(q, positions=d["pos"], max_positions=5000)   # leaves a table of 5000 rows or more
+    kw = dict(positions=d["pos"], max_positions=400, rope_table=api.rope_table(D, 10000.0, 500) if given else None)
+    far = (d["pos"] >= 400)
+    assert far.any() and not far.all()
+
+    def nan_rows(t, far):
+        bad = far[:, None, :, None].expand(t.shape)
+        return torch.equal(t.isnan(), bad)
+
+    fine = dict(kw, max_positions=500)
+    want = api.attnfuse_qknorm_rope(q, k, w, w, **fine)
+    got = api.attnfuse_qknorm_rope(q, k, w, w, **kw)
+    for a, b in zip(got, want):
+        assert nan_rows(a, far) and torch.equal(a[~a.isnan()], b[~a.isnan()])
+    leaves = [x.detach().requires_grad_() for x in (q, k, w, w)]
+    out = autograd.qknorm_rope(*leaves, **kw)
+    assert all(nan_rows(o, far) for o in out)
+    grads = torch.autograd.grad(out, leaves, (d["do"], k))
+    assert nan_rows(grads[0], far) and nan_rows(grads[1], far) and grads[2].isnan().all() and grads[3].isnan().all()
+    for a, b in zip(api.attnfuse_qknorm_rope_bwd(q, k, d["do"], k, w, w, **kw), grads):
+        assert torch.equal(a.isnan(), b.isnan()) and torch.equal(a.nan_to_num(), b.nan_to_num())
+    tok, tk = q.transpose(1, 2).reshape(B * S, H, D), k.transpose(1, 2).reshape(B * S, HKV, D)
+    kw["positions"] = d["pos"].reshape(-1)
+    kc, vc = (torch.zeros_like(x) for x in d["pages"])
+    qr = api.attnfuse_qknorm_rope_append(tok, tk, tk, kc, vc, d["slots"], **kw)
+    assert torch.equal(qr.isnan(), far.reshape(-1, 1, 1).expand(qr.shape))
+    assert int(kc.isnan().sum()) == int(far.sum()) * HKV * D and not vc.isnan().any()
+    for few in (0, -1):
+        with pytest.raises(ValueError, match="max_positions"):
+            api.attnfuse_qknorm_rope(q, **dict(kw, positions=d["pos"], max_positions=few))
