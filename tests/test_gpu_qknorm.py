@@ -271,3 +271,63 @@ def test_on_two_streams():
                 got[i] = api.attnfuse_qknorm_rope_bwd(xs[i], None, dos[i], None, w)
         torch.cuda.synchronize()
         assert all(torch.equal(got[i][j], want[i][j]) for i in range(2) for j in (0, 2))
+
+
+# ---------------------------------------------------------------- the weights' gradients, row by row
+DW = [
+    # H, S, B, D, dtype, rope
+    (64, 700, 1, 64, torch.bfloat16, "neox"),            # more units than workgroups
+    (9, 2000, 2, 128, torch.float32, "neox"),            # as above, a last head group that is not full
+    (5, 1, 67, 128, torch.bfloat16, "none"),             # several sequences a workgroup, a last one that is not full
+    (7, 3, 23, 64, torch.float32, "interleaved"),
+    (1, 1, 1, 64, torch.bfloat16, "none"),
+]
+
+
+def _dw_setup(H, S, B, D, dtype):
+    g = torch.Generator().manual_seed(S + H)
+    return g, rows((B, H, S, D), dtype, g, "slice"), rows((B, H, S, D), dtype, g, "bhsd"), weights(D, "fp32", dtype, g)[0]
+
+
+@pytest.mark.parametrize("H,S,B,D,dtype,rope", DW, ids=lambda x: str(x).replace("torch.", ""))
+def test_every_row_counts_once(H, S, B, D, dtype, rope):
+    """An incoming gradient in one row: dw is that row's dy xh alone, each element to 64 u, at the edges of what threads,
+    workgroups and their shares take.  (A row lost, or added twice, is off by all of it.)"""
+    need_gpu()
+    announce(f"dw rows H={H} S={S} B={B} D={D} {dtype} {rope}")
+    g, q, do, w = _dw_setup(H, S, B, D, dtype)
+    R = 4096 // D
+    at = {(b, h, n) for b in (0, B // 2, B - 1) for h in (0, 1, H - 2, H - 1)
+          for n in (0, 1, R - 1, R, R * (S // R) - 1, R * (S // R), S - 1) if 0 <= h < H and 0 <= n < S}
+    at |= {tuple(int(torch.randint(x, (1,), generator=g)) for x in (B, H, S)) for _ in range(20)}
+    one = torch.zeros_like(do)
+    for b, h, n in sorted(at):
+        one[b, h, n] = do[b, h, n]
+        got = api.attnfuse_qknorm_rope_bwd(q, None, one, None, w, eps=EPS, rope=rope)[2]
+        one[b, h, n] = 0
+        pos = torch.tensor([n])
+        _, want, _, size = qknorm_bwd(q[b, h, n:n + 1], w, do[b, h, n:n + 1], pos, rope, 10000.0, EPS)
+        # rotated terms: each element of dy is a sum of two, no larger together than the row's largest |dout|
+        size = size + want.new_tensor(float(do[b, h, n].abs().max())) * (f64(q[b, h, n]).abs() /
+                                                                        f64(q[b, h, n]).square().mean().sqrt())
+        assert_within(got, want, 64 * U32 * size, f"dw of row {b, h, n}")
+
+
+@pytest.mark.parametrize("H,S,B,D,dtype,rope", DW, ids=lambda x: str(x).replace("torch.", ""))
+def test_weight_gradient_to_the_length_of_its_sums(H, S, B, D, dtype, rope):
+    """All rows: an element's additions are a thread's rows (two heads for each of its units), the rows of a workgroup, a
+    32nd of the workgroups and 32 sums of those, each of 2^-24 of the magnitudes at most; a term itself is 64 of them off."""
+    need_gpu()
+    announce(f"dw sums H={H} S={S} B={B} D={D} {dtype} {rope}")
+    _, q, do, w = _dw_setup(H, S, B, D, dtype)
+    R = 4096 // D
+    wgs = api.attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, 0, S, D, dtype) // (4 * D)
+    per = R // S if 2 * S <= R else 1
+    units = -(-B // per) * -(-H // 2) * -(-S // R)
+    depth = 2 * -(-units // wgs) + R + -(-wgs // 32) + 32
+    got = api.attnfuse_qknorm_rope_bwd(q, None, do, None, w, eps=EPS, rope=rope)[2]
+    _, want, _, size = qknorm_bwd(q, w, do, torch.arange(S), rope, 10000.0, EPS)
+    if rope != "none":   # (as above, over all rows)
+        x = f64(q)
+        size = size + (f64(do).abs().amax(-1, keepdim=True) * x.abs() / x.square().mean(-1, keepdim=True).sqrt()).sum((0, 1, 2))
+    assert_within(got, want, (depth + 64) * U32 * size, "dw")
