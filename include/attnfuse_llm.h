@@ -113,7 +113,8 @@ int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, cons
  *   norm                          0: rotation alone (eps is ignored; weights
  *                                 must be NULL), else as attnfuse_qknorm_rope
  *   1 <= T <= 2^20; H, H_kv <= 16384.  Other slots of the pages are left as
- *   they are.
+ *   they are.  (attnfuse_decode_paged reads bf16 pages; pages of AF_DTYPE_FP32 are for
+ *   the caller's own use.)
  */
 int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
                                 const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
@@ -147,7 +148,8 @@ int attnfuse_fwd_sinks(const void* Q, const void* K, const void* V, void* O, flo
 
 /* Backward of attnfuse_fwd_sinks; workspace of attnfuse_bwd_sinks_workspace_bytes
  * (0 for invalid sizes), of which the last part, as there, is not required;
- * otherwise as attnfuse_bwd. */
+ * otherwise as attnfuse_bwd.  The size does not know the type: AF_DTYPE_FP32 needs
+ * it too, and uses the part that holds the row statistics. */
 size_t attnfuse_bwd_sinks_workspace_bytes(int B, int H, int H_kv, int S, int D, int rope, int window, int sinks);
 int attnfuse_bwd_sinks(const void* Q, const void* K, const void* V, const void* O, const void* dO, const float* LSE,
                        void* dQ, void* dK, void* dV, void* workspace, size_t workspace_bytes,
@@ -200,9 +202,11 @@ size_t attnfuse_decode_paged_workspace_bytes(int B, int H, int H_kv, int S_kv, i
  *   D in {64, 128}; B < 2^16; any H <= 16384 that is a multiple of H_kv (a group of
  *   more than 32 query heads reads the cache once for each 32)
  *
- * A sequence's result depends on its own keys and length only, not on the other
- * sequences.  What lies in places that are not visible is never used, whatever
- * it is.
+ * In a call of given B, max_pages and page_size a sequence's result depends on its own
+ * keys and length only, not on the other sequences.  With another B or table width the
+ * keys may be shared out otherwise among workgroups: the same result to the rounding of
+ * fp32 sums, not the same bits.  What lies in places that are not visible is never used,
+ * whatever it is.
  */
 int attnfuse_decode_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table,
                           const int* cache_lens, void* O, float* LSE, void* workspace, size_t workspace_bytes,

@@ -98,8 +98,8 @@ int bwd_splits_sparse(int B, int H, int H_kv, int S, int D, int mask, int window
 
 // Backward workspace: [delta f32 | lse2 f32 | dO fp16 | dO scale f32 | partial
 // max |dO| u32 | Q' fp16 | K' fp16 | partial dK' and dV f32], each section
-// starting on a 256-byte boundary; Q' and K' only with RoPE, the partials only
-// where some mask's dK/dV pass is split.  The partial maxima cover chunks of
+// starting on a 256-byte boundary; Q' and K' only with RoPE (and with sinks, where they
+// hold Q and K without it), the partials only where some mask's dK/dV pass is split.  The partial maxima cover chunks of
 // at least kDmaxChunk elements of each (batch, K/V head)'s dO.
 constexpr long long kDmaxChunk = 16384;
 
@@ -156,6 +156,7 @@ bool all_visible(int S, int window, int sinks) { return (long long)window + sink
 // D64 window 256, us for 512 / 768 workgroups: 4 sinks 10.9 / 14.6, 37 sinks 14.6 / 17.0.
 // This pass and the sum of its parts, H8/1 D64 window 256, for at most 32 / 64 / 256
 // parts: S3000 22.8 / 23.6 / 38.5, S16000 56.5 / 42.4 / 61.7; D128 S3000 29.8 / 26.6 / 38.3.
+// (The fp32 kernels have no such pass; the size does not know the type.)
 struct FarLayout {
   int parts = 0;
   size_t bytes = 0;

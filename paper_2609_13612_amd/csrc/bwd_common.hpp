@@ -1,5 +1,5 @@
 // Helpers shared by the two gradient passes of the bf16 backward (the dQ pass
-// in bwd_bf16.hip, the dK/dV pass in bwd_dkdv.hip): row operands, gradient
+// in dq_kernel.hpp, the dK/dV pass in dkdv_kernel.hpp): row operands, gradient
 // stores through the inverse rotation, transposed and swizzled LDS operands,
 // and the dispatch from runtime variant arguments to kernel instantiations.
 #pragma once

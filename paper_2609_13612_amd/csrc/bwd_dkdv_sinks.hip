@@ -1,5 +1,6 @@
-// dK/dV pass under a window with sinks (dkdv_kernel.hpp): the window's pairs, to
-// which the key blocks that hold sinks add what bwd_sinks.hip summed.
+// dK/dV pass under a window with sinks (dkdv_kernel.hpp): the window's pairs.  The key
+// blocks that hold sinks start from what bwd_sinks.hip summed; with splits the
+// reduction (bwd_dkdv_split.hip) adds it.
 #include "dkdv_kernel.hpp"
 
 namespace af {

@@ -140,7 +140,9 @@ __global__ __launch_bounds__(64 * F32_NW) void bwd_fp32_dkdv_kernel(BwdParams p)
   const int W = p.window;
   int tq = 0, tq_end = (S + F32_T - 1) / F32_T;
   if constexpr (MASK != MASK_NONE) tq = kb;
-  if constexpr (windowed(MASK))   // (a block with sinks is seen to the end)
+  // A block with sinks is seen to the end: its workgroup walks all later queries, alone
+  // (B1 H8/2 S2048 D128 window 256: 683 us with 4 sinks, 100 without).
+  if constexpr (windowed(MASK))
     if (MASK != MASK_SINKS || n0 >= p.sinks) tq_end = min(tq_end, (min(n0 + F32_T, S) - 1 + W - 1) / F32_T + 1);
   const int nt = tq_end - tq, items = G * nt;
 

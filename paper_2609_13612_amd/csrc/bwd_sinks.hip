@@ -8,8 +8,9 @@
 // all keys alike, and this one the sinks' pairs past it,
 //   (i, j) with j < sinks and i - j >= window:   dV_j += P_ij dO_i,  dK'_j += dS_ij Q'_i,
 // split over the queries: the workgroups of 32 sinks share their (query head,
-// query tile) steps and leave fp32 partial sums, which the dK/dV pass adds in
-// their order (no atomics) before it rotates and rounds dK and dV once.
+// query tile) steps and leave fp32 partial sums.  The dK/dV pass sums them in their
+// order (no atomics) and starts from them, or, where it is split itself, its reduction
+// adds them to its own; dK and dV are rotated and rounded once, after that.
 //
 // Without RoPE K and Q go through the workspace in fp16 too (ROPE_F16), so that the
 // passes copy their tiles straight to LDS in workgroups of four waves: converted as

@@ -11,7 +11,8 @@
 // shares of those tiles for one (sequence, K/V head, up to 32 query heads): wave w of
 // share s takes tiles 4 s + w, 4 (s + nsplit) + w, ..., so shares are even whatever
 // the length, the first tile's page is looked up before the length is known, and a
-// sequence's result depends on its own length alone.  The four waves' (max, sum, O)
+// sequence's result depends, at a given nsplit, on its own length alone.  (nsplit comes
+// from the batch and the most keys a sequence may have.)  The four waves' (max, sum, O)
 // are joined through LDS and leave as one partial per workgroup, or as the result
 // where a sequence is one workgroup's; a second kernel joins the partials.
 //

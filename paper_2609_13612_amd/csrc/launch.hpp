@@ -48,8 +48,8 @@ struct BwdParams {
   float* dscale;          // workspace [B*H_kv]: sigma, a power of two per (batch, K/V head)
   uint32_t* dmax;         // workspace [B*H_kv*dmax_chunks]: partial max |dO| (bf16 magnitude bits)
   int dmax_chunks;        // partial maxima per (batch, K/V head), at most DMAX_PARTS
-  void* qr16;             // workspace [B,H,S,D] fp16: Q' = R Q (RoPE only, else nullptr)
-  void* kr16;             // workspace [B,H_kv,S,D] fp16: K' = R K (RoPE only, else nullptr)
+  void* qr16;             // workspace [B,H,S,D] fp16: Q' = R Q (with RoPE, and Q itself with sinks; else nullptr)
+  void* kr16;             // workspace [B,H_kv,S,D] fp16: K' = R K (as qr16)
   int B, H, Hkv, S, window;
   const float* slopes;
   float scale;
