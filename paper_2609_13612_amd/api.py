@@ -184,12 +184,18 @@ def _tab(t):
     return (None, 0) if t is None else (t.data_ptr(), t.shape[0])
 
 
+def _count(n):
+    """A window, or a number of sinks, in the library's 32 bits (ctypes would drop the others): from there on a larger one
+    shows no more keys, and a negative one is refused as -1 is."""
+    return max(-1, min(int(n or 0), 2 ** 31 - 1))
+
+
 def _variant(rope, theta, mask, window, alibi_slopes, scale, D, H=None, device=None):
     if scale is None:
         scale = 1.0 / math.sqrt(D)
     if alibi_slopes is not None:
         _need(alibi_slopes, "alibi_slopes", (H,), torch.float32, device)
-    return ROPE[rope], float(theta), MASK[mask], int(window or 0), scale
+    return ROPE[rope], float(theta), MASK[mask], _count(window), scale
 
 
 @functools.lru_cache(maxsize=4096)
@@ -730,19 +736,20 @@ def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None,
 
 
 def attnfuse_decode_paged_workspace_bytes(B, H, H_kv, S_kv, D, window=0, sinks=0):
-    return _lib.load().attnfuse_decode_paged_workspace_bytes(B, H, H_kv, S_kv, D, window or 0, sinks)
+    return _lib.load().attnfuse_decode_paged_workspace_bytes(B, H, H_kv, S_kv, D, _count(window), _count(sinks))
 
 
 def _need_sinks(sinks, mask, window, alibi_slopes):
-    """Sinks belong to a sliding window, without ALiBi."""
+    """(window, sinks): sinks belong to a sliding window, without ALiBi."""
     if sinks < 0 or mask != "sliding_window" or not window or window < 1:
         raise ValueError("sinks (>= 1) need mask='sliding_window' and a window")
     if alibi_slopes is not None:
         raise ValueError("sinks do not go with ALiBi slopes")
+    return _count(window), _count(sinks)
 
 
 def _fwd_sinks(q, k, v, rope, theta, mask, window, alibi_slopes, scale, out, lse, rope_table, sinks):
-    _need_sinks(sinks, mask, window, alibi_slopes)
+    window, sinks = _need_sinks(sinks, mask, window, alibi_slopes)
     if _native is not None:
         r = _native.fwd_sinks(q, k, v, out, lse, rope_table, _TABLES, ROPE.get(rope, -1), theta, window, sinks, scale)
         if r is not None:
@@ -758,17 +765,17 @@ def _fwd_sinks(q, k, v, rope, theta, mask, window, alibi_slopes, scale, out, lse
     ws = torch.empty(nbytes, device=dev, dtype=torch.uint8) if nbytes else None
     with torch.cuda.device(dev):
         code = _lib.load().attnfuse_fwd_sinks(_ptr(q), _ptr(k), _ptr(v), _ptr(out), _ptr(lse), _ptr(ws), nbytes, B, H, Hkv, S,
-                                              D, DTYPE[q.dtype], r, th, tp, tr, w, int(sinks), sc, _stream())
+                                              D, DTYPE[q.dtype], r, th, tp, tr, w, sinks, sc, _stream())
     _check(code, "attnfuse_fwd_sinks")
     return out, lse
 
 
 def attnfuse_bwd_sinks_workspace_bytes(B, H, H_kv, S, D, rope, window, sinks):
-    return _lib.load().attnfuse_bwd_sinks_workspace_bytes(B, H, H_kv, S, D, ROPE[rope], window, sinks)
+    return _lib.load().attnfuse_bwd_sinks_workspace_bytes(B, H, H_kv, S, D, ROPE[rope], _count(window), _count(sinks))
 
 
 def _bwd_sinks(q, k, v, o, do, lse, rope, theta, mask, window, alibi_slopes, scale, dq, dk, dv, workspace, rope_table, sinks):
-    _need_sinks(sinks, mask, window, alibi_slopes)
+    window, sinks = _need_sinks(sinks, mask, window, alibi_slopes)
     if _native is not None:
         r = _native.bwd_sinks(q, k, v, o, do, lse, dq, dk, dv, workspace, rope_table, _TABLES, ROPE.get(rope, -1), theta,
                               window, sinks, scale)
@@ -784,14 +791,14 @@ def _bwd_sinks(q, k, v, o, do, lse, rope, theta, mask, window, alibi_slopes, sca
     with torch.cuda.device(dev):
         code = _lib.load().attnfuse_bwd_sinks(_ptr(q), _ptr(k), _ptr(v), _ptr(o), _ptr(do), _ptr(lse), _ptr(dq), _ptr(dk),
                                               _ptr(dv), _ptr(workspace), wbytes, B, H, Hkv, S, D, DTYPE[q.dtype], r, th, tp,
-                                              tr, w, int(sinks), sc, _stream())
+                                              tr, w, sinks, sc, _stream())
     _check(code, "attnfuse_bwd_sinks")
     return dq, dk, dv
 
 
 def _decode_sinks(q, k_cache, v_cache, cache_lens, rope, theta, mask, window, alibi_slopes, scale, out, lse, workspace,
                   rope_table, sinks):
-    _need_sinks(sinks, mask, window, alibi_slopes)
+    window, sinks = _need_sinks(sinks, mask, window, alibi_slopes)
     if _native is not None:
         r = _native.decode_sinks(q, k_cache, v_cache, cache_lens, out, lse, workspace, rope_table, _TABLES,
                                  ROPE.get(rope, -1), theta, window, sinks, scale)
@@ -820,7 +827,7 @@ def attnfuse_decode_paged(q, k_cache, v_cache, block_table, cache_lens=None, *, 
     attnfuse_decode_paged in include/attnfuse_llm.h.  The pages may lie apart (pages [num_pages, page_size, H_kv, D]
     transposed)."""
     if sinks:
-        _need_sinks(sinks, mask, window, alibi_slopes)
+        window, sinks = _need_sinks(sinks, mask, window, alibi_slopes)
     if _native is not None:
         r = _native.decode_paged(q, k_cache, v_cache, block_table, cache_lens, out, lse, workspace, alibi_slopes, rope_table,
                                  _TABLES, ROPE.get(rope, -1), theta, MASK.get(mask, -1), window, sinks, scale)

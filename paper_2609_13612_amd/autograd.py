@@ -145,7 +145,7 @@ def attention(q, k, v, *, rope="none", theta=10000.0, mask="causal", window=None
     """Differentiable fused attention: O [B, H, S, D] (and the non-differentiable
     LSE [B, H, S] with ``return_lse``); arguments as api.attnfuse_fwd."""
     if sinks and api._native is not None:   # the same function, its backward in C++
-        api._need_sinks(sinks, mask, window, alibi_slopes)
+        window, sinks = api._need_sinks(sinks, mask, window, alibi_slopes)
         r = api._native.sinks_grad(q, k, v, None, api._TABLES, api.ROPE.get(rope, -1), theta, window, sinks, scale)
         if r is not None:
             o, lse = api._result(r, "attnfuse_fwd_sinks")

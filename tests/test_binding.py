@@ -101,3 +101,18 @@ def test_package_never_uses_the_oracle():
         text = f.read_text()
         assert not re.search(r"^\s*(import|from)\s+oracle\b", text, flags=re.M), f"{f.name} imports the oracle"
         assert "scaled_dot_product_attention" not in text, f"{f.name} calls a torch attention routine"
+
+
+@pytest.mark.parametrize("given,taken", [(None, 0), (0, 0), (1, 1), (2 ** 31 - 1, 2 ** 31 - 1), (2 ** 31, 2 ** 31 - 1),
+                                         (2 ** 32 + 5, 2 ** 31 - 1), (10 ** 30, 2 ** 31 - 1), (-1, -1), (-2 ** 32 + 7, -1)])
+def test_windows_and_sinks_keep_to_32_bits(given, taken):
+    """A window of 2^32 + 5 keys is a window over everything, not one of 5; a negative one stays negative."""
+    assert api._variant("none", 1e4, "sliding_window", given, None, None, 64)[3] == taken
+    if given and given > 0:
+        assert api._need_sinks(given, "sliding_window", 7, None) == (7, taken)
+        assert api._need_sinks(3, "sliding_window", given, None) == (taken, 3)
+    sizes = (1, 8, 2, 4096, 64)
+    assert api.attnfuse_bwd_sinks_workspace_bytes(*sizes, "neox", 2 ** 32 + 5, 4) == \
+        api.attnfuse_bwd_sinks_workspace_bytes(*sizes, "neox", 4096, 4)
+    assert api.attnfuse_decode_paged_workspace_bytes(*sizes, 64, 2 ** 32 + 5) == \
+        api.attnfuse_decode_paged_workspace_bytes(*sizes, 64, 4096)

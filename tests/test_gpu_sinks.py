@@ -233,3 +233,29 @@ def test_refusals():
             api.attnfuse_bwd(*args, args[0], d["do"], torch.zeros(1, 4, 64, device="cuda"), **bad)
     with pytest.raises(ValueError):
         api.attnfuse_fwd(args[0], args[1].float(), args[2], mask="sliding_window", window=4, sinks=1)
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_windows_and_sinks_past_32_bits(monkeypatch, native):
+    """As every key's: forward, backward, autograd and both decodes; a plain window too."""
+    need_gpu()
+    announce(f"sinks past 32 bits native={native}")
+    if not native:
+        monkeypatch.setattr(api, "_native", None)
+    _, d = device_inputs(1, 4, 2, 100, 64, seed=5, with_do=True)
+    q, k, v, do = (d[n] for n in ("q", "k", "v", "do"))
+    one = q[:, :, 7].contiguous()
+    pages = [x.transpose(1, 2).reshape(1, 100, 2, 64)[:, :96].reshape(6, 16, 2, 64).transpose(1, 2) for x in (k, v)]
+    table = torch.arange(6, dtype=torch.int32, device="cuda")[None]
+    want = api.attnfuse_fwd(q, k, v)
+    grads = api.attnfuse_bwd(q, k, v, *want[:1], do, want[1])
+    for window, sinks in ((2 ** 32 + 5, 4), (5, 2 ** 32 + 1), (2 ** 31, 2 ** 31), (2 ** 32 + 5, 0)):
+        kw = dict(mask="sliding_window", window=window, sinks=sinks)
+        o, lse = api.attnfuse_fwd(q, k, v, **kw)
+        assert torch.equal(o, want[0]) and torch.equal(lse, want[1])
+        assert all(torch.equal(a, b) for a, b in zip(api.attnfuse_bwd(q, k, v, o, do, lse, **kw), grads))
+        leaves = [x.detach().requires_grad_() for x in (q, k, v)]
+        assert all(torch.equal(a, b) for a, b in zip(torch.autograd.grad(autograd.attention(*leaves, **kw), leaves, do), grads))
+        most = dict(mask="sliding_window", window=100, sinks=min(sinks, 1))
+        for call in (lambda **m: api.attnfuse_decode(one, k, v, **m), lambda **m: api.attnfuse_decode_paged(one, *pages, table, **m)):
+            assert all(torch.equal(a, b) for a, b in zip(call(**kw), call(**most)))
