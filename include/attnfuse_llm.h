@@ -139,6 +139,9 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
  *                                 the rotated keys; 0 bytes, and it may be NULL,
  *                                 without RoPE and for AF_DTYPE_FP32
  *   other arguments and results as attnfuse_fwd; no ALiBi
+ * As there, a pair that is not visible counts with weight 0 inside the tiles that a
+ * workgroup visits: a NaN or an infinity in a row of V (in the backward of Q, K or
+ * dO too) reaches queries that do not see that row.  Every row up to S is finite.
  */
 size_t attnfuse_fwd_sinks_workspace_bytes(int B, int H_kv, int S, int D, int dtype, int rope);
 int attnfuse_fwd_sinks(const void* Q, const void* K, const void* V, void* O, float* LSE, void* workspace,
