@@ -128,6 +128,72 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
                                 const int* positions, void* stream);
 
 /*
+ * Positions of several axes: the same three calls where a row has a position on
+ * each of up to four axes (time, height and width of a patch of a video; text
+ * has the same on all).  The D/2 pairs of a row are shared out among the axes,
+ * sections[a] (>= 1) of them to axis a, D/2 in all:
+ *     AF_SECTIONS_BLOCKS   the first sections[0] pairs turn by axis 0, ...
+ *     AF_SECTIONS_TURNS    one pair to each axis in turn, as long as it has some
+ *                          left
+ * Pair i turns by positions[its axis] * w_i; the w_i are those of the table:
+ *     AF_FREQUENCIES_SHARED  w_i = theta^(-2i/D) whatever the axis: the table of
+ *                            attnfuse_rope_table_fill
+ *     AF_FREQUENCIES_OWN     the j-th pair of axis a (from 0) has theta^(-j /
+ *                            sections[a]): every axis a ladder of its own
+ *
+ *   rope           AF_ROPE_NEOX or AF_ROPE_INTERLEAVED: what makes a pair (NONE:
+ *                  INVALID)
+ *   positions      device int32 [axes, B, S] ([axes, T]), contiguous, needed.  A
+ *                  row with a position on any axis that is not in [0,
+ *                  rope_table_rows) comes out as NaN.
+ *   axes           1 .. 4
+ *   sections       [axes] in HOST memory, read during the call
+ *   norm           0: rotation alone (r = 1; eps is ignored; weights must be
+ *                  NULL).  The backward is then dx = R^T dout: Q, K and the
+ *                  workspace are not used and may be NULL (keys are there where
+ *                  dKr is), and the weights' gradients must be NULL.
+ *   other arguments, workspaces and results as those of the calls above
+ */
+#define AF_SECTIONS_BLOCKS 0
+#define AF_SECTIONS_TURNS 1
+#define AF_FREQUENCIES_SHARED 0
+#define AF_FREQUENCIES_OWN 1
+
+/* Fill a table [rows, D/2] of (cos, sin) for these sections and frequencies, as
+ * attnfuse_rope_table_fill does (its size is attnfuse_rope_table_bytes; one
+ * launch). */
+int attnfuse_axes_table_fill(float* table, int rows, int D, float rope_theta, int axes, const int* sections,
+                             int section_order, int frequencies, void* stream);
+int attnfuse_qknorm_axes(const void* Q, const void* K, void* Qr, void* Kr, const void* q_weight, const void* k_weight,
+                         int weight_dtype, int norm, float eps,
+                         long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                         long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                         int B, int H, int H_kv, int S, int D, int dtype,
+                         int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                         const int* positions, int axes, const int* sections, int section_order, void* stream);
+int attnfuse_qknorm_axes_bwd(const void* Q, const void* K, const void* dQr, const void* dKr, void* dQ, void* dK,
+                             void* dq_weight, void* dk_weight, const void* q_weight, const void* k_weight,
+                             int weight_dtype, int norm, float eps,
+                             long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                             long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                             long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
+                             long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
+                             void* workspace, size_t workspace_bytes,
+                             int B, int H, int H_kv, int S, int D, int dtype,
+                             int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                             const int* positions, int axes, const int* sections, int section_order, void* stream);
+int attnfuse_qknorm_axes_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
+                                const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
+                                int norm, float eps,
+                                long long q_stride_t, long long q_stride_h, long long k_stride_t, long long k_stride_h,
+                                long long v_stride_t, long long v_stride_h,
+                                long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                                long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                                int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
+                                int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                                const int* positions, int axes, const int* sections, int section_order, void* stream);
+
+/*
  * attnfuse_fwd under a sliding window whose first tokens stay visible: query i
  * sees key j when j <= i and (j > i - window or j < sinks); positions (RoPE) are
  * those in the sequence for sinks too.

@@ -46,6 +46,12 @@ LLM_SIGNATURES = {
     "attnfuse_qknorm_rope_bwd": (_I, [_P] * 10 + [_I, _F] + [_L] * 12 + [_P, ctypes.c_size_t] + [_I] * 7
                                  + [_F, _P, _I, _P, _P]),
     "attnfuse_qknorm_rope_append": (_I, [_P] * 9 + [_I, _I, _F] + [_L] * 12 + [_I] * 8 + [_F, _P, _I, _P, _P]),
+    "attnfuse_axes_table_fill": (_I, [_P, _I, _I, _F, _I, _P, _I, _I, _P]),
+    "attnfuse_qknorm_axes": (_I, [_P] * 6 + [_I, _I, _F] + [_L] * 6 + [_I] * 7 + [_F, _P, _I, _P, _I, _P, _I, _P]),
+    "attnfuse_qknorm_axes_bwd": (_I, [_P] * 10 + [_I, _I, _F] + [_L] * 12 + [_P, ctypes.c_size_t] + [_I] * 7
+                                 + [_F, _P, _I, _P, _I, _P, _I, _P]),
+    "attnfuse_qknorm_axes_append": (_I, [_P] * 9 + [_I, _I, _F] + [_L] * 12 + [_I] * 8
+                                    + [_F, _P, _I, _P, _I, _P, _I, _P]),
     "attnfuse_fwd_sinks_workspace_bytes": (ctypes.c_size_t, [_I] * 6),
     "attnfuse_fwd_sinks": (_I, [_P] * 6 + [ctypes.c_size_t] + [_I] * 7 + [_F, _P, _I, _I, _I, _F, _P]),
     "attnfuse_bwd_sinks_workspace_bytes": (ctypes.c_size_t, [_I] * 8),

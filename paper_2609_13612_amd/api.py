@@ -9,6 +9,7 @@ Plain calls are marshalled by native/binding.cpp, which does the same checks;
 it declines (returns None) whatever it does not recognise, and the Python code
 after it then marshals the call or raises.
 """
+import ctypes
 import functools
 import math
 
@@ -25,6 +26,8 @@ except ImportError:   # not built for this interpreter: every call is marshalled
 DTYPE = {torch.bfloat16: 0, torch.float32: 1}
 ROPE = {"none": 0, "neox": 1, "interleaved": 2}
 MASK = {"none": 0, "causal": 1, "sliding_window": 2}
+SECTION_ORDER = {"blocks": 0, "turns": 1}
+FREQUENCIES = {"shared": 0, "own": 1}
 
 
 class AttnFuseError(RuntimeError):
@@ -130,11 +133,13 @@ _TABLES = {}
 _TABLE_MIN_ROWS = 4096
 
 
-def rope_table(D, theta, rows, device=None, out=None):
+def rope_table(D, theta, rows, device=None, out=None, *, sections=None, section_order="blocks", frequencies="shared"):
     """A RoPE cos/sin table for positions 0..rows-1: T[n][i] = (cos, sin) of
     n * theta^(-2i/D), filled by attnfuse_rope_table_fill on the current stream
     (see include/attnfuse.h).  Pass it as ``rope_table=`` to any call with the
-    same D and theta and S <= rows."""
+    same D and theta and S <= rows.  With ``sections`` and frequencies="own" it is
+    that of positions of several axes, each with its own ladder of frequencies
+    (attnfuse_axes_table_fill), for calls with the same sections in the same order."""
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
     shape = (rows, D // 2, 2)
     if out is None:
@@ -142,17 +147,23 @@ def rope_table(D, theta, rows, device=None, out=None):
     else:
         _need(out, "out", shape, torch.float32, device)
     with torch.cuda.device(device):
-        code = _lib.load().attnfuse_rope_table_fill(out.data_ptr(), rows, D, float(theta), _stream())
-    _check(code, "attnfuse_rope_table_fill")
+        if sections is None:
+            code = _lib.load().attnfuse_rope_table_fill(out.data_ptr(), rows, D, float(theta), _stream())
+        else:
+            code = _lib.load().attnfuse_axes_table_fill(out.data_ptr(), rows, D, float(theta), len(sections),
+                                                        (ctypes.c_int * len(sections))(*sections),
+                                                        SECTION_ORDER[section_order], FREQUENCIES[frequencies], _stream())
+    _check(code, "attnfuse_rope_table_fill" if sections is None else "attnfuse_axes_table_fill")
     return out
 
 
-def _table(rope, theta, D, S, device, given):
+def _table(rope, theta, D, S, device, given, own=None):
     """The cos/sin table a call reads, as a tensor: the caller's (checked), or
     one this binding keeps for (device, D, theta).  Under HIP graph capture a
     table not yet built is filled inside the capture (stream-ordered before the
     call that reads it) and not kept; the caller holds the returned tensor
-    until its launch is enqueued.  None without RoPE."""
+    until its launch is enqueued.  own: (sections, section_order) where every axis
+    has its own frequencies.  None without RoPE."""
     if ROPE[rope] == ROPE["none"]:
         return None
     if given is not None:
@@ -162,7 +173,8 @@ def _table(rope, theta, D, S, device, given):
         if given.shape[0] < S:
             raise ValueError(f"rope_table has {given.shape[0]} rows, the call needs {S}")
         return given
-    key = (device.index, D, float(np.float32(theta)))
+    key = (device.index, D, float(np.float32(theta))) + (own or ())
+    axes = dict(sections=own[0], section_order=own[1], frequencies="own") if own else {}
     for t in _TABLES.get(key, ()):
         if t.shape[0] >= S:
             return t
@@ -171,8 +183,8 @@ def _table(rope, theta, D, S, device, given):
         rows *= 2
     with torch.cuda.device(device):
         if torch.cuda.is_current_stream_capturing():
-            return rope_table(D, theta, S, device)
-        t = rope_table(D, theta, rows, device)
+            return rope_table(D, theta, S, device, **axes)
+        t = rope_table(D, theta, rows, device, **axes)
         # ready for any stream before it is shared: one wait, once per table
         torch.cuda.current_stream().synchronize()
     _TABLES.setdefault(key, []).append(t)
@@ -612,6 +624,41 @@ def _position_table(rope, theta, D, n, device, positions, shape, max_positions, 
     return _table(rope, theta, D, int(max_positions), device, rope_table)[:int(max_positions)]
 
 
+def _axes(sections, section_order, frequencies, norm, rope, D, positions):
+    """The sections of positions of several axes, as a tuple, and their order; None without any."""
+    if sections is None:
+        if not norm:
+            raise ValueError("norm=False needs sections (one axis: sections=(D // 2,) and positions [1, ...])")
+        return None
+    sections = tuple(int(n) for n in sections)
+    if section_order not in SECTION_ORDER or frequencies not in FREQUENCIES:
+        raise ValueError("section_order is 'blocks' or 'turns', frequencies 'shared' or 'own'")
+    if not 1 <= len(sections) <= 4 or min(sections) < 1 or 2 * sum(sections) != D:
+        raise ValueError(f"sections must be one to four numbers of pairs, {D // 2} in all (they are {sections})")
+    if rope not in ("neox", "interleaved") or positions is None:
+        raise ValueError("sections need positions and rope='neox' or 'interleaved'")
+    return sections, section_order
+
+
+def _axes_table(axes, frequencies, rope, theta, D, device, max_positions, rope_table):
+    """The table of a call with sections, whatever rows it has from max_positions on."""
+    if rope_table is None and max_positions is None:
+        raise ValueError("positions need max_positions (every position is below it) or rope_table")
+    if max_positions is not None and int(max_positions) < 1:
+        raise ValueError(f"max_positions must be at least 1 (it is {max_positions})")
+    return _table(rope, theta, D, 1 if max_positions is None else int(max_positions), device, rope_table,
+                  axes if frequencies == "own" else None)
+
+
+def _axes_args(axes):
+    """axes, sections, section_order of the library's calls."""
+    return len(axes[0]), (ctypes.c_int * len(axes[0]))(*axes[0]), SECTION_ORDER[axes[1]]
+
+
+def _axes_rows(table, max_positions):
+    return table.data_ptr(), table.shape[0] if max_positions is None else int(max_positions)
+
+
 def _qknorm_shape(q, k):
     dev = _device(q)
     if q.dim() != 4 or (k is not None and (not isinstance(k, torch.Tensor) or k.dim() != 4)):
@@ -624,11 +671,19 @@ def _qknorm_shape(q, k):
 
 
 def attnfuse_qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0, positions=None,
-                         max_positions=None, out_q=None, out_k=None, rope_table=None):
+                         max_positions=None, out_q=None, out_k=None, rope_table=None, sections=None,
+                         section_order="blocks", frequencies="shared", norm=True):
     """Qr, Kr: the rows of q and k over their root mean square, times the weights, rotated at their positions (0..S-1, or
     ``positions`` int32 [B, S], all below ``max_positions``: a row at another one comes out as NaN); see
     attnfuse_qknorm_rope in include/attnfuse_llm.h.  q and k may be slices whose rows lie apart; Qr and Kr are
-    contiguous."""
+    contiguous.
+
+    With ``sections``, ``positions`` is int32 [axes, B, S]: a row has one on each of up to four axes (time, height, width),
+    and sections[a] of its D / 2 pairs turn by axis a, in "blocks" or dealt out in "turns", with the "shared" frequencies
+    theta^(-2i/D) or a ladder of each axis's "own"; norm=False is then the rotation alone.  See attnfuse_qknorm_axes."""
+    if sections is not None or not norm:
+        return _axes_fwd(q, k, q_weight, k_weight, eps, rope, theta, positions, max_positions, out_q, out_k, rope_table,
+                         sections, section_order, frequencies, norm)
     if _native is not None:
         r = _native.qknorm(q, k, q_weight, k_weight, out_q, out_k, positions, rope_table, _TABLES, eps, ROPE.get(rope, -1),
                            theta, max_positions)
@@ -650,15 +705,52 @@ def attnfuse_qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, r
     return out_q, out_k
 
 
+def _axes_fwd(q, k, q_weight, k_weight, eps, rope, theta, positions, max_positions, out_q, out_k, rope_table, sections,
+              section_order, frequencies, norm):
+    dev = _device(q)
+    axes = _axes(sections, section_order, frequencies, norm, rope, q.shape[-1], positions)
+    tab = _axes_table(axes, frequencies, rope, theta, q.shape[-1], dev, max_positions, rope_table)
+    if _native is not None:
+        r = _native.axes(q, k, q_weight, k_weight, out_q, out_k, positions, tab, eps, ROPE[rope], theta, max_positions,
+                         int(bool(norm)), axes[0], SECTION_ORDER[axes[1]])
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_axes")
+    dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
+    wt = _axes_weights(q_weight, k_weight, norm, D, q.dtype, dev)
+    _need(positions, "positions", (len(axes[0]), B, S), torch.int32, dev)
+    out_q = _opt(out_q, "out_q", (B, H, S, D), q.dtype, dev)
+    if k is not None:
+        out_k = _opt(out_k, "out_k", (B, Hkv, S, D), q.dtype, dev)
+    elif out_k is not None or k_weight is not None:
+        raise ValueError("out_k and k_weight need k")
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_qknorm_axes(_ptr(q), _ptr(k), _ptr(out_q), _ptr(out_k), _ptr(q_weight), _ptr(k_weight), wt,
+                                                int(bool(norm)), float(eps), *qs, *ks, B, H, Hkv, S, D, DTYPE[q.dtype],
+                                                ROPE[rope], float(theta), *_axes_rows(tab, max_positions), _ptr(positions),
+                                                *_axes_args(axes), _stream())
+    _check(code, "attnfuse_qknorm_axes")
+    return out_q, out_k
+
+
+def _axes_weights(q_weight, k_weight, norm, D, dtype, dev):
+    if not norm and (q_weight is not None or k_weight is not None):
+        raise ValueError("norm=False takes no weights")
+    return _norm_weights(q_weight, k_weight, D, dtype, dev)
+
+
 def attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, H_kv, S, D, dtype=torch.bfloat16):
     return _lib.load().attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, H_kv, S, D, DTYPE[dtype])
 
 
 def attnfuse_qknorm_rope_bwd(q, k, dqr, dkr, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0,
                              positions=None, max_positions=None, weight_grads=True, dq=None, dk=None, workspace=None,
-                             rope_table=None):
+                             rope_table=None, sections=None, section_order="blocks", frequencies="shared", norm=True):
     """dQ, dK, dq_weight, dk_weight of attnfuse_qknorm_rope (k and dkr None: of q alone; without ``weight_grads`` the last
-    two are None); see attnfuse_qknorm_rope_bwd.  dQ and dK lie in memory as q and k do, without gaps."""
+    two are None); see attnfuse_qknorm_rope_bwd.  dQ and dK lie in memory as q and k do, without gaps.  With norm=False q
+    and k are not used (None will do), there are no weights, and dQ and dK are contiguous where none are given."""
+    if sections is not None or not norm:
+        return _axes_bwd(q, k, dqr, dkr, q_weight, k_weight, eps, rope, theta, positions, max_positions, weight_grads, dq, dk,
+                         workspace, rope_table, sections, section_order, frequencies, norm)
     if _native is not None:
         r = _native.qknorm_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, rope_table, _TABLES, eps,
                                ROPE.get(rope, -1), theta, max_positions, int(bool(weight_grads)))
@@ -690,6 +782,55 @@ def attnfuse_qknorm_rope_bwd(q, k, dqr, dkr, q_weight=None, k_weight=None, *, ep
     return dq, dk, dwq, dwk
 
 
+def _axes_bwd(q, k, dqr, dkr, q_weight, k_weight, eps, rope, theta, positions, max_positions, weight_grads, dq, dk, workspace,
+              rope_table, sections, section_order, frequencies, norm):
+    dev = _device(dqr)
+    if dqr.dim() != 4 or (dkr is not None and (not isinstance(dkr, torch.Tensor) or dkr.dim() != 4)):
+        raise ValueError("dqr must be [B, H, S, D] and dkr [B, H_kv, S, D]")
+    axes = _axes(sections, section_order, frequencies, norm, rope, dqr.shape[-1], positions)
+    tab = _axes_table(axes, frequencies, rope, theta, dqr.shape[-1], dev, max_positions, rope_table)
+    if not norm:
+        q = k = None
+        weight_grads = False
+    if _native is not None:
+        r = _native.axes_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, tab, eps, ROPE[rope], theta,
+                             max_positions, int(bool(weight_grads)), int(bool(norm)), axes[0], SECTION_ORDER[axes[1]])
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_axes_bwd")
+    if norm:
+        dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
+        if k is None and (dkr is not None or dk is not None or k_weight is not None):
+            raise ValueError("dkr, dk and k_weight need k")
+        if k is not None and dkr is None:
+            raise ValueError("k needs dkr")
+        dtype = q.dtype
+    else:
+        (B, H, S, D), Hkv, dtype, qs, ks = dqr.shape, 0 if dkr is None else dkr.shape[1], dqr.dtype, [0] * 3, [0] * 3
+        if dkr is None and dk is not None:
+            raise ValueError("dk needs dkr")
+    wt = _axes_weights(q_weight, k_weight, norm, D, dtype, dev)
+    _need(dqr, "dqr", (B, H, S, D), dtype, dev)
+    _need(positions, "positions", (len(axes[0]), B, S), torch.int32, dev)
+    dq = torch.empty_like(q if norm else dqr) if dq is None else dq
+    dqs, dks, dwq, dwk, wbytes = _rows(dq, "dq", (B, H, S, D), dtype, dev), [0, 0, 0], None, None, 0
+    if dkr is not None:
+        _need(dkr, "dkr", (B, Hkv, S, D), dtype, dev)
+        dk = torch.empty_like(k if norm else dkr) if dk is None else dk
+        dks = _rows(dk, "dk", (B, Hkv, S, D), dtype, dev)
+    if weight_grads:
+        t = torch.float32 if wt else torch.bfloat16
+        dwq = torch.empty(D, device=dev, dtype=t)
+        dwk = None if k is None else torch.empty(D, device=dev, dtype=t)
+        workspace, wbytes = _workspace(workspace, attnfuse_qknorm_rope_bwd_workspace_bytes(B, H, Hkv, S, D, dtype), dev)
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_qknorm_axes_bwd(
+            _ptr(q), _ptr(k), _ptr(dqr), _ptr(dkr), _ptr(dq), _ptr(dk), _ptr(dwq), _ptr(dwk), _ptr(q_weight), _ptr(k_weight),
+            wt, int(bool(norm)), float(eps), *qs, *ks, *dqs, *dks, _ptr(workspace), wbytes, B, H, Hkv, S, D, DTYPE[dtype],
+            ROPE[rope], float(theta), *_axes_rows(tab, max_positions), _ptr(positions), *_axes_args(axes), _stream())
+    _check(code, "attnfuse_qknorm_axes_bwd")
+    return dq, dk, dwq, dwk
+
+
 def _pages(k_cache, v_cache, Hkv, D, dtype, device):
     """(pages, page size, strides of both) of a paged cache [num_pages, H_kv, page_size, D]."""
     if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
@@ -701,12 +842,15 @@ def _pages(k_cache, v_cache, Hkv, D, dtype, device):
 
 def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None, k_weight=None, *, norm=True, eps=1e-6,
                                 rope="neox", theta=10000.0, positions=None, max_positions=None, out_q=None,
-                                rope_table=None):
+                                rope_table=None, sections=None, section_order="blocks", frequencies="shared"):
     """Qr [T, H, D]: the queries of T new tokens, normed (unless ``norm`` is False) and rotated at ``positions`` (int32
     [T], all below ``max_positions``, or NaN); their keys, likewise, and values are written to the pages [num_pages, H_kv,
     page_size, D] at ``slots`` (int64 [T]: page * page_size + place; -1: nowhere); see attnfuse_qknorm_rope_append in
     include/attnfuse_llm.h.  q, k, v and the pages may lie apart (a fused projection's slices, pages [num_pages, page_size,
-    H_kv, D] transposed)."""
+    H_kv, D] transposed).  With ``sections`` the positions are int32 [axes, T], as in attnfuse_qknorm_rope."""
+    if sections is not None:
+        return _axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, norm, eps, rope, theta, positions,
+                            max_positions, out_q, rope_table, sections, section_order, frequencies)
     if _native is not None:
         r = _native.append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, rope_table, _TABLES,
                            int(bool(norm)), eps, ROPE.get(rope, -1), theta, max_positions)
@@ -732,6 +876,36 @@ def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None,
             wt, int(bool(norm)), float(eps), *qs, *ks, *vs, *kps, *vps, T, H, Hkv, D, pages, page, DTYPE[q.dtype],
             ROPE[rope], float(theta), tp, tr, _ptr(positions), _stream())
     _check(code, "attnfuse_qknorm_rope_append")
+    return out_q
+
+
+def _axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, norm, eps, rope, theta, positions, max_positions, out_q,
+                 rope_table, sections, section_order, frequencies):
+    dev = _device(q)
+    axes = _axes(sections, section_order, frequencies, norm, rope, q.shape[-1], positions)
+    tab = _axes_table(axes, frequencies, rope, theta, q.shape[-1], dev, max_positions, rope_table)
+    if _native is not None:
+        r = _native.axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, tab, eps, ROPE[rope],
+                                theta, max_positions, int(bool(norm)), axes[0], SECTION_ORDER[axes[1]])
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_axes_append")[0]
+    if q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
+        raise ValueError("q must be [T, H, D] and k/v [T, H_kv, D]")
+    T, H, D = q.shape
+    Hkv = k.shape[1]
+    qs = _rows(q, "q", (T, H, D), q.dtype, dev)
+    ks, vs = _rows(k, "k", (T, Hkv, D), q.dtype, dev), _rows(v, "v", (T, Hkv, D), q.dtype, dev)
+    wt = _axes_weights(q_weight, k_weight, norm, D, q.dtype, dev)
+    pages, page, (kps, vps) = _pages(k_cache, v_cache, Hkv, D, q.dtype, dev)
+    _need(slots, "slots", (T,), torch.int64, dev)
+    _need(positions, "positions", (len(axes[0]), T), torch.int32, dev)
+    out_q = _opt(out_q, "out_q", (T, H, D), q.dtype, dev)
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_qknorm_axes_append(
+            _ptr(q), _ptr(k), _ptr(v), _ptr(out_q), _ptr(k_cache), _ptr(v_cache), _ptr(slots), _ptr(q_weight), _ptr(k_weight),
+            wt, int(bool(norm)), float(eps), *qs, *ks, *vs, *kps, *vps, T, H, Hkv, D, pages, page, DTYPE[q.dtype],
+            ROPE[rope], float(theta), *_axes_rows(tab, max_positions), _ptr(positions), *_axes_args(axes), _stream())
+    _check(code, "attnfuse_qknorm_axes_append")
     return out_q
 
 

@@ -126,10 +126,49 @@ class _QkNormRope(torch.autograd.Function):
         return dq, dk, dqw if want[2] else None, dkw if want[3] else None, None, None, None, None, None, None
 
 
+class _QkNormAxes(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, q, k, q_weight, k_weight, positions, rope_table, cfg):
+        ctx.cfg = cfg
+        kept = (q, k, q_weight, k_weight) if cfg["norm"] else (None,) * 4   # the rotation alone needs none of them
+        ctx.save_for_backward(*kept, positions, rope_table)
+        return api.attnfuse_qknorm_rope(q, k, q_weight, k_weight, positions=positions, rope_table=rope_table, **cfg)
+
+    @staticmethod
+    @_once
+    def backward(ctx, dqr, dkr):
+        q, k, qw, kw, positions, table = ctx.saved_tensors
+        want = ctx.needs_input_grad
+        dq, dk, dqw, dkw = api.attnfuse_qknorm_rope_bwd(
+            q, k, dqr.contiguous(), None if dkr is None else dkr.contiguous(), qw, kw, positions=positions, rope_table=table,
+            weight_grads=want[2] or want[3], **ctx.cfg)
+        return dq, dk, dqw if want[2] else None, dkw if want[3] else None, None, None, None
+
+
+def _axes_grad(q, k, q_weight, k_weight, eps, rope, theta, positions, max_positions, rope_table, sections, section_order,
+               frequencies, norm):
+    dev = api._device(q)
+    axes = api._axes(sections, section_order, frequencies, norm, rope, q.shape[-1], positions)
+    tab = api._axes_table(axes, frequencies, rope, theta, q.shape[-1], dev, max_positions, rope_table)
+    if api._native is not None:   # the same function, its backward in C++
+        r = api._native.axes_grad(q, k, q_weight, k_weight, positions, tab, eps, api.ROPE[rope], theta, max_positions,
+                                  int(bool(norm)), axes[0], api.SECTION_ORDER[axes[1]])
+        if r is not None:
+            return api._result(r, "attnfuse_qknorm_axes")
+    cfg = dict(eps=eps, rope=rope, theta=theta, max_positions=max_positions, sections=axes[0], section_order=section_order,
+               frequencies=frequencies, norm=bool(norm))
+    return _QkNormAxes.apply(q, k, q_weight, k_weight, positions, tab, cfg)
+
+
 def qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, rope="neox", theta=10000.0, positions=None,
-                max_positions=None, rope_table=None):
+                max_positions=None, rope_table=None, sections=None, section_order="blocks", frequencies="shared", norm=True):
     """Differentiable norm and rotation of query and key rows: (Qr, Kr), or Qr without k; gradients for q, k and the
-    weights.  Arguments as api.attnfuse_qknorm_rope."""
+    weights.  Arguments as api.attnfuse_qknorm_rope (with ``sections``: positions of several axes; norm=False then keeps
+    nothing but the positions for the backward)."""
+    if sections is not None or not norm:
+        qr, kr = _axes_grad(q, k, q_weight, k_weight, eps, rope, theta, positions, max_positions, rope_table, sections,
+                            section_order, frequencies, norm)
+        return qr if k is None else (qr, kr)
     if api._native is not None:   # the same function, its backward in C++
         r = api._native.qknorm_grad(q, k, q_weight, k_weight, positions, rope_table, api._TABLES, eps, api.ROPE.get(rope, -1),
                                     theta, max_positions)

@@ -73,6 +73,51 @@ bool qknorm_wgs(int B, int H, int H_kv, int S, int D, int (&wgs)[2]) {
   return true;
 }
 
+// ---------------------------------------------------------------- positions of several axes
+// Which axis each of the D / 2 pairs turns by (n 0: positions of one axis for all).
+struct Axes {
+  int n = 0;
+  uint8_t axis[64], rung[64], size[64];   // of a pair: its axis, how many pairs of that axis come before it, and the axis's pairs
+
+  void fill(af::QkNormParams& p, int D) const {
+    if (!n) return;
+    p.axes = n;
+    p.by_two = true;
+    for (int i = 0; i < D / 2; ++i) {
+      p.axis[i / 16] |= (uint32_t)axis[i] << (2 * (i % 16));
+      p.by_two = p.by_two && axis[i] == axis[i & ~1];
+    }
+  }
+};
+
+int check_axes(int axes, const int* sections, int order, int D, Axes& out) {
+  if (axes < 1 || axes > 4 || !sections || D < 2 || D % 2 != 0) return AF_ERR_INVALID_ARG;
+  if (order != AF_SECTIONS_BLOCKS && order != AF_SECTIONS_TURNS) return AF_ERR_INVALID_ARG;
+  long long sum = 0;
+  for (int a = 0; a < axes; ++a) {
+    if (sections[a] < 1 || sections[a] > D / 2) return AF_ERR_INVALID_ARG;
+    sum += sections[a];
+  }
+  if (sum != D / 2) return AF_ERR_INVALID_ARG;
+  if (!supported_d(D)) return AF_ERR_UNSUPPORTED;
+  out.n = axes;
+  int i = 0;
+  auto give = [&](int a, int r) {
+    out.axis[i] = (uint8_t)a;
+    out.rung[i] = (uint8_t)r;
+    out.size[i++] = (uint8_t)sections[a];
+  };
+  if (order == AF_SECTIONS_BLOCKS) {
+    for (int a = 0; a < axes; ++a)
+      for (int r = 0; r < sections[a]; ++r) give(a, r);
+  } else {
+    for (int r = 0; r < D / 2; ++r)
+      for (int a = 0; a < axes; ++a)
+        if (r < sections[a]) give(a, r);
+  }
+  return AF_OK;
+}
+
 // Page size -> shift, or -1 where the kernels have none.
 int page_shift_of(int page_size) {
   for (int s = 4; s <= 20; ++s)
@@ -165,23 +210,21 @@ int decode_impl(af::PagedParams& p, const void* Q, const void* K, const void* V,
   return map_launch(af::launch_decode_paged(D, rope, alibi_slopes != nullptr, p, static_cast<hipStream_t>(stream)));
 }
 
-}  // namespace
-
-extern "C" {
-
-int attnfuse_qknorm_rope(const void* Q, const void* K, void* Qr, void* Kr, const void* q_weight, const void* k_weight,
-                         int weight_dtype, float eps,
-                         long long q_stride_b, long long q_stride_h, long long q_stride_s,
-                         long long k_stride_b, long long k_stride_h, long long k_stride_s,
-                         int B, int H, int H_kv, int S, int D, int dtype,
-                         int rope, float rope_theta, const float* rope_table, int rope_table_rows,
-                         const int* positions, void* stream) {
+// attnfuse_qknorm_rope, or with axes.n > 0 attnfuse_qknorm_axes.
+int qknorm_fwd(const void* Q, const void* K, void* Qr, void* Kr, const void* q_weight, const void* k_weight,
+               int weight_dtype, int norm, float eps,
+               long long q_stride_b, long long q_stride_h, long long q_stride_s,
+               long long k_stride_b, long long k_stride_h, long long k_stride_s,
+               int B, int H, int H_kv, int S, int D, int dtype,
+               int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+               const int* positions, const Axes& axes, void* stream) {
   if (!Q || !Qr || !K != !Kr) return AF_ERR_INVALID_ARG;
   if (!K) H_kv = 0;
   else if (H_kv < 1) return AF_ERR_INVALID_ARG;
   for (const void* x : {Q, K, (const void*)Qr, (const void*)Kr, q_weight, k_weight})
     if (!aligned16(x)) return AF_ERR_INVALID_ARG;
-  if (!qknorm_sizes(B, H, H_kv, S, D, dtype) || !(std::isfinite(eps) && eps >= 0.f)) return AF_ERR_INVALID_ARG;
+  if (!qknorm_sizes(B, H, H_kv, S, D, dtype) || (norm && !(std::isfinite(eps) && eps >= 0.f))) return AF_ERR_INVALID_ARG;
+  if (!norm && (q_weight || k_weight)) return AF_ERR_INVALID_ARG;
   if (weight_dtype != AF_DTYPE_BF16 && weight_dtype != AF_DTYPE_FP32) return AF_ERR_INVALID_ARG;
   if (!strides_ok({{B, q_stride_b}, {H, q_stride_h}, {S, q_stride_s}}, D, dtype, false)) return AF_ERR_INVALID_ARG;
   if (K && !strides_ok({{B, k_stride_b}, {H_kv, k_stride_h}, {S, k_stride_s}}, D, dtype, false)) return AF_ERR_INVALID_ARG;
@@ -196,6 +239,7 @@ int attnfuse_qknorm_rope(const void* Q, const void* K, void* Qr, void* Kr, const
   if (K && Kr == K && !same(H_kv, k_stride_b, k_stride_h, k_stride_s)) return AF_ERR_INVALID_ARG;
   int rc = check_rope(rope, rope_theta);
   if (rc != AF_OK) return rc;
+  if (axes.n && (rope == AF_ROPE_NONE || !positions)) return AF_ERR_INVALID_ARG;
   const void* outs[] = {Qr, Kr};
   if ((rc = check_table(rope, rope_table, rope_table_rows, positions ? 1 : S, outs, 2)) != AF_OK) return rc;
   if (!aligned4(positions)) return AF_ERR_INVALID_ARG;
@@ -210,29 +254,26 @@ int attnfuse_qknorm_rope(const void* Q, const void* K, void* Qr, void* Kr, const
   p.xs[1][0] = k_stride_b; p.xs[1][1] = k_stride_h; p.xs[1][2] = k_stride_s;
   p.heads[0] = H; p.heads[1] = H_kv;
   p.B = B; p.S = S; p.eps = eps;
+  p.norm = norm != 0;
+  axes.fill(p, D);
   p.table = reinterpret_cast<const float2*>(rope_table);
   p.rows = rope_table_rows;
   p.positions = rope != AF_ROPE_NONE ? positions : nullptr;
   return map_launch(af::launch_qknorm(af::QKNORM_FWD, dtype == AF_DTYPE_FP32, D, rope, p, static_cast<hipStream_t>(stream)));
 }
 
-size_t attnfuse_qknorm_rope_bwd_workspace_bytes(int B, int H, int H_kv, int S, int D, int dtype) {
-  int wgs[2];
-  if (!qknorm_sizes(B, H, H_kv, S, D, dtype) || !supported_d(D) || !qknorm_wgs(B, H, H_kv, S, D, wgs)) return 0;
-  return (size_t)(wgs[0] + wgs[1]) * D * sizeof(float);
-}
-
-int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, const void* dKr, void* dQ, void* dK,
-                             void* dq_weight, void* dk_weight, const void* q_weight, const void* k_weight,
-                             int weight_dtype, float eps,
-                             long long q_stride_b, long long q_stride_h, long long q_stride_s,
-                             long long k_stride_b, long long k_stride_h, long long k_stride_s,
-                             long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
-                             long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
-                             void* workspace, size_t workspace_bytes,
-                             int B, int H, int H_kv, int S, int D, int dtype,
-                             int rope, float rope_theta, const float* rope_table, int rope_table_rows,
-                             const int* positions, void* stream) {
+// attnfuse_qknorm_rope_bwd, or with axes.n > 0 attnfuse_qknorm_axes_bwd under a norm.
+int qknorm_bwd(const void* Q, const void* K, const void* dQr, const void* dKr, void* dQ, void* dK,
+               void* dq_weight, void* dk_weight, const void* q_weight, const void* k_weight,
+               int weight_dtype, float eps,
+               long long q_stride_b, long long q_stride_h, long long q_stride_s,
+               long long k_stride_b, long long k_stride_h, long long k_stride_s,
+               long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
+               long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
+               void* workspace, size_t workspace_bytes,
+               int B, int H, int H_kv, int S, int D, int dtype,
+               int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+               const int* positions, const Axes& axes, void* stream) {
   if (!Q || !dQr || !dQ || !K != !dKr || !K != !dK) return AF_ERR_INVALID_ARG;
   if (!K) { H_kv = 0; dk_weight = nullptr; }
   else if (H_kv < 1) return AF_ERR_INVALID_ARG;
@@ -256,6 +297,7 @@ int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, cons
     return AF_ERR_INVALID_ARG;
   int rc = check_rope(rope, rope_theta);
   if (rc != AF_OK) return rc;
+  if (axes.n && (rope == AF_ROPE_NONE || !positions)) return AF_ERR_INVALID_ARG;
   if ((rc = check_table(rope, rope_table, rope_table_rows, positions ? 1 : S, nullptr, 0)) != AF_OK) return rc;
   if (!supported_d(D)) return AF_ERR_UNSUPPORTED;
   af::QkNormParams p{};
@@ -274,6 +316,8 @@ int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, cons
   p.ys[1][0] = dk_stride_b; p.ys[1][1] = dk_stride_h; p.ys[1][2] = dk_stride_s;
   p.heads[0] = H; p.heads[1] = H_kv;
   p.B = B; p.S = S; p.eps = eps;
+  p.norm = true;
+  axes.fill(p, D);
   p.table = reinterpret_cast<const float2*>(rope_table);
   p.rows = rope_table_rows;
   p.positions = rope != AF_ROPE_NONE ? positions : nullptr;
@@ -281,16 +325,59 @@ int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, cons
   return map_launch(af::launch_qknorm(af::QKNORM_BWD, dtype == AF_DTYPE_FP32, D, rope, p, static_cast<hipStream_t>(stream)));
 }
 
-int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
-                                const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
-                                int norm, float eps,
-                                long long q_stride_t, long long q_stride_h, long long k_stride_t, long long k_stride_h,
-                                long long v_stride_t, long long v_stride_h,
-                                long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
-                                long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
-                                int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
-                                int rope, float rope_theta, const float* rope_table, int rope_table_rows,
-                                const int* positions, void* stream) {
+// The backward of attnfuse_qknorm_axes without norm: dx = R^T dout.
+int qknorm_unturn(const void* dQr, const void* dKr, void* dQ, void* dK,
+                  long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
+                  long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
+                  int B, int H, int H_kv, int S, int D, int dtype,
+                  int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                  const int* positions, const Axes& axes, void* stream) {
+  if (!dQr || !dQ || !dKr != !dK) return AF_ERR_INVALID_ARG;
+  if (!dK) H_kv = 0;
+  else if (H_kv < 1) return AF_ERR_INVALID_ARG;
+  for (const void* x : {dQr, dKr, (const void*)dQ, (const void*)dK})
+    if (!aligned16(x)) return AF_ERR_INVALID_ARG;
+  if (!qknorm_sizes(B, H, H_kv, S, D, dtype)) return AF_ERR_INVALID_ARG;
+  if (!strides_ok({{B, dq_stride_b}, {H, dq_stride_h}, {S, dq_stride_s}}, D, dtype, true)) return AF_ERR_INVALID_ARG;
+  if (dK && !strides_ok({{B, dk_stride_b}, {H_kv, dk_stride_h}, {S, dk_stride_s}}, D, dtype, true)) return AF_ERR_INVALID_ARG;
+  if (any_alias({dQ, dK}, {dQr, dKr, positions}) || outs_alias({dQ, dK})) return AF_ERR_INVALID_ARG;
+  int rc = check_rope(rope, rope_theta);
+  if (rc != AF_OK) return rc;
+  if (rope == AF_ROPE_NONE || !positions || !aligned4(positions)) return AF_ERR_INVALID_ARG;
+  const void* outs[] = {dQ, dK};
+  if ((rc = check_table(rope, rope_table, rope_table_rows, 1, outs, 2)) != AF_OK) return rc;
+  if (!supported_d(D)) return AF_ERR_UNSUPPORTED;
+
+  af::QkNormParams p{};
+  p.x[0] = dQr; p.x[1] = dKr;
+  p.y[0] = dQ; p.y[1] = dK;
+  const int heads[2] = {H, H_kv};
+  for (int t = 0; t < 2; ++t) {
+    p.xs[t][0] = (long long)heads[t] * S * D; p.xs[t][1] = (long long)S * D; p.xs[t][2] = D;
+  }
+  p.ys[0][0] = dq_stride_b; p.ys[0][1] = dq_stride_h; p.ys[0][2] = dq_stride_s;
+  p.ys[1][0] = dk_stride_b; p.ys[1][1] = dk_stride_h; p.ys[1][2] = dk_stride_s;
+  p.heads[0] = H; p.heads[1] = H_kv;
+  p.B = B; p.S = S;
+  axes.fill(p, D);
+  p.table = reinterpret_cast<const float2*>(rope_table);
+  p.rows = rope_table_rows;
+  p.positions = positions;
+  return map_launch(
+      af::launch_qknorm(af::QKNORM_UNTURN, dtype == AF_DTYPE_FP32, D, rope, p, static_cast<hipStream_t>(stream)));
+}
+
+// attnfuse_qknorm_rope_append, or with axes.n > 0 attnfuse_qknorm_axes_append.
+int qknorm_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
+                  const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
+                  int norm, float eps,
+                  long long q_stride_t, long long q_stride_h, long long k_stride_t, long long k_stride_h,
+                  long long v_stride_t, long long v_stride_h,
+                  long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                  long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                  int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
+                  int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                  const int* positions, const Axes& axes, void* stream) {
   if (!Q || !K || !V || !Qr || !K_pages || !V_pages || !slots) return AF_ERR_INVALID_ARG;
   for (const void* x : {Q, K, V, (const void*)Qr, (const void*)K_pages, (const void*)V_pages, q_weight, k_weight})
     if (!aligned16(x)) return AF_ERR_INVALID_ARG;
@@ -309,7 +396,7 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
     return AF_ERR_INVALID_ARG;
   int rc = check_rope(rope, rope_theta);
   if (rc != AF_OK) return rc;
-  if (rope != AF_ROPE_NONE && !positions) return AF_ERR_INVALID_ARG;
+  if (rope != AF_ROPE_NONE ? !positions : axes.n > 0) return AF_ERR_INVALID_ARG;
   const void* outs[] = {Qr, K_pages, V_pages};
   if ((rc = check_table(rope, rope_table, rope_table_rows, 1, outs, 3)) != AF_OK) return rc;
   const int shift = page_shift_of(page_size);
@@ -329,6 +416,7 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
   p.ys[2][0] = vp_stride_p; p.ys[2][1] = vp_stride_h; p.ys[2][2] = vp_stride_s;
   p.heads[0] = H; p.heads[1] = H_kv;
   p.B = 1; p.S = T;
+  axes.fill(p, D);
   p.table = reinterpret_cast<const float2*>(rope_table);
   p.rows = rope_table_rows;
   p.positions = rope != AF_ROPE_NONE ? positions : nullptr;
@@ -337,6 +425,138 @@ int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, voi
   p.page_shift = shift;
   return map_launch(
       af::launch_qknorm(af::QKNORM_APPEND, dtype == AF_DTYPE_FP32, D, rope, p, static_cast<hipStream_t>(stream)));
+}
+
+}  // namespace
+
+extern "C" {
+
+int attnfuse_qknorm_rope(const void* Q, const void* K, void* Qr, void* Kr, const void* q_weight, const void* k_weight,
+                         int weight_dtype, float eps,
+                         long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                         long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                         int B, int H, int H_kv, int S, int D, int dtype,
+                         int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                         const int* positions, void* stream) {
+  return qknorm_fwd(Q, K, Qr, Kr, q_weight, k_weight, weight_dtype, 1, eps, q_stride_b, q_stride_h, q_stride_s, k_stride_b,
+                    k_stride_h, k_stride_s, B, H, H_kv, S, D, dtype, rope, rope_theta, rope_table, rope_table_rows, positions,
+                    Axes{}, stream);
+}
+
+int attnfuse_qknorm_axes(const void* Q, const void* K, void* Qr, void* Kr, const void* q_weight, const void* k_weight,
+                         int weight_dtype, int norm, float eps,
+                         long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                         long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                         int B, int H, int H_kv, int S, int D, int dtype,
+                         int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                         const int* positions, int axes, const int* sections, int section_order, void* stream) {
+  Axes x;
+  const int rc = check_axes(axes, sections, section_order, D, x);
+  if (rc != AF_OK) return rc;
+  return qknorm_fwd(Q, K, Qr, Kr, q_weight, k_weight, weight_dtype, norm, eps, q_stride_b, q_stride_h, q_stride_s, k_stride_b,
+                    k_stride_h, k_stride_s, B, H, H_kv, S, D, dtype, rope, rope_theta, rope_table, rope_table_rows, positions,
+                    x, stream);
+}
+
+int attnfuse_axes_table_fill(float* table, int rows, int D, float rope_theta, int axes, const int* sections,
+                             int section_order, int frequencies, void* stream) {
+  if (!table || !aligned16(table) || rows < 1 || rows > kMaxTableRows) return AF_ERR_INVALID_ARG;
+  if (!(std::isfinite(rope_theta) && rope_theta > 0.f)) return AF_ERR_INVALID_ARG;
+  if (frequencies != AF_FREQUENCIES_SHARED && frequencies != AF_FREQUENCIES_OWN) return AF_ERR_INVALID_ARG;
+  Axes x;
+  const int rc = check_axes(axes, sections, section_order, D, x);
+  if (rc != AF_OK) return rc;
+  af::AxesRungs r{};
+  r.half = D / 2;
+  for (int i = 0; i < D / 2; ++i) {
+    r.num[i] = frequencies == AF_FREQUENCIES_OWN ? x.rung[i] : (uint8_t)i;
+    r.den[i] = frequencies == AF_FREQUENCIES_OWN ? x.size[i] : (uint8_t)(D / 2);
+  }
+  return map_launch(af::launch_axes_table(reinterpret_cast<float2*>(table), rows, r, (double)rope_theta,
+                                          static_cast<hipStream_t>(stream)));
+}
+
+size_t attnfuse_qknorm_rope_bwd_workspace_bytes(int B, int H, int H_kv, int S, int D, int dtype) {
+  int wgs[2];
+  if (!qknorm_sizes(B, H, H_kv, S, D, dtype) || !supported_d(D) || !qknorm_wgs(B, H, H_kv, S, D, wgs)) return 0;
+  return (size_t)(wgs[0] + wgs[1]) * D * sizeof(float);
+}
+
+int attnfuse_qknorm_rope_bwd(const void* Q, const void* K, const void* dQr, const void* dKr, void* dQ, void* dK,
+                             void* dq_weight, void* dk_weight, const void* q_weight, const void* k_weight,
+                             int weight_dtype, float eps,
+                             long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                             long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                             long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
+                             long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
+                             void* workspace, size_t workspace_bytes,
+                             int B, int H, int H_kv, int S, int D, int dtype,
+                             int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                             const int* positions, void* stream) {
+  return qknorm_bwd(Q, K, dQr, dKr, dQ, dK, dq_weight, dk_weight, q_weight, k_weight, weight_dtype, eps, q_stride_b,
+                    q_stride_h, q_stride_s, k_stride_b, k_stride_h, k_stride_s, dq_stride_b, dq_stride_h, dq_stride_s,
+                    dk_stride_b, dk_stride_h, dk_stride_s, workspace, workspace_bytes, B, H, H_kv, S, D, dtype, rope,
+                    rope_theta, rope_table, rope_table_rows, positions, Axes{}, stream);
+}
+
+int attnfuse_qknorm_axes_bwd(const void* Q, const void* K, const void* dQr, const void* dKr, void* dQ, void* dK,
+                             void* dq_weight, void* dk_weight, const void* q_weight, const void* k_weight,
+                             int weight_dtype, int norm, float eps,
+                             long long q_stride_b, long long q_stride_h, long long q_stride_s,
+                             long long k_stride_b, long long k_stride_h, long long k_stride_s,
+                             long long dq_stride_b, long long dq_stride_h, long long dq_stride_s,
+                             long long dk_stride_b, long long dk_stride_h, long long dk_stride_s,
+                             void* workspace, size_t workspace_bytes,
+                             int B, int H, int H_kv, int S, int D, int dtype,
+                             int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                             const int* positions, int axes, const int* sections, int section_order, void* stream) {
+  Axes x;
+  const int rc = check_axes(axes, sections, section_order, D, x);
+  if (rc != AF_OK) return rc;
+  if (!norm) {
+    if (q_weight || k_weight || dq_weight || dk_weight) return AF_ERR_INVALID_ARG;
+    return qknorm_unturn(dQr, dKr, dQ, dK, dq_stride_b, dq_stride_h, dq_stride_s, dk_stride_b, dk_stride_h, dk_stride_s, B, H,
+                         H_kv, S, D, dtype, rope, rope_theta, rope_table, rope_table_rows, positions, x, stream);
+  }
+  return qknorm_bwd(Q, K, dQr, dKr, dQ, dK, dq_weight, dk_weight, q_weight, k_weight, weight_dtype, eps, q_stride_b,
+                    q_stride_h, q_stride_s, k_stride_b, k_stride_h, k_stride_s, dq_stride_b, dq_stride_h, dq_stride_s,
+                    dk_stride_b, dk_stride_h, dk_stride_s, workspace, workspace_bytes, B, H, H_kv, S, D, dtype, rope,
+                    rope_theta, rope_table, rope_table_rows, positions, x, stream);
+}
+
+int attnfuse_qknorm_rope_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
+                                const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
+                                int norm, float eps,
+                                long long q_stride_t, long long q_stride_h, long long k_stride_t, long long k_stride_h,
+                                long long v_stride_t, long long v_stride_h,
+                                long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                                long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                                int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
+                                int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                                const int* positions, void* stream) {
+  return qknorm_append(Q, K, V, Qr, K_pages, V_pages, slots, q_weight, k_weight, weight_dtype, norm, eps, q_stride_t,
+                       q_stride_h, k_stride_t, k_stride_h, v_stride_t, v_stride_h, kp_stride_p, kp_stride_h, kp_stride_s,
+                       vp_stride_p, vp_stride_h, vp_stride_s, T, H, H_kv, D, num_pages, page_size, dtype, rope,
+                       rope_theta, rope_table, rope_table_rows, positions, Axes{}, stream);
+}
+
+int attnfuse_qknorm_axes_append(const void* Q, const void* K, const void* V, void* Qr, void* K_pages, void* V_pages,
+                                const long long* slots, const void* q_weight, const void* k_weight, int weight_dtype,
+                                int norm, float eps,
+                                long long q_stride_t, long long q_stride_h, long long k_stride_t, long long k_stride_h,
+                                long long v_stride_t, long long v_stride_h,
+                                long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                                long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                                int T, int H, int H_kv, int D, int num_pages, int page_size, int dtype,
+                                int rope, float rope_theta, const float* rope_table, int rope_table_rows,
+                                const int* positions, int axes, const int* sections, int section_order, void* stream) {
+  Axes x;
+  const int rc = check_axes(axes, sections, section_order, D, x);
+  if (rc != AF_OK) return rc;
+  return qknorm_append(Q, K, V, Qr, K_pages, V_pages, slots, q_weight, k_weight, weight_dtype, norm, eps, q_stride_t,
+                       q_stride_h, k_stride_t, k_stride_h, v_stride_t, v_stride_h, kp_stride_p, kp_stride_h, kp_stride_s,
+                       vp_stride_p, vp_stride_h, vp_stride_s, T, H, H_kv, D, num_pages, page_size, dtype, rope,
+                       rope_theta, rope_table, rope_table_rows, positions, x, stream);
 }
 
 size_t attnfuse_decode_paged_workspace_bytes(int B, int H, int H_kv, int S_kv, int D, int window, int sinks) {

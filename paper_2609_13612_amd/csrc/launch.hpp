@@ -94,7 +94,8 @@ struct RopeParams {
 
 // Norm and rotation of query and key rows (qknorm.hip).  Index 0 is q, 1 k, 2 v;
 // strides in elements: batch (of a cache: page), head, position.
-enum { QKNORM_FWD = 0, QKNORM_BWD = 1, QKNORM_APPEND = 2 };
+// UNTURN: the inverse rotation alone (y with strides), for positions of several axes.
+enum { QKNORM_FWD = 0, QKNORM_BWD = 1, QKNORM_APPEND = 2, QKNORM_UNTURN = 3 };
 constexpr int QKNORM_BWD_HPT = 2;   // heads a thread takes in the backward
 // Batches whose rows share a workgroup of 256 / (D / 16) rows: several of them fit.
 inline int qknorm_per(int S, int D) { return 2 * S <= 4096 / D ? 4096 / D / S : 1; }
@@ -109,11 +110,14 @@ struct QkNormParams {
   int heads[2];           // H, H_kv (0: no k)
   int B, S;               // append: 1, the tokens
   int per;                // batches a workgroup takes the rows of (qknorm_per)
-  bool w32, norm;         // weights are fp32; append: norm the rows
+  bool w32, norm;         // weights are fp32; append and several axes: norm the rows
   float eps;
   const float2* table;    // [rows][D/2] (cos, sin)
   int rows;
-  const int* positions;   // [B, S], nullptr: 0..S-1
+  const int* positions;   // [B, S], nullptr: 0..S-1; several axes: [axes, B, S]
+  int axes;               // 0: positions of one axis for every pair; else 1 .. 4
+  uint32_t axis[4];       // the axis of every pair, two bits each from the lowest on
+  bool by_two;            // pairs 2 i and 2 i + 1 are on one axis, for every i
   const long long* slots; // append: [T]
   long long nslots;       // append: pages * page size
   int page_shift;
@@ -174,6 +178,15 @@ int launch_rope(bool fp32, int D, int rope, bool inverse, const RopeParams& p, h
 int launch_rope_f16(int D, int rope, const RopeParams& p, hipStream_t st);
 int launch_decode_paged(int D, int rope, bool alibi, const PagedParams& p, hipStream_t st);
 int launch_qknorm(int what, bool fp32, int D, int rope, const QkNormParams& p, hipStream_t st);
+int launch_qknorm_axes(int what, bool fp32, int D, int rope, const QkNormParams& p, hipStream_t st);   // p.axes > 0
+
+// The exponents of theta of a table whose axes have ladders of their own: pair i has
+// frequency theta^(-num[i] / den[i]).
+struct AxesRungs {
+  int half;               // D / 2
+  uint8_t num[64], den[64];
+};
+int launch_axes_table(float2* table, int rows, const AxesRungs& r, double theta, hipStream_t st);
 int launch_rope_table(float2* table, int rows, int D, double theta, hipStream_t st);
 
 // Static device scratch of the decode entry point that allocates nothing: its

@@ -516,18 +516,37 @@ struct Qk {
   }
 };
 
-// A norm call's variant.
+// A norm call's variant; positions of several axes: their sections (n 0: one axis).
 struct Norm {
   float eps;
   int rope;
   double theta;
+  bool norm = true;
+  int n = 0, sections[4] = {0, 0, 0, 0}, order = 0;
   explicit Norm(Args& a) : eps((float)a.number()), rope(a.index()), theta(a.number()) {}
   Norm(float e, int r, double t) : eps(e), rope(r), theta(t) {}
+  void take_axes(Args& a) {   // norm, sections, section_order
+    norm = a.whole() != 0;
+    PyObject* s = a.next();
+    if (!PyTuple_CheckExact(s) || PyTuple_GET_SIZE(s) < 1 || PyTuple_GET_SIZE(s) > 4) throw NotPlain{};
+    n = (int)PyTuple_GET_SIZE(s);
+    for (int i = 0; i < n; ++i) {
+      PyObject* x = PyTuple_GET_ITEM(s, i);
+      Args one{&x, 1};
+      sections[i] = one.size();
+    }
+    order = a.index();
+  }
 };
 
 int norm_fwd(const Qk& x, const Weights& w, const Norm& n, const Table& table, const int* positions, const Tensor& oq,
              const Tensor& ok) {
   return enqueue(x.dev, [&](void* st) {
+    if (n.n)
+      return attnfuse_qknorm_axes(in(x.q), x.k ? in(*x.k) : nullptr, out(oq), x.k ? out(ok) : nullptr, w.q, w.k, w.type,
+                                  n.norm, n.eps, x.qs.s[0], x.qs.s[1], x.qs.s[2], x.ks.s[0], x.ks.s[1], x.ks.s[2], (int)x.B,
+                                  (int)x.H, (int)x.Hkv, (int)x.S, (int)x.D, x.dtype, n.rope, (float)n.theta, table.ptr,
+                                  table.rows, positions, n.n, n.sections, n.order, st);
     return attnfuse_qknorm_rope(in(x.q), x.k ? in(*x.k) : nullptr, out(oq), x.k ? out(ok) : nullptr, w.q, w.k, w.type, n.eps,
                                 x.qs.s[0], x.qs.s[1], x.qs.s[2], x.ks.s[0], x.ks.s[1], x.ks.s[2], (int)x.B, (int)x.H,
                                 (int)x.Hkv, (int)x.S, (int)x.D, x.dtype, n.rope, (float)n.theta, table.ptr, table.rows,
@@ -551,6 +570,13 @@ int norm_bwd(const Qk& x, const Weights& w, const Norm& n, const Table& table, c
                                                                     x.dtype), x.dev);
   }
   return enqueue(x.dev, [&](void* st) {
+    if (n.n)
+      return attnfuse_qknorm_axes_bwd(
+          in(x.q), x.k ? in(*x.k) : nullptr, in(dqr), dkr ? in(*dkr) : nullptr, out(dq), x.k ? out(dk) : nullptr,
+          grads ? out(dqw) : nullptr, grads && x.k ? out(dkw) : nullptr, w.q, w.k, w.type, 1, n.eps, x.qs.s[0], x.qs.s[1],
+          x.qs.s[2], x.ks.s[0], x.ks.s[1], x.ks.s[2], dqs.s[0], dqs.s[1], dqs.s[2], dks.s[0], dks.s[1], dks.s[2],
+          grads ? out(ws) : nullptr, grads ? bytes_of(ws) : 0, (int)x.B, (int)x.H, (int)x.Hkv, (int)x.S, (int)x.D, x.dtype,
+          n.rope, (float)n.theta, table.ptr, table.rows, positions, n.n, n.sections, n.order, st);
     return attnfuse_qknorm_rope_bwd(
         in(x.q), x.k ? in(*x.k) : nullptr, in(dqr), dkr ? in(*dkr) : nullptr, out(dq), x.k ? out(dk) : nullptr,
         grads ? out(dqw) : nullptr, grads && x.k ? out(dkw) : nullptr, w.q, w.k, w.type, n.eps, x.qs.s[0], x.qs.s[1],
@@ -602,28 +628,146 @@ PyObject* qknorm_bwd(Args a) {
   return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dqw, &dkw});
 }
 
+// The angles of positions of several axes [axes, lead...]: the given table, of its rows
+// the first max_positions (0: all).
+struct AxesPlaced {
+  const int* positions;
+  Table table;
+  AxesPlaced(const Tensor& pos, const Tensor& tab, int64_t D, at::IntArrayRef shape, long long most, c10::Device dev) {
+    same(pos, shape, at::kInt, dev);
+    positions = static_cast<const int*>(pos.const_data_ptr());
+    if (tab.dim() != 3 || tab.size(0) > INT_MAX || most > tab.size(0)) throw NotPlain{};
+    same(tab, {tab.size(0), D / 2, 2}, at::kFloat, dev);
+    table.ptr = static_cast<const float*>(tab.const_data_ptr());
+    table.rows = (int)(most > 0 ? most : tab.size(0));
+    table.own = tab;
+  }
+};
+
+// dX = R^T dXr of a rotation without norm; dq, dk: given, or undefined and then made.
+int unturn(const Tensor& dqr, const Tensor* dkr, Tensor& dq, Tensor& dk, const Norm& n, const Table& table,
+           const int* positions) {
+  const int dtype = dtype_of(dqr);
+  const c10::Device dev = dqr.device();
+  const at::ScalarType type = dqr.scalar_type();
+  const int64_t B = dqr.size(0), H = dqr.size(1), S = dqr.size(2), D = dqr.size(3), Hkv = dkr ? dkr->size(1) : 0;
+  for (int64_t x : {B, H, S, D, Hkv}) if (x > INT_MAX) throw NotPlain{};
+  same(dqr, dqr.sizes(), type, dev);
+  if (dkr) same(*dkr, {B, Hkv, S, D}, type, dev);
+  if (!dq.defined()) dq = at::empty_like(dqr);
+  if (dkr && !dk.defined()) dk = at::empty_like(*dkr);
+  const Rows qs(dq, dqr.sizes(), type, dev);
+  Rows ks;
+  if (dkr) ks = Rows(dk, dkr->sizes(), type, dev);
+  return enqueue(dev, [&](void* st) {
+    return attnfuse_qknorm_axes_bwd(nullptr, nullptr, in(dqr), dkr ? in(*dkr) : nullptr, out(dq), dkr ? out(dk) : nullptr,
+                                    nullptr, nullptr, nullptr, nullptr, AF_DTYPE_FP32, 0, 0.f, 0, 0, 0, 0, 0, 0, qs.s[0],
+                                    qs.s[1], qs.s[2], ks.s[0], ks.s[1], ks.s[2], nullptr, 0, (int)B, (int)H, (int)Hkv, (int)S,
+                                    (int)D, dtype, n.rope, (float)n.theta, table.ptr, table.rows, positions, n.n, n.sections,
+                                    n.order, st);
+  });
+}
+
+// axes(q, k, q_weight, k_weight, out_q, out_k, positions, table, eps, rope, theta, max_positions, norm, sections,
+//      section_order) -> (Qr, Kr)
+PyObject* axes(Args a) {
+  const Tensor &q = a.need(), *k = a.tensor();
+  const Qk x(q, k);
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *ok_ = a.tensor();
+  const Tensor &pos = a.need(), &tab = a.need();
+  Norm n(a);
+  const long long most = a.positive();
+  n.take_axes(a);
+  if ((!x.k && (kw || ok_)) || (!n.norm && (qw || kw))) throw NotPlain{};
+  const Weights w(qw, kw, x.D, x.type, x.dev);
+  const AxesPlaced at_(pos, tab, x.D, {n.n, x.B, x.S}, most, x.dev);
+  const Tensor oq = out_or(oq_, x.q.sizes(), x.type, x.dev);
+  Tensor ok;
+  if (x.k) ok = out_or(ok_, x.k->sizes(), x.type, x.dev);
+  const int rc = norm_fwd(x, w, n, at_.table, at_.positions, oq, ok);
+  return rc ? PyLong_FromLong(rc) : tuple_of({&oq, &ok});
+}
+
+// axes_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, table, eps, rope, theta, max_positions,
+//          weight_grads, norm, sections, section_order) -> (dQ, dK, dq_weight, dk_weight); without norm q and k are None
+PyObject* axes_bwd(Args a) {
+  const Tensor *q = a.tensor(), *k = a.tensor(), &dqr = a.need();
+  const Tensor *dkr = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *dq_ = a.tensor(), *dk_ = a.tensor(), *ws_ = a.tensor();
+  const Tensor &pos = a.need(), &tab = a.need();
+  Norm n(a);
+  const long long most = a.positive();
+  const bool grads = a.whole() != 0;
+  n.take_axes(a);
+  Tensor dq, dk, dqw, dkw;
+  if (dq_) dq = *dq_;
+  if (dk_) dk = *dk_;
+  int rc;
+  if (!n.norm) {
+    if (q || k || qw || kw || grads || (!dkr && dk_) || dqr.dim() != 4 || (dkr && dkr->dim() != 4)) throw NotPlain{};
+    const AxesPlaced at_(pos, tab, dqr.size(3), {n.n, dqr.size(0), dqr.size(2)}, most, dqr.device());
+    rc = unturn(dqr, dkr, dq, dk, n, at_.table, at_.positions);
+  } else {
+    if (!q || !k != !dkr || (!k && (kw || dk_))) throw NotPlain{};
+    const Qk x(*q, k);
+    const Weights w(qw, kw, x.D, x.type, x.dev);
+    const AxesPlaced at_(pos, tab, x.D, {n.n, x.B, x.S}, most, x.dev);
+    if (!dq_) dq = at::empty_like(x.q);
+    if (k && !dk_) dk = at::empty_like(*k);
+    rc = norm_bwd(x, w, n, at_.table, at_.positions, dqr, dkr, dq, dk, dqw, dkw, ws_, grads);
+  }
+  return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dqw, &dkw});
+}
+
 // append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, table, tables, norm, eps, rope, theta,
 //        max_positions) -> (Qr,)
+// axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, table, eps, rope, theta,
+//             max_positions, norm, sections, section_order) -> (Qr,)
+template <bool AXES>
 PyObject* append(Args a) {
   const Tensor &q = a.need(), &k = a.need(), &v = a.need(), &kc = a.need(), &vc = a.need(), &slots = a.need();
   const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *pos = a.tensor();
   Args late = a;
-  a.i += 2;
-  const bool norm = a.whole() != 0;
-  const float eps = (float)a.number();
-  const int rope = a.index();
-  const double theta = a.number();
+  const Tensor* tab = nullptr;
+  bool norm = true;
+  if constexpr (AXES) {
+    tab = &a.need();
+  } else {
+    a.i += 2;
+    norm = a.whole() != 0;
+  }
+  Norm n(a);
+  const float eps = n.eps;
+  const int rope = n.rope;
+  const double theta = n.theta;
   const long long most = a.positive();
+  if constexpr (AXES) {
+    n.take_axes(a);
+    norm = n.norm;
+    if (!pos) throw NotPlain{};
+  }
   const int dtype = dtype_of(q);
   const c10::Device dev = q.device();
   const at::ScalarType type = q.scalar_type();
   if (q.dim() != 3 || k.dim() != 3 || kc.dim() != 4 || (rope != AF_ROPE_NONE && !pos)) throw NotPlain{};
   const int64_t T = q.size(0), H = q.size(1), D = q.size(2), Hkv = k.size(1), pages = kc.size(0), page = kc.size(2);
-  for (int64_t n : {T, H, D, Hkv, pages, page}) if (n > INT_MAX) throw NotPlain{};
+  for (int64_t m : {T, H, D, Hkv, pages, page}) if (m > INT_MAX) throw NotPlain{};
   const Rows qs(q, {T, H, D}, type, dev), ks(k, {T, Hkv, D}, type, dev), vs(v, {T, Hkv, D}, type, dev),
       kcs(kc, {pages, Hkv, page, D}, type, dev), vcs(vc, {pages, Hkv, page, D}, type, dev);
   same(slots, {T}, at::kLong, dev);
   const Weights w(qw, kw, D, type, dev);
+  if constexpr (AXES) {
+    if (!norm && (qw || kw)) throw NotPlain{};
+    const AxesPlaced at_(*pos, *tab, D, {n.n, T}, most, dev);
+    const Tensor oq = out_or(oq_, q.sizes(), type, dev);
+    const int rc = enqueue(dev, [&](void* st) {
+      return attnfuse_qknorm_axes_append(
+          in(q), in(k), in(v), out(oq), out(kc), out(vc), reinterpret_cast<const long long*>(slots.const_data_ptr()), w.q,
+          w.k, w.type, norm, eps, qs.s[0], qs.s[1], ks.s[0], ks.s[1], vs.s[0], vs.s[1], kcs.s[0], kcs.s[1], kcs.s[2],
+          vcs.s[0], vcs.s[1], vcs.s[2], (int)T, (int)H, (int)Hkv, (int)D, (int)pages, (int)page, dtype, rope, (float)theta,
+          at_.table.ptr, at_.table.rows, at_.positions, n.n, n.sections, n.order, st);
+    });
+    return rc ? PyLong_FromLong(rc) : tuple_of({&oq});
+  }
   const Placed at_(pos, late, rope, theta, D, 1, {T}, most, dev);
   const Tensor oq = out_or(oq_, q.sizes(), type, dev);
   const int rc = enqueue(dev, [&](void* st) {
@@ -827,6 +971,18 @@ Table table_in(const Tensor& t, int64_t rows) {
 // clears its bit.
 enum { HAS_K = 1, HAS_QW = 2, HAS_KW = 4, HAS_POSITIONS = 8, HAS_TABLE = 16, WEIGHT_GRADS = 32 };
 
+// The variant of a call with several axes behind the others in a context's numbers.
+void keep_axes(std::vector<double>& v, const Norm& n) {
+  v.push_back(n.n);
+  for (int s : n.sections) v.push_back(s);
+  v.push_back(n.order);
+}
+void with_axes(Norm& n, const double* v) {
+  n.n = (int)v[0];
+  for (int i = 0; i < 4; ++i) n.sections[i] = (int)v[1 + i];
+  n.order = (int)v[5];
+}
+
 struct NormFunction : torch::autograd::Function<NormFunction> {
   // The call's tensors, as forward and backward both see them.
   struct Call {
@@ -844,16 +1000,17 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
   };
 
   static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& qw, const Tensor& kw,
-                               const Tensor& positions, const Tensor& table, int64_t rows, double eps, int64_t rope,
-                               double theta, int64_t has) {
+                               const Tensor& positions, const Tensor& table, int64_t rows, const Norm& n, int64_t has) {
     const Call c(q, k, qw, kw, positions, table, rows, has);
     const Tensor oq = out_or(nullptr, c.x.q.sizes(), c.x.type, c.x.dev);
     Tensor ok;
     if (c.x.k) ok = out_or(nullptr, c.x.k->sizes(), c.x.type, c.x.dev);
-    const int rc = norm_fwd(c.x, c.w, Norm((float)eps, (int)rope, theta), c.table, c.positions, oq, ok);
+    const int rc = norm_fwd(c.x, c.w, n, c.table, c.positions, oq, ok);
     if (rc) throw Failed{rc};
     ctx->save_for_backward({q, k, qw, kw, positions, table});
-    ctx->saved_data["variant"] = std::vector<double>{eps, (double)rope, theta, (double)has, (double)rows};
+    std::vector<double> v{n.eps, (double)n.rope, n.theta, (double)has, (double)rows};
+    keep_axes(v, n);
+    ctx->saved_data["variant"] = v;
     if (c.x.k) return {oq, ok};
     return {oq};
   }
@@ -867,15 +1024,33 @@ struct NormFunction : torch::autograd::Function<NormFunction> {
       const Tensor dqr = grad[0].contiguous(), dkr = c.x.k ? grad[1].contiguous() : Tensor();
       dq = at::empty_like(c.x.q);
       if (c.x.k) dk = at::empty_like(*c.x.k);
-      const int rc = norm_bwd(c.x, c.w, Norm((float)v[0], (int)v[1], v[2]), c.table, c.positions, dqr,
+      Norm n((float)v[0], (int)v[1], v[2]);
+      with_axes(n, &v[5]);
+      const int rc = norm_bwd(c.x, c.w, n, c.table, c.positions, dqr,
                               c.x.k ? &dkr : nullptr, dq, dk, dqw, dkw, nullptr, c.has & WEIGHT_GRADS);
       if (!(c.has & HAS_QW)) dqw.reset();
       if (!(c.has & HAS_KW)) dkw.reset();
       return rc;
     });
-    return once({dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2], s[3]}, grad);
+    return once({dq, dk, dqw, dkw, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {s[0], s[1], s[2], s[3]}, grad);
   }
 };
+
+PyObject* norm_apply(const Tensor& q, const Tensor* k, const Tensor* qw, const Tensor* kw, const Tensor* pos, const Table& tab,
+                     const Norm& n) {
+  const Tensor& table = tab.own;
+  const bool grads = (qw && qw->requires_grad()) || (kw && kw->requires_grad());
+  const int64_t has = (k ? HAS_K : 0) | (qw ? HAS_QW : 0) | (kw ? HAS_KW : 0) | (pos ? HAS_POSITIONS : 0) |
+                      (table.defined() ? HAS_TABLE : 0) | (grads ? WEIGHT_GRADS : 0);
+  try {
+    const variable_list r = NormFunction::apply(q, k ? *k : q, qw ? *qw : q, kw ? *kw : q, pos ? *pos : q,
+                                                table.defined() ? table : q, (int64_t)tab.rows, n, has);
+    const Tensor ok = r.size() > 1 ? r[1] : Tensor();
+    return tuple_of({&r[0], &ok});
+  } catch (const Failed& f) {
+    return PyLong_FromLong(f.code);
+  }
+}
 
 // qknorm_grad(q, k, q_weight, k_weight, positions, table, tables, eps, rope, theta, max_positions) -> (Qr, Kr)
 PyObject* qknorm_grad(Args a) {
@@ -888,14 +1063,58 @@ PyObject* qknorm_grad(Args a) {
   if (!k && kw) throw NotPlain{};
   const Qk x(q, k);
   const Placed at_(pos, late, n.rope, n.theta, x.D, x.S, {x.B, x.S}, most, x.dev);
-  const Tensor& table = at_.table.own;
-  const bool grads = (qw && qw->requires_grad()) || (kw && kw->requires_grad());
-  const int64_t has = (k ? HAS_K : 0) | (qw ? HAS_QW : 0) | (kw ? HAS_KW : 0) | (at_.positions ? HAS_POSITIONS : 0) |
-                      (table.defined() ? HAS_TABLE : 0) | (grads ? WEIGHT_GRADS : 0);
+  return norm_apply(q, k, qw, kw, at_.positions ? pos : nullptr, at_.table, n);
+}
+
+// The rotation at positions of several axes without a norm: the backward needs the
+// positions and the table alone.
+struct TurnFunction : torch::autograd::Function<TurnFunction> {
+  static variable_list forward(AutogradContext* ctx, const Tensor& q, const Tensor& k, const Tensor& positions,
+                               const Tensor& table, int64_t rows, const Norm& n, bool has_k) {
+    const Qk x(q, has_k ? &k : nullptr);
+    const Tensor oq = out_or(nullptr, x.q.sizes(), x.type, x.dev);
+    Tensor ok;
+    if (x.k) ok = out_or(nullptr, x.k->sizes(), x.type, x.dev);
+    const int rc = norm_fwd(x, Weights(nullptr, nullptr, x.D, x.type, x.dev), n, table_in(table, rows),
+                            static_cast<const int*>(positions.const_data_ptr()), oq, ok);
+    if (rc) throw Failed{rc};
+    ctx->save_for_backward({positions, table});
+    std::vector<double> v{(double)n.rope, n.theta, (double)rows};
+    keep_axes(v, n);
+    ctx->saved_data["variant"] = v;
+    if (x.k) return {oq, ok};
+    return {oq};
+  }
+
+  static variable_list backward(AutogradContext* ctx, variable_list grad) {
+    const variable_list s = ctx->get_saved_variables();
+    Tensor dq, dk;
+    in_backward("attnfuse_qknorm_axes_bwd", [&] {
+      const std::vector<double> v = ctx->saved_data["variant"].toDoubleVector();
+      Norm n(0.f, (int)v[0], v[1]);
+      with_axes(n, &v[3]);
+      const Tensor dqr = grad[0].contiguous(), dkr = grad.size() > 1 ? grad[1].contiguous() : Tensor();
+      return unturn(dqr, grad.size() > 1 ? &dkr : nullptr, dq, dk, n, table_in(s[1], (int64_t)v[2]),
+                    static_cast<const int*>(s[0].const_data_ptr()));
+    });
+    return once({dq, dk, Tensor(), Tensor(), Tensor(), Tensor(), Tensor()}, {}, grad);
+  }
+};
+
+// axes_grad(q, k, q_weight, k_weight, positions, table, eps, rope, theta, max_positions, norm, sections, section_order)
+//     -> (Qr, Kr)
+PyObject* axes_grad(Args a) {
+  const Tensor &q = a.need(), *k = a.tensor();
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), &pos = a.need(), &tab = a.need();
+  Norm n(a);
+  const long long most = a.positive();
+  n.take_axes(a);
+  if ((!k && kw) || (!n.norm && (qw || kw))) throw NotPlain{};
+  const Qk x(q, k);
+  const AxesPlaced at_(pos, tab, x.D, {n.n, x.B, x.S}, most, x.dev);
+  if (n.norm) return norm_apply(q, k, qw, kw, &pos, at_.table, n);
   try {
-    const variable_list r =
-        NormFunction::apply(q, k ? *k : q, qw ? *qw : q, kw ? *kw : q, at_.positions ? *pos : q, table.defined() ? table : q,
-                            (int64_t)at_.table.rows, (double)n.eps, (int64_t)n.rope, n.theta, has);
+    const variable_list r = TurnFunction::apply(q, k ? *k : q, pos, tab, (int64_t)at_.table.rows, n, k != nullptr);
     const Tensor ok = r.size() > 1 ? r[1] : Tensor();
     return tuple_of({&r[0], &ok});
   } catch (const Failed& f) {
@@ -966,7 +1185,9 @@ constexpr PyMethodDef method(const char* name) {
 }
 
 PyMethodDef methods[] = {method<fwd>("fwd"), method<bwd>("bwd"), method<decode>("decode"), method<rope>("rope"),
-                         method<qknorm>("qknorm"), method<qknorm_bwd>("qknorm_bwd"), method<qknorm_grad>("qknorm_grad"), method<append>("append"),
+                         method<qknorm>("qknorm"), method<qknorm_bwd>("qknorm_bwd"), method<qknorm_grad>("qknorm_grad"), 
+                         method<append<false>>("append"), method<axes>("axes"), method<axes_bwd>("axes_bwd"),
+                         method<axes_grad>("axes_grad"), method<append<true>>("axes_append"),
                          method<decode_paged>("decode_paged"), method<decode_sinks>("decode_sinks"),
                          method<fwd_sinks>("fwd_sinks"), method<bwd_sinks>("bwd_sinks"), method<sinks_grad>("sinks_grad"),
                          {nullptr, nullptr, 0, nullptr}};
