@@ -286,6 +286,64 @@ int attnfuse_decode_paged(const void* Q, const void* K_pages, const void* V_page
                           int mask, int window, int sinks,
                           const float* alibi_slopes, float softmax_scale, void* stream);
 
+/* Bytes of device workspace of attnfuse_fwd_paged: partials (max, sum, accumulator)
+ * of every (token, query head), 0 where there are none.  own_keys is max_pages *
+ * page_size, prefix_keys prefix_pages * page_size (0: no prefix).  With one token of
+ * each sequence T is B.  Returns 0 for invalid sizes too. */
+size_t attnfuse_fwd_paged_workspace_bytes(int T, int B, int H, int H_kv, int D, int own_keys, int prefix_keys);
+
+/*
+ * Attention of new tokens over a paged cache, behind a prefix that the whole
+ * batch shares and that is read once for all of it: prompts in chunks, questions
+ * about one text, or one new token of each sequence.
+ *
+ * Sequence b has the queries of tokens q_starts[b] .. q_starts[b+1] - 1, which are
+ * the last n_b of its L_b = cache_lens[b] own keys (written before, as for
+ * attnfuse_decode_paged).  Its query t sees every key of the prefix and its own
+ * keys 0 .. L_b - n_b + t; where that is none (no prefix, and more queries than own
+ * keys), O = 0 and LSE = -inf.
+ *
+ *   Q [T,H,D]                     queries (bf16), already rotated
+ *                                 (attnfuse_qknorm_rope_append): where the prefix
+ *                                 ends, and positions of several axes, are the
+ *                                 caller's
+ *   K_pages, V_pages, strides, page_size   as attnfuse_decode_paged
+ *   block_table                   device int32 [B, max_pages]: the pages of each
+ *                                 sequence's own keys; as there
+ *   q_starts                      device int32 [B + 1], not decreasing, within
+ *                                 0 .. T (values outside are clamped), or NULL:
+ *                                 one token of each sequence (T == B).  Rows of O
+ *                                 and LSE of tokens before q_starts[0] and from
+ *                                 q_starts[B] on are left as they are.
+ *   cache_lens                    device int32 [B] or NULL (max_pages * page_size
+ *                                 each); larger values are clamped to that
+ *   prefix_table                  device int32 [prefix_pages]: the pages of the
+ *                                 prefix, in order; an entry outside [0,
+ *                                 num_pages) holds no keys.  prefix_pages 0, and
+ *                                 NULL: no prefix
+ *   prefix_len                    device int32 [1]: keys of the prefix, clamped to
+ *                                 prefix_pages * page_size; NULL: all of them
+ *   O [T,H,D] (bf16), LSE [T,H] fp32
+ *   workspace                     >= attnfuse_fwd_paged_workspace_bytes bytes,
+ *                                 16-byte aligned; may be NULL where that is 0
+ *   D in {64, 128}; B < 2^16, T <= 2^20, T * H <= 2^30; prefix_pages * page_size and
+ *   max_pages * page_size <= 2^20; H <= 16384, a multiple of H_kv
+ *
+ * A NaN in a query, or in a key or value that it sees, comes out as NaN.  A NaN or an
+ * infinity in the value of a later own key of the same sequence reaches queries that do
+ * not see it yet, where both lie in a 64-key tile that some query in between sees (its
+ * weight is 0); what lies in pages past a sequence's length, and in places that are no
+ * key, is never used.  Keys are shared out among workgroups by sizes alone (T, B and the
+ * tables' widths): with others a result is the same to the rounding of fp32 sums.
+ */
+int attnfuse_fwd_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table, const int* q_starts,
+                       const int* cache_lens, const int* prefix_table, const int* prefix_len, void* O, float* LSE,
+                       void* workspace, size_t workspace_bytes,
+                       long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                       long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                       int T, int B, int H, int H_kv, int D, int num_pages, int page_size, int max_pages, int prefix_pages,
+                       float softmax_scale, void* stream);
+
 /*
  * attnfuse_decode (a contiguous cache [B,H_kv,S_kv,D]) with sinks: the last
  * `window` keys and the first `sinks` keys of each sequence are visible.

@@ -59,6 +59,8 @@ LLM_SIGNATURES = {
     "attnfuse_decode_paged_workspace_bytes": (ctypes.c_size_t, [_I] * 7),
     "attnfuse_decode_paged": (_I, [_P] * 8 + [ctypes.c_size_t] + [_L] * 6 + [_I] * 8 + [_F, _P, _I, _I, _I, _I, _P, _F,
                                                                                        _P]),
+    "attnfuse_fwd_paged_workspace_bytes": (ctypes.c_size_t, [_I] * 7),
+    "attnfuse_fwd_paged": (_I, [_P] * 11 + [ctypes.c_size_t] + [_L] * 6 + [_I] * 9 + [_F, _P]),
     "attnfuse_decode_sinks": (_I, [_P] * 7 + [ctypes.c_size_t] + [_I] * 6 + [_F, _P, _I, _I, _I, _F, _P]),
 }
 

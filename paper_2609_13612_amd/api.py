@@ -995,11 +995,21 @@ def _decode_sinks(q, k_cache, v_cache, cache_lens, rope, theta, mask, window, al
 
 def attnfuse_decode_paged(q, k_cache, v_cache, block_table, cache_lens=None, *, rope="none", theta=10000.0, mask="causal",
                           window=None, sinks=0, alibi_slopes=None, scale=None, out=None, lse=None, workspace=None,
-                          rope_table=None):
+                          rope_table=None, prefix_table=None, prefix_len=None):
     """O [B,H,D], LSE [B,H] of one query per sequence against pages [num_pages, H_kv, page_size, D] of already-rotated
     keys and their values, key n of sequence b in page ``block_table[b, n // page_size]`` (int32 [B, max_pages]); see
     attnfuse_decode_paged in include/attnfuse_llm.h.  The pages may lie apart (pages [num_pages, page_size, H_kv, D]
-    transposed)."""
+    transposed).
+
+    With ``prefix_table`` (int32 [prefix_pages]) every sequence sees, before its own keys, those of a prefix that the
+    batch shares and that is read once for all of it: ``prefix_len`` keys (int32 [1] on the GPU; None: all) in those pages.
+    The queries come rotated then (rope="none"), and there are no windows and no ALiBi; see attnfuse_fwd_paged."""
+    if prefix_table is not None or prefix_len is not None:
+        if rope != "none" or mask not in ("none", "causal") or window or sinks or alibi_slopes is not None or rope_table is not None:
+            raise ValueError("a shared prefix goes with rotated queries (rope='none'), without windows, sinks and ALiBi")
+        if prefix_table is None:
+            raise ValueError("prefix_len needs prefix_table")
+        return _fwd_paged(q, k_cache, v_cache, block_table, None, cache_lens, prefix_table, prefix_len, scale, out, lse, workspace)
     if sinks:
         window, sinks = _need_sinks(sinks, mask, window, alibi_slopes)
     if _native is not None:
@@ -1034,6 +1044,70 @@ def attnfuse_decode_paged(q, k_cache, v_cache, block_table, cache_lens=None, *, 
             _ptr(workspace), wbytes, *kps, *vps, B, H, Hkv, D, pages, page, block_table.shape[1], r, th, tp, tr, m, w, sinks,
             _ptr(alibi_slopes), sc, _stream())
     _check(code, "attnfuse_decode_paged")
+    return out, lse
+
+
+def attnfuse_fwd_paged_workspace_bytes(T, B, H, H_kv, D, own_keys, prefix_keys=0):
+    return _lib.load().attnfuse_fwd_paged_workspace_bytes(T, B, H, H_kv, D, own_keys, prefix_keys)
+
+
+def attnfuse_fwd_paged(q, k_cache, v_cache, block_table, q_starts, cache_lens=None, *, prefix_table=None, prefix_len=None,
+                       scale=None, out=None, lse=None, workspace=None):
+    """O [T,H,D], LSE [T,H] of several new tokens per sequence, queries q [T,H,D] already rotated, against pages as
+    attnfuse_decode_paged takes them: tokens ``q_starts[b]`` .. ``q_starts[b + 1] - 1`` (int32 [B + 1]) are the last ones
+    of sequence b's ``cache_lens[b]`` own keys and see those up to their own, after the prefix that the batch shares
+    (``prefix_table`` int32 [prefix_pages], ``prefix_len`` int32 [1]), if any.  Rows of ``out`` and ``lse`` of tokens that no
+    sequence has are left as they are.  See attnfuse_fwd_paged in include/attnfuse_llm.h."""
+    if q_starts is None:
+        raise ValueError("q_starts must be an int32 tensor [B + 1]")
+    return _fwd_paged(q, k_cache, v_cache, block_table, q_starts, cache_lens, prefix_table, prefix_len, scale, out, lse, workspace)
+
+
+def _fwd_paged(q, k_cache, v_cache, block_table, q_starts, cache_lens, prefix_table, prefix_len, scale, out, lse, workspace):
+    if _native is not None:
+        r = _native.fwd_paged(q, k_cache, v_cache, block_table, q_starts, cache_lens, prefix_table, prefix_len, out, lse,
+                              workspace, scale)
+        if r is not None:
+            return _result(r, "attnfuse_fwd_paged")
+    dev = _device(q)
+    if q.dim() != 3 or q.dtype != torch.bfloat16:
+        raise ValueError("q must be a bf16 tensor [T, H, D]")
+    if not isinstance(k_cache, torch.Tensor) or k_cache.dim() != 4:
+        raise ValueError("the caches must be [num_pages, H_kv, page_size, D]")
+    T, H, D = q.shape
+    Hkv = k_cache.shape[1]
+    _need(q, "q", (T, H, D), q.dtype, dev)
+    pages, page, (kps, vps) = _pages(k_cache, v_cache, Hkv, D, q.dtype, dev)
+    if not isinstance(block_table, torch.Tensor) or block_table.dim() != 2:
+        raise ValueError("block_table must be an int32 tensor [B, max_pages]")
+    B, most = block_table.shape
+    _need(block_table, "block_table", (B, most), torch.int32, dev)
+    if q_starts is not None:
+        _need(q_starts, "q_starts", (B + 1,), torch.int32, dev)
+    elif B != T:
+        raise ValueError(f"block_table must have {T} rows, one for each query (it has {B})")
+    if cache_lens is not None:
+        _need(cache_lens, "cache_lens", (B,), torch.int32, dev)
+    ahead = 0
+    if prefix_table is not None:
+        if not isinstance(prefix_table, torch.Tensor) or prefix_table.dim() != 1 or prefix_table.shape[0] < 1:
+            raise ValueError("prefix_table must be an int32 tensor [prefix_pages]")
+        ahead = prefix_table.shape[0]
+        _need(prefix_table, "prefix_table", (ahead,), torch.int32, dev)
+        if prefix_len is not None:
+            _need(prefix_len, "prefix_len", (1,), torch.int32, dev)
+    elif prefix_len is not None:
+        raise ValueError("prefix_len needs prefix_table")
+    out = _opt(out, "out", (T, H, D), q.dtype, dev)
+    lse = _opt(lse, "lse", (T, H), torch.float32, dev)
+    scale = 1.0 / math.sqrt(D) if scale is None else scale
+    workspace, wbytes = _workspace(workspace, attnfuse_fwd_paged_workspace_bytes(T, B, H, Hkv, D, most * page, ahead * page), dev)
+    with torch.cuda.device(dev):
+        code = _lib.load().attnfuse_fwd_paged(
+            _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(block_table), _ptr(q_starts), _ptr(cache_lens), _ptr(prefix_table),
+            _ptr(prefix_len), _ptr(out), _ptr(lse), _ptr(workspace) if wbytes else None, wbytes, *kps, *vps, T, B, H, Hkv, D,
+            pages, page, most, ahead, scale, _stream())
+    _check(code, "attnfuse_fwd_paged")
     return out, lse
 
 

@@ -32,7 +32,8 @@ COMMON = ["-O3", "-std=c++17", "-fPIC", f"--offload-arch={ARCH}", f"-I{INCLUDE}"
 
 SOURCES = ["api.cpp", "rope.hip", "fwd_bf16.hip", "fwd_prerot.hip", "fwd_norope.hip", "fwd_fp32.hip", "bwd_bf16.hip",
            "bwd_dkdv.hip", "bwd_dkdv_split.hip", "bwd_fp32.hip", "decode.hip", "api_llm.cpp", "qknorm.hip", "qknorm_axes.hip",
-           "decode_paged.hip", "fwd_sinks.hip", "bwd_sinks.hip", "bwd_dkdv_sinks.hip"]
+           "decode_paged.hip", "paged_tiles.hip",
+           "fwd_sinks.hip", "bwd_sinks.hip", "bwd_dkdv_sinks.hip"]
 # Code-generation options of single translation units.  The dK/dV kernels
 # run faster when the machine scheduler keeps its first schedule instead of
 # re-scheduling high-register-pressure regions without memory-op clustering

@@ -427,6 +427,45 @@ int qknorm_append(const void* Q, const void* K, const void* V, void* Qr, void* K
       af::launch_qknorm(af::QKNORM_APPEND, dtype == AF_DTYPE_FP32, D, rope, p, static_cast<hipStream_t>(stream)));
 }
 
+// ---------------------------------------------------------------- new tokens over pages
+struct TilesLayout {
+  int nw, nsp, nso, prefix_items, own_items;
+  bool joined;
+  size_t ml, acc, total;
+};
+
+// T queries of B sequences (one_each: one of each) against up to S own keys and P of the
+// prefix: see paged_tiles.hip for what is apart and joined.
+TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, int P, int D) {
+  TilesLayout L{};
+  const long long G = H / H_kv, rows = T * G;
+  L.joined = P > 0 && rows >= 256LL * B;
+  L.nw = 4;
+  const long long R = 32 * L.nw;
+  const long long lists = one_each ? B * ((G + R - 1) / R) : rows / R + B;   // tiles of rows of the sequences
+  const long long flat = (rows + R - 1) / R;                                 // and of all tokens
+  auto shares = [&](long long units, long long keys) {
+    long long n = units < 512 ? 512 / units : 1;
+    const long long most = (keys + 63) / 64 / 4;   // four tiles at least
+    if (n > most) n = most;
+    return (int)(n < 1 ? 1 : n);
+  };
+  L.nsp = P > 0 && !L.joined ? shares(flat * H_kv, P) : 0;
+  L.nso = shares(lists * H_kv, (long long)S + (L.joined ? P : 0));
+  L.prefix_items = (int)(L.nsp * flat);
+  L.own_items = (int)(L.nso * lists);
+  const size_t parts = L.nsp + L.nso, all = parts > 1 ? parts * (size_t)T * H : 0;
+  L.acc = align256(all * 2 * sizeof(float));
+  L.total = L.acc + align256(all * D * sizeof(float));
+  return L;
+}
+
+bool tiles_sizes(int T, int B, int H, int H_kv, long long S, long long P, int D) {
+  return T >= 1 && T <= kMaxS && B >= 1 && B < (1 << 16) && H >= 1 && H <= kMaxHeads && H_kv >= 1 && H % H_kv == 0 && S >= 1 &&
+         S <= kMaxS && P >= 0 && P <= kMaxS && D >= 2 && D % 2 == 0 && (long long)T * H <= (1 << 30) &&
+         ((long long)T * (H / H_kv) / 128 + B) * H_kv * 1024 < (1LL << 31);
+}
+
 }  // namespace
 
 extern "C" {
@@ -588,6 +627,64 @@ int attnfuse_decode_paged(const void* Q, const void* K_pages, const void* V_page
   return decode_impl(p, Q, K_pages, V_pages, cache_lens, O, LSE, workspace, workspace_bytes, B, H, H_kv,
                      max_pages * page_size, D, rope, rope_theta, rope_table, rope_table_rows, mask, window, sinks,
                      alibi_slopes, softmax_scale, stream);
+}
+
+size_t attnfuse_fwd_paged_workspace_bytes(int T, int B, int H, int H_kv, int D, int own_keys, int prefix_keys) {
+  if (!tiles_sizes(T, B, H, H_kv, own_keys, prefix_keys, D)) return 0;
+  const size_t one = T == B ? tiles_layout(T, B, true, H, H_kv, own_keys, prefix_keys, D).total : 0;
+  const size_t any = tiles_layout(T, B, false, H, H_kv, own_keys, prefix_keys, D).total;
+  return one > any ? one : any;
+}
+
+int attnfuse_fwd_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table, const int* q_starts,
+                       const int* cache_lens, const int* prefix_table, const int* prefix_len, void* O, float* LSE,
+                       void* workspace, size_t workspace_bytes,
+                       long long kp_stride_p, long long kp_stride_h, long long kp_stride_s,
+                       long long vp_stride_p, long long vp_stride_h, long long vp_stride_s,
+                       int T, int B, int H, int H_kv, int D, int num_pages, int page_size, int max_pages, int prefix_pages,
+                       float softmax_scale, void* stream) {
+  if (!Q || !K_pages || !V_pages || !block_table || !O || !LSE) return AF_ERR_INVALID_ARG;
+  if (num_pages < 1 || page_size < 1 || max_pages < 1 || prefix_pages < 0) return AF_ERR_INVALID_ARG;
+  if (prefix_pages > 0 ? !prefix_table : prefix_table || prefix_len) return AF_ERR_INVALID_ARG;
+  if (!q_starts && T != B) return AF_ERR_INVALID_ARG;
+  for (const void* x : {Q, K_pages, V_pages, (const void*)O, (const void*)workspace})
+    if (!aligned16(x)) return AF_ERR_INVALID_ARG;
+  for (const void* x : {(const void*)LSE, (const void*)block_table, (const void*)q_starts, (const void*)cache_lens,
+                        (const void*)prefix_table, (const void*)prefix_len})
+    if (!aligned4(x)) return AF_ERR_INVALID_ARG;
+  if (any_alias({O, LSE, workspace}, {Q, K_pages, V_pages, block_table, q_starts, cache_lens, prefix_table, prefix_len}) ||
+      outs_alias({O, LSE, workspace}))
+    return AF_ERR_INVALID_ARG;
+  const long long S = (long long)max_pages * page_size, P = (long long)prefix_pages * page_size;
+  if (!tiles_sizes(T, B, H, H_kv, S, P, D)) return AF_ERR_INVALID_ARG;
+  if (!strides_ok({{num_pages, kp_stride_p}, {H_kv, kp_stride_h}, {page_size, kp_stride_s}}, 0, AF_DTYPE_BF16, false) ||
+      !strides_ok({{num_pages, vp_stride_p}, {H_kv, vp_stride_h}, {page_size, vp_stride_s}}, 0, AF_DTYPE_BF16, false) ||
+      kp_stride_s > (1 << 24) || vp_stride_s > (1 << 24))
+    return AF_ERR_INVALID_ARG;
+  if (!(std::isfinite(softmax_scale) && softmax_scale > 0.f)) return AF_ERR_INVALID_ARG;
+  const TilesLayout L = tiles_layout(T, B, !q_starts, H, H_kv, (int)S, (int)P, D);
+  if (L.total > 0 && (!workspace || workspace_bytes < L.total)) return AF_ERR_INVALID_ARG;
+  const int shift = page_shift_of(page_size);
+  if (shift < 0 || !supported_d(D)) return AF_ERR_UNSUPPORTED;
+
+  af::TilesParams p{};
+  p.q = Q; p.k = K_pages; p.v = V_pages;
+  p.ks[0] = kp_stride_p; p.ks[1] = kp_stride_h; p.ks[2] = kp_stride_s;
+  p.vs[0] = vp_stride_p; p.vs[1] = vp_stride_h; p.vs[2] = vp_stride_s;
+  p.table = block_table;
+  p.max_pages = max_pages; p.num_pages = num_pages; p.page_shift = shift;
+  p.lens = cache_lens; p.starts = q_starts;
+  p.prefix_table = prefix_table; p.prefix_len = prefix_len; p.prefix_pages = prefix_pages;
+  p.o = O; p.lse = LSE;
+  p.part_ml = static_cast<float*>(workspace);
+  p.part_acc = reinterpret_cast<float*>(static_cast<char*>(workspace) + L.acc);
+  p.T = T; p.B = B; p.H = H; p.Hkv = H_kv; p.G = H / H_kv;
+  p.S = (int)S; p.P = (int)P;
+  p.joined = L.joined;
+  p.nsp = L.nsp; p.nso = L.nso; p.parts = L.nsp + L.nso;
+  p.prefix_items = L.prefix_items; p.own_items = L.own_items;
+  p.scale = softmax_scale;
+  return map_launch(af::launch_paged_tiles(D, p, L.nw, static_cast<hipStream_t>(stream)));
 }
 
 int attnfuse_decode_sinks(const void* Q, const void* K, const void* V, const int* cache_lens, void* O, float* LSE,

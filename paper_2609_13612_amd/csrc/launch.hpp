@@ -148,6 +148,33 @@ struct PagedParams {
   const float2* rope;     // [rows >= S][D/2] (cos, sin)
 };
 
+// Attention over pages of several new tokens a sequence, behind a prefix that the batch
+// shares (paged_tiles.hip).
+struct TilesParams {
+  const void* q;          // [T, H, D]
+  const void* k;          // pages
+  const void* v;
+  long long ks[3], vs[3]; // their strides in elements: page, head, place
+  const int* table;       // [B, max_pages] page numbers
+  int max_pages, num_pages, page_shift;
+  const int* lens;        // device [B] own keys, or nullptr (all S)
+  const int* starts;      // device [B + 1]: the first token of each sequence; nullptr: one token each
+  const int* prefix_table;  // [prefix_pages]
+  const int* prefix_len;  // device [1] keys of the prefix, or nullptr (all P)
+  int prefix_pages;       // 0: no prefix
+  void* o;                // [T, H, D]
+  float* lse;             // [T, H]
+  float* part_ml;         // workspace [parts, T, H, 2]: partial max and sum (log2 units)
+  float* part_acc;        // workspace [parts, T, H, D]
+  int T, B, H, Hkv, G;
+  int S, P;               // the most own keys of a sequence, and of the prefix
+  bool joined;            // a sequence's rows walk the prefix's tiles too (no list of all tokens' rows)
+  int nsp, nso;           // shares of the prefix's tiles (0: joined, or no prefix), of a sequence's
+  int parts;              // nsp + nso; 1: results are written at once
+  int prefix_items, own_items;   // workgroups per K/V head over the prefix, over the sequences' lists
+  float scale;
+};
+
 // Waves per workgroup, four or eight, of a dense bf16 forward that has both
 // forms; rope: the rotation of its key tiles in the loop (ROPE_NONE where they
 // are copied to LDS as they are); bias: 0 without one, 1 where one row serves
@@ -177,6 +204,7 @@ int launch_rope(bool fp32, int D, int rope, bool inverse, const RopeParams& p, h
 // x0 (bf16) rotated into y0 (fp16); x1 unused.
 int launch_rope_f16(int D, int rope, const RopeParams& p, hipStream_t st);
 int launch_decode_paged(int D, int rope, bool alibi, const PagedParams& p, hipStream_t st);
+int launch_paged_tiles(int D, const TilesParams& p, int nw, hipStream_t st);   // nw: waves to a workgroup, 4 or 8
 int launch_qknorm(int what, bool fp32, int D, int rope, const QkNormParams& p, hipStream_t st);
 int launch_qknorm_axes(int what, bool fp32, int D, int rope, const QkNormParams& p, hipStream_t st);   // p.axes > 0
 

@@ -1,0 +1,457 @@
+// Attention of new tokens over paged keys and values, several tokens a sequence or
+// one, behind a prefix that the whole batch shares; bf16, fp32 accumulation.
+//
+// Sequence b has n_b queries, the last n_b of its L_b own keys; query t of them sees
+// the P keys of the prefix and its own keys 0 .. L_b - n_b + t:
+//   s_j = scale q . k_j,  O = sum_j softmax(s)_j v_j,  LSE = log sum_j exp(s_j).
+//
+// A row is one (token, query head) of a K/V head's group of G: row r of a list of tokens
+// is head r % G of token r / G.  Workgroup = NW waves = 32 NW rows against every ns-th
+// 64-key tile of a list of key tiles.  What makes rows meet the prefix once:
+//   * apart: the rows of all tokens of the batch are one list for the prefix's tiles, so
+//     a workgroup's tile of K and V serves 32 NW rows of any sequences; the rows of a
+//     sequence are a list for its own tiles.  Both kinds of workgroup run in one launch and leave
+//     partials (max, sum, O), which a second kernel joins;
+//   * joined: where sequences have tokens enough to fill tiles of rows by themselves, the
+//     rows of a sequence walk the prefix's tiles and then their own: fewer partials, none
+//     with one share.
+// The tiles of a list are dealt out in turn to ns shares, so shares are even whatever the
+// lengths, which are known on the device alone.
+//
+// Inside a workgroup the tiles go straight from the pages to LDS (attn_tiles.hpp), one
+// 16-key unit of a page at a time, whose address is wave-uniform; the page numbers are scalar
+// loads one tile ahead.  The loop is the forward's: while the products S^T = K Q^T of the
+// next tile run, this tile's scores become probabilities, and its P V runs while the next tile's
+// scores are masked and reduced.  Q and K meet in bf16 exactly; P is rounded to bf16
+// (2^-9 of each weight; the bf16 O is rounded as much), sums, maxima and O stay fp32.
+//
+// What lies in places that are no key of any row of the workgroup may be anything: scores
+// are replaced and rows of V cleared in LDS after they landed.
+#include "attn_tiles.hpp"
+#include "launch.hpp"
+
+namespace af {
+
+// A value that no kernel writes while this one runs, at a wave-uniform address.
+__device__ __forceinline__ int scalar_load(const int* p) {
+  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
+}
+
+// A pointer that is the same in every lane, in scalar registers.
+__device__ __forceinline__ const uint16_t* uniform(const uint16_t* p) {
+  const uint64_t x = (uint64_t)p;
+  return (const uint16_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
+                           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
+}
+
+// The queries of a sequence: tokens [first, first + n), and its own keys.
+struct Sequence {
+  int b, first, n, keys;
+};
+
+__device__ __forceinline__ Sequence sequence_at(const TilesParams& p, int b) {
+  Sequence s{b, b, 1, 0};
+  if (p.starts) {
+    s.first = min(max(scalar_load(p.starts + b), 0), p.T);
+    s.n = min(max(scalar_load(p.starts + b + 1), s.first), p.T) - s.first;
+  }
+  s.keys = p.lens ? min(max(scalar_load(p.lens + b), 0), p.S) : p.S;
+  return s;
+}
+
+// The sequence of a slot (a tile of rows) and the tile's first row.  Sequence b has the
+// slots from first_b G / rows + b on, which leaves it room for a tile that is not full; its
+// number is that of the sequences that start at or before the slot.  -1: no sequence's.
+__device__ __forceinline__ int sequence_of(const TilesParams& p, int slot, int rows, int lane, int& r0) {
+  if (!p.starts) {
+    const int per = (p.G + rows - 1) / rows;
+    r0 = slot % per * rows;
+    return slot / per;
+  }
+  int count = 0, mine = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int b = b0 + lane;
+    const int at = b < p.B ? (int)((long long)min(max(p.starts[b], 0), p.T) * p.G / rows) + b : 0x7fffffff;
+    const unsigned long long before = __ballot(at <= slot);
+    if (before) mine = __builtin_amdgcn_readlane(at, 63 - __clzll(before));
+    count += __popcll(before);
+  }
+  r0 = (slot - mine) * rows;
+  return count - 1;
+}
+
+template <int D, int NW>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
+void paged_tiles_kernel(TilesParams p) {
+  using AT = AsyncTile<D, NW>;
+  constexpr int BN = 64, KS = D / 16, MT = D / 32, ROWS = 32 * NW, RPG = AT::RPG;
+  __shared__ __attribute__((aligned(16))) uint16_t smem[4 * AT::ELEMS];
+
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int lq = lane & 31, lg = lane >> 5;
+
+  // ---- what this workgroup does: rows [r0, r0 + ROWS) of a list of nrows, from token
+  // `first` on; tiles share, share + ns, ... of the prefix's (np keys) and then the
+  // sequence's; part: where its partial goes.
+  const int g = blockIdx.x % p.Hkv;
+  int i = blockIdx.x / p.Hkv, r0, nrows, first, np = 0, share, ns, part, shift_keys = 0;
+  const int* table = p.table;
+  const bool prefix_list = i < p.prefix_items;             // (apart: a list of all tokens' rows)
+  if (p.prefix_pages > 0 && (prefix_list || p.joined))
+    np = p.prefix_len ? min(max(scalar_load(p.prefix_len), 0), p.P) : p.P;
+  int own = 0;                                             // own keys that any row of the workgroup sees
+  if (prefix_list) {
+    ns = p.nsp;
+    share = i % ns;
+    r0 = i / ns * ROWS;
+    nrows = p.T * p.G;
+    first = 0;
+    part = share;
+  } else {
+    i -= p.prefix_items;
+    ns = p.nso;
+    share = i % ns;
+    const int b = __builtin_amdgcn_readfirstlane(sequence_of(p, i / ns, ROWS, lane, r0));
+    r0 = __builtin_amdgcn_readfirstlane(r0);
+    if (b < 0) return;
+    const Sequence s = sequence_at(p, b);
+    nrows = s.n * p.G;
+    if (r0 >= nrows) return;
+    first = s.first;
+    table += (size_t)b * p.max_pages;
+    shift_keys = s.keys - s.n;                             // token t sees its keys up to shift_keys + t
+    own = max(0, shift_keys + (min(r0 + ROWS, nrows) - 1) / p.G + 1);
+    part = p.nsp + share;
+  }
+  const int tp = (np + BN - 1) / BN, all = tp + (own + BN - 1) / BN;
+  const int nt = all > share ? (all - share + ns - 1) / ns : 0;
+  const bool direct = p.parts == 1;
+  const int G = p.G;
+  const int row = r0 + 32 * wave + lq, rowc = min(row, nrows - 1);
+  const int token = rowc / G;                              // of the list
+  const size_t at_row = (size_t)(first + token) * p.H + g * G + (rowc - token * G);   // of Q, O and LSE
+
+  if (nt == 0) {                                           // no key: nothing to join, or an empty row
+    for (int j = tid; j < ROWS && r0 + j < nrows; j += 64 * NW) {
+      const int t = (r0 + j) / G;
+      const size_t at = (size_t)(first + t) * p.H + g * G + (r0 + j - t * G);
+      if (direct) {
+        for (int d = 0; d < D; d += 8) st16(static_cast<uint16_t*>(p.o) + at * D + d, u32x4{0, 0, 0, 0});
+        p.lse[at] = -INFINITY;
+      } else {
+        *reinterpret_cast<float2*>(p.part_ml + 2 * ((size_t)part * p.T * p.H + at)) = float2{-INFINITY, 0.f};
+      }
+    }
+    return;
+  }
+
+  const bool live = r0 + 32 * wave < nrows;                // (a wave without rows only copies)
+  const int lim = shift_keys + token;                      // the last own key that this lane's row sees
+  const int lim_wave = shift_keys + min(r0 + 32 * wave, nrows - 1) / G;   // the least of the wave's
+
+  // ---- tiles
+  const uint16_t* __restrict__ K = static_cast<const uint16_t*>(p.k) + g * p.ks[1];
+  const uint16_t* __restrict__ V = static_cast<const uint16_t*>(p.v) + g * p.vs[1];
+  struct Tile {
+    int n0, end;          // its first key in the prefix or in the sequence, and where those end
+    bool prefix;
+    int pg[4];            // pages of its units, -1: none there
+  };
+  auto tile_at = [&](int i) {
+    Tile t;
+    const int idx = share + i * ns;
+    t.prefix = idx < tp;
+    t.n0 = BN * (t.prefix ? idx : idx - tp);
+    t.end = t.prefix ? np : own;
+    const int* pages = t.prefix ? p.prefix_table : table;
+    const int last = (t.prefix ? p.prefix_pages : p.max_pages) - 1;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const int e = scalar_load(pages + min((t.n0 + 16 * u) >> p.page_shift, last));
+      t.pg[u] = (unsigned)e < (unsigned)p.num_pages ? e : -1;
+    }
+    return t;
+  };
+  auto whole = [&](const Tile& t) { return t.n0 + BN <= t.end && (t.pg[0] | t.pg[1] | t.pg[2] | t.pg[3]) >= 0; };
+
+  const AT at(lane, wave);
+  auto akst = [&](int par) { return smem + 2 * par * AT::ELEMS; };
+  auto avst = [&](int par) { return smem + (2 * par + 1) * AT::ELEMS; };
+  constexpr int CPR = D / 8;
+  const int unit0 = wave * RPG / 16, row_in_unit = wave * RPG % 16 + lane / CPR;   // of the wave's first group
+  auto unit_of = [&](int i) { return unit0 + NW * RPG / 16 * i; };
+  auto page_of = [&](const Tile& t, int i) {
+    int x = t.pg[0];
+#pragma unroll
+    for (int u = 1; u < 4; ++u) x = unit_of(i) == u ? t.pg[u] : x;
+    return x;
+  };
+  auto load = [&](const uint16_t* X, const long long (&st)[3], const Tile& t, uint16_t* dst) {
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)dst;
+    const uint32_t voff = (uint32_t)row_in_unit * (uint32_t)(2 * st[2]) + at.col;
+#pragma unroll
+    for (int i = 0; i < AT::NI; ++i) {
+      const int n = t.n0 + 16 * unit_of(i);
+      const uint16_t* base = X + (long long)max(page_of(t, i), 0) * st[0] + (long long)(n & ((1 << p.page_shift) - 1)) * st[2];
+      async_copy16(uniform(base), voff, __builtin_amdgcn_readfirstlane(lds + (wave + NW * i) * (AT::GROUP * 2)));
+    }
+  };
+  // Rows of V that are no key: 0 x NaN is NaN.  (Each lane clears what it copied.)
+  auto clear = [&](const Tile& t, uint16_t* dst) {
+    if (whole(t)) return;
+#pragma unroll
+    for (int i = 0; i < AT::NI; ++i) {
+      const int n = t.n0 + 16 * unit_of(i) + row_in_unit;
+      if (n >= t.end || page_of(t, i) < 0)
+        *reinterpret_cast<u32x4*>(dst + (wave + NW * i) * AT::GROUP + 8 * lane) = u32x4{0, 0, 0, 0};
+    }
+  };
+
+  Tile cur_t = tile_at(0), nxt_t = tile_at(min(1, nt - 1));
+  load(K, p.ks, cur_t, akst(0));
+  load(V, p.vs, cur_t, avst(0));
+  if (nt > 1) load(K, p.ks, nxt_t, akst(1));
+  Tile far_t = tile_at(min(2, nt - 1));
+
+  // Query operand (B of S^T = K Q^T): lane holds its row, dims 16 s + 8 lg .. +7.
+  u32x4 qreg[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qreg[s] = ld16(static_cast<const uint16_t*>(p.q) + at_row * D + 16 * s + 8 * lg);
+
+  f32x16 acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f, m_new = -INFINITY;   // log2 units
+  const float c2 = p.scale * kLog2e;
+
+  auto scores = [&](f32x16 (&sc)[2], const uint16_t* Ks) {
+    sc[0] = f32x16{};
+    sc[1] = f32x16{};
+#pragma unroll
+    for (int s = 0; s < KS; ++s)
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt) sc[kt] = mfma32(at.row(Ks, 32 * kt, s), qreg[s], sc[kt]);
+  };
+  auto pv = [&](const u32x4 (&pop)[2][2], const uint16_t* Vs) {
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int mt = 0; mt < MT; ++mt) acc[mt] = mfma32(at.tr(Vs, 32 * kt + 16 * hf, mt), pop[kt][hf], acc[mt]);
+  };
+  // Mask and maximum.  Element r of subtile kt is key n0 + 32 kt + 8 (r / 4) + r % 4 + 4 lg,
+  // of unit 2 kt + r / 8.
+  auto prepare = [&](f32x16 (&sc)[2], const Tile& t) {
+    if (!whole(t) || (!t.prefix && t.n0 + BN - 1 > lim_wave)) {   // (wave-uniform)
+      const int seen = (t.prefix ? t.end - 1 : lim) - t.n0 - 4 * lg;
+#pragma unroll
+      for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+          const bool ok = 32 * kt + 8 * (r >> 2) + (r & 3) <= seen && t.pg[2 * kt + (r >> 3)] >= 0;
+          sc[kt][r] = ok ? sc[kt][r] : -INFINITY;
+        }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt)
+#pragma unroll
+      for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[kt][r]);
+    m_new = fmaxf(m_run, pair_max(mx) * c2);
+  };
+  auto raise = [&]() {   // the reference maximum, where a row's grew by more than 2^8
+    if (__any(m_new > m_run + 8.f)) {
+      const float alpha = (m_run == -INFINITY) ? 0.f : fast_exp2(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[m] *= alpha;
+      m_run = m_new;
+    }
+  };
+  auto probs = [&](const f32x16 (&sc)[2], u32x4 (&pop)[2][2]) {
+    const float m_use = (m_run == -INFINITY) ? 0.f : m_run;
+    float rs = 0.f;
+#pragma unroll
+    for (int kt = 0; kt < 2; ++kt) {
+      float e[16];
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        e[r] = fast_exp2(__builtin_fmaf(sc[kt][r], c2, -m_use));
+        rs += e[r];
+      }
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+        for (int w = 0; w < 4; ++w) pop[kt][hf][w] = pack_bf16(e[8 * hf + 2 * w], e[8 * hf + 2 * w + 1]);
+    }
+    l_run += rs;
+  };
+  auto pin_values = [](u32x4 (&pp)[2][2], float& l) {   // (keeps the softmax work beside the next scores' products)
+    asm volatile("" : "+v"(pp[0][0]), "+v"(pp[0][1]), "+v"(pp[1][0]), "+v"(pp[1][1]), "+v"(l));
+  };
+
+  f32x16 sa[2], sb[2];
+  u32x4 pop[2][2];
+  async_wait();
+  clear(cur_t, avst(0));
+  __syncthreads();
+  if (live) {
+    scores(sa, akst(0));
+    prepare(sa, cur_t);
+    raise();
+  }
+  __syncthreads();
+  // Iteration t turns tile t's scores into its share of O while tile t + 1's scores are
+  // formed; it copies K of tile t + 2 and V of tile t + 1 into the stage halves that the
+  // last barrier freed (past the last tile: that one again, which nobody reads).
+  int t = 0;
+  auto iteration = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], auto parity) {
+    constexpr int PAR = decltype(parity)::value;   // t & 1
+    load(K, p.ks, far_t, akst(PAR));
+    load(V, p.vs, nxt_t, avst(1 - PAR));
+    if (live) {
+      probs(cur, pop);
+      scores(nxt, akst(1 - PAR));
+      pin_values(pop, l_run);
+      prepare(nxt, nxt_t);
+      pv(pop, avst(PAR));
+      raise();
+    }
+    const Tile after = tile_at(min(t + 3, nt - 1));
+    async_wait();
+    clear(nxt_t, avst(1 - PAR));
+    __syncthreads();
+    nxt_t = far_t;
+    far_t = after;
+    ++t;
+  };
+  using P0 = std::integral_constant<int, 0>;
+  using P1 = std::integral_constant<int, 1>;
+  while (t + 2 < nt) {
+    iteration(sa, sb, P0{});
+    iteration(sb, sa, P1{});
+  }
+  if (t + 1 < nt) {
+    iteration(sa, sb, P0{});
+    if (live) {
+      probs(sb, pop);
+      pv(pop, avst(1));
+    }
+  } else if (live) {
+    probs(sa, pop);
+    pv(pop, avst(0));
+  }
+
+  // ---- the result, or this share's partial
+  const float l_tot = pair_sum(l_run);
+  if (!direct) {
+    if (live && row < nrows) {
+      const size_t at = (size_t)part * p.T * p.H + at_row;
+      float* dst = p.part_acc + at * D + 4 * lg;
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+        for (int a = 0; a < 4; ++a)
+          *reinterpret_cast<float4*>(dst + 32 * mt + 8 * a) =
+              float4{acc[mt][4 * a], acc[mt][4 * a + 1], acc[mt][4 * a + 2], acc[mt][4 * a + 3]};
+      if (lg == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at) = float2{m_run, l_tot};
+    }
+    return;
+  }
+  const float inv = l_tot == 0.f ? 0.f : 1.f / l_tot;
+  if (live && row < nrows) {
+    uint16_t* dst = static_cast<uint16_t*>(p.o) + at_row * D + 4 * lg;
+#pragma unroll
+    for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+      for (int a = 0; a < 4; ++a)
+        *reinterpret_cast<u32x2*>(dst + 32 * mt + 8 * a) =
+            u32x2{pack_bf16(acc[mt][4 * a] * inv, acc[mt][4 * a + 1] * inv),
+                  pack_bf16(acc[mt][4 * a + 2] * inv, acc[mt][4 * a + 3] * inv)};
+    if (lg == 0) p.lse[at_row] = l_tot == 0.f ? -INFINITY : (m_run + __log2f(l_tot)) * kLn2;
+  }
+}
+
+// Join the partials of rows (token, query head): D / 4 lanes hold a row's dims, GP groups
+// of lanes take every GP-th partial, 256 / (D / 4) / GP rows to a workgroup.  A partial of
+// a share without a visible key, (-inf, 0), has no O.  Scores that are all NaN leave -inf
+// and NaN: those are added, times 0, and stay NaN.
+template <int D, int GP>
+__global__ __launch_bounds__(256) void tiles_join_kernel(TilesParams p) {
+  constexpr int LPR = D / 4, NG = 256 / LPR, NR = NG / GP;
+  __shared__ float4 red[NG][LPR];
+  __shared__ float2 stat[NG];
+  const int c = threadIdx.x % LPR, grp = threadIdx.x / LPR, gp = grp % GP;
+  const size_t rows = (size_t)p.T * p.H;
+  const size_t r = (size_t)blockIdx.x * NR + grp / GP;
+  bool live = r < rows;
+  if (live && p.starts) {   // rows outside every sequence are left as they are
+    const int token = (int)(r / p.H);
+    live = token >= p.starts[0] && token < p.starts[p.B];
+  }
+  float M = -INFINITY, l = 0.f;
+  float4 sum = {0.f, 0.f, 0.f, 0.f};
+  if (live) {
+    for (int i = gp; i < p.parts; i += GP) {
+      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (i * rows + r));
+      if (ml.x == -INFINITY && ml.y == 0.f) continue;
+      const float4 x = *reinterpret_cast<const float4*>(p.part_acc + (i * rows + r) * D + 4 * c);
+      const float m = fmaxf(M, ml.x);
+      const float a = M == -INFINITY ? 0.f : fast_exp2(M - m), w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+      sum.x = __builtin_fmaf(sum.x, a, x.x * w);
+      sum.y = __builtin_fmaf(sum.y, a, x.y * w);
+      sum.z = __builtin_fmaf(sum.z, a, x.z * w);
+      sum.w = __builtin_fmaf(sum.w, a, x.w * w);
+      l = __builtin_fmaf(l, a, ml.y * w);
+      M = m;
+    }
+  }
+  if constexpr (GP > 1) {
+    red[grp][c] = sum;
+    if (c == 0) stat[grp] = float2{M, l};
+    __syncthreads();
+    if (gp != 0 || !live) return;
+    for (int i = 1; i < GP; ++i) {
+      const float2 ml = stat[grp + i];
+      const float4 x = red[grp + i][c];
+      const float m = fmaxf(M, ml.x);
+      const float a = M == -INFINITY ? 0.f : fast_exp2(M - m), w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+      sum.x = __builtin_fmaf(sum.x, a, x.x * w);
+      sum.y = __builtin_fmaf(sum.y, a, x.y * w);
+      sum.z = __builtin_fmaf(sum.z, a, x.z * w);
+      sum.w = __builtin_fmaf(sum.w, a, x.w * w);
+      l = __builtin_fmaf(l, a, ml.y * w);
+      M = m;
+    }
+  }
+  if (!live) return;
+  const float inv = l == 0.f ? 0.f : 1.f / l;
+  *reinterpret_cast<u32x2*>(static_cast<uint16_t*>(p.o) + r * D + 4 * c) =
+      u32x2{pack_bf16(sum.x * inv, sum.y * inv), pack_bf16(sum.z * inv, sum.w * inv)};
+  if (c == 0) p.lse[r] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+}
+
+// ---------------------------------------------------------------- launch
+template <int D>
+static int launch_one(const TilesParams& p, int nw, hipStream_t st) {
+  const dim3 grid((unsigned)((p.prefix_items + p.own_items) * p.Hkv));
+  if (nw == 8) hipLaunchKernelGGL((paged_tiles_kernel<D, 8>), grid, dim3(512), 0, st, p);
+  else hipLaunchKernelGGL((paged_tiles_kernel<D, 4>), grid, dim3(256), 0, st, p);
+  if (p.parts > 1) {
+    const long long rows = (long long)p.T * p.H;
+    constexpr int NG = 1024 / D;
+    if (p.parts >= 8) hipLaunchKernelGGL((tiles_join_kernel<D, NG>), dim3((unsigned)rows), dim3(256), 0, st, p);
+    else hipLaunchKernelGGL((tiles_join_kernel<D, 1>), dim3((unsigned)((rows + NG - 1) / NG)), dim3(256), 0, st, p);
+  }
+  return hipGetLastError() == hipSuccess ? 0 : -3;
+}
+
+int launch_paged_tiles(int D, const TilesParams& p, int nw, hipStream_t st) {
+  if (D == 64) return launch_one<64>(p, nw, st);
+  if (D == 128) return launch_one<128>(p, nw, st);
+  return -2;
+}
+
+}  // namespace af

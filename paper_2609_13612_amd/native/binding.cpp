@@ -819,6 +819,42 @@ PyObject* decode_paged(Args a) {
   return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
 }
 
+// fwd_paged(q, k_cache, v_cache, block_table, q_starts, lens, prefix_table, prefix_len, out, lse, workspace, scale) -> (O, LSE)
+PyObject* fwd_paged(Args a) {
+  const Tensor &q = a.need(), &kc = a.need(), &vc = a.need(), &table = a.need();
+  const Tensor *starts = a.tensor(), *lens = a.tensor(), *prefix = a.tensor(), *plen = a.tensor(), *out_ = a.tensor(),
+               *lse = a.tensor(), *ws_ = a.tensor();
+  const c10::Device dev = q.device();
+  const at::ScalarType type = q.scalar_type();
+  if (dtype_of(q) != AF_DTYPE_BF16 || q.dim() != 3 || kc.dim() != 4 || table.dim() != 2) throw NotPlain{};
+  const int64_t T = q.size(0), H = q.size(1), D = q.size(2), pages = kc.size(0), Hkv = kc.size(1), page = kc.size(2),
+                B = table.size(0), most = table.size(1);
+  if (prefix && (prefix->dim() != 1 || prefix->size(0) < 1)) throw NotPlain{};
+  const int64_t ahead = prefix ? prefix->size(0) : 0;
+  for (int64_t n : {T, B, H, D, Hkv, pages, page, most, ahead}) if (n > (1 << 28)) throw NotPlain{};
+  if (most * page > INT_MAX || ahead * page > INT_MAX || (!starts && B != T) || (!prefix && plen)) throw NotPlain{};
+  const float scale = a.scale(D);
+  same(q, q.sizes(), type, dev);
+  const Rows ks(kc, {pages, Hkv, page, D}, type, dev), vs(vc, {pages, Hkv, page, D}, type, dev);
+  same(table, {B, most}, at::kInt, dev);
+  if (starts) same(*starts, {B + 1}, at::kInt, dev);
+  if (lens) same(*lens, {B}, at::kInt, dev);
+  if (prefix) same(*prefix, {ahead}, at::kInt, dev);
+  if (plen) same(*plen, {1}, at::kInt, dev);
+  const auto whole = [](const Tensor* t) { return t ? static_cast<const int*>(t->const_data_ptr()) : nullptr; };
+  const Tensor o = out_or(out_, q.sizes(), type, dev), l = out_or(lse, {T, H}, at::kFloat, dev);
+  const Tensor ws = workspace_or(ws_, attnfuse_fwd_paged_workspace_bytes((int)T, (int)B, (int)H, (int)Hkv, (int)D,
+                                                                         (int)(most * page), (int)(ahead * page)), dev);
+  const size_t bytes = bytes_of(ws);
+  const int rc = enqueue(dev, [&](void* st) {
+    return attnfuse_fwd_paged(in(q), in(kc), in(vc), whole(&table), whole(starts), whole(lens), whole(prefix), whole(plen),
+                              out(o), static_cast<float*>(out(l)), bytes ? out(ws) : nullptr, bytes, ks.s[0], ks.s[1], ks.s[2],
+                              vs.s[0], vs.s[1], vs.s[2], (int)T, (int)B, (int)H, (int)Hkv, (int)D, (int)pages, (int)page,
+                              (int)most, (int)ahead, scale, st);
+  });
+  return rc ? PyLong_FromLong(rc) : tuple_of({&o, &l});
+}
+
 // decode_sinks(q, k, v, lens, out, lse, workspace, table, tables, rope, theta, window, sinks, scale) -> (O, LSE)
 PyObject* decode_sinks(Args a) {
   const Tensor &q = a.need(), &k = a.need(), &v = a.need();
@@ -1188,7 +1224,7 @@ PyMethodDef methods[] = {method<fwd>("fwd"), method<bwd>("bwd"), method<decode>(
                          method<qknorm>("qknorm"), method<qknorm_bwd>("qknorm_bwd"), method<qknorm_grad>("qknorm_grad"), 
                          method<append<false>>("append"), method<axes>("axes"), method<axes_bwd>("axes_bwd"),
                          method<axes_grad>("axes_grad"), method<append<true>>("axes_append"),
-                         method<decode_paged>("decode_paged"), method<decode_sinks>("decode_sinks"),
+                         method<decode_paged>("decode_paged"), method<decode_sinks>("decode_sinks"), method<fwd_paged>("fwd_paged"),
                          method<fwd_sinks>("fwd_sinks"), method<bwd_sinks>("bwd_sinks"), method<sinks_grad>("sinks_grad"),
                          {nullptr, nullptr, 0, nullptr}};
 
