@@ -37,13 +37,6 @@ __device__ __forceinline__ int scalar_load(const int* p) {
   return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
 }
 
-// A pointer that is the same in every lane, in scalar registers.
-__device__ __forceinline__ const uint16_t* uniform(const uint16_t* p) {
-  const uint64_t x = (uint64_t)p;
-  return (const uint16_t*)((uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)x) |
-                           (uint64_t)(uint32_t)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32);
-}
-
 // The queries of a sequence: tokens [first, first + n), and its own keys.
 struct Sequence {
   int b, first, n, keys;
@@ -151,29 +144,40 @@ void paged_tiles_kernel(TilesParams p) {
   const int lim_wave = shift_keys + min(r0 + 32 * wave, nrows - 1) / G;   // the least of the wave's
 
   // ---- tiles
-  const uint16_t* __restrict__ K = static_cast<const uint16_t*>(p.k) + g * p.ks[1];
-  const uint16_t* __restrict__ V = static_cast<const uint16_t*>(p.v) + g * p.vs[1];
+  // A tile's page numbers come by a vector load, lane u that of unit u % 4, and so do its
+  // rows' addresses: lanes 0 .. 3 hold K's units', lanes 4 .. 7 V's.  They are read two
+  // tiles ahead, on the way behind the copies that the loop waits for anyway.
+  const int lane_unit = lane & 3;
+  const bool lane_v = lane & 4;
+  const uint16_t* lane_base = static_cast<const uint16_t*>(lane_v ? p.v : p.k) + g * (lane_v ? p.vs[1] : p.ks[1]);
+  const long long lane_page = lane_v ? p.vs[0] : p.ks[0];
+  const uint32_t lane_place = (uint32_t)(lane_v ? p.vs[2] : p.ks[2]);
   struct Tile {
     int n0, end;          // its first key in the prefix or in the sequence, and where those end
     bool prefix;
-    int pg[4];            // pages of its units, -1: none there
+    uint32_t valid;       // bit u: unit u has a page
+    uint64_t base;        // lane u: K's unit u, lane 4 + u: V's
   };
-  auto tile_at = [&](int i) {
-    Tile t;
+  auto place_of = [&](int i) {   // of the workgroup's i-th tile
+    Tile t{};
     const int idx = share + i * ns;
     t.prefix = idx < tp;
     t.n0 = BN * (t.prefix ? idx : idx - tp);
     t.end = t.prefix ? np : own;
-    const int* pages = t.prefix ? p.prefix_table : table;
-    const int last = (t.prefix ? p.prefix_pages : p.max_pages) - 1;
-#pragma unroll
-    for (int u = 0; u < 4; ++u) {
-      const int e = scalar_load(pages + min((t.n0 + 16 * u) >> p.page_shift, last));
-      t.pg[u] = (unsigned)e < (unsigned)p.num_pages ? e : -1;
-    }
     return t;
   };
-  auto whole = [&](const Tile& t) { return t.n0 + BN <= t.end && (t.pg[0] | t.pg[1] | t.pg[2] | t.pg[3]) >= 0; };
+  auto entry_of = [&](const Tile& t) {
+    const int* pages = t.prefix ? p.prefix_table : table;
+    const int last = (t.prefix ? p.prefix_pages : p.max_pages) - 1;
+    return pages[min((t.n0 + 16 * lane_unit) >> p.page_shift, last)];
+  };
+  auto settle = [&](Tile& t, int e) {
+    const bool ok = (unsigned)e < (unsigned)p.num_pages;
+    t.valid = (uint32_t)__ballot(ok) & 15u;
+    const uint32_t place = (uint32_t)(t.n0 + 16 * lane_unit) & ((1u << p.page_shift) - 1);
+    t.base = (uint64_t)(lane_base + (ok ? e : 0) * lane_page + (uint64_t)place * lane_place);
+  };
+  auto whole = [&](const Tile& t) { return t.n0 + BN <= t.end && t.valid == 15u; };
 
   const AT at(lane, wave);
   auto akst = [&](int par) { return smem + 2 * par * AT::ELEMS; };
@@ -181,38 +185,41 @@ void paged_tiles_kernel(TilesParams p) {
   constexpr int CPR = D / 8;
   const int unit0 = wave * RPG / 16, row_in_unit = wave * RPG % 16 + lane / CPR;   // of the wave's first group
   auto unit_of = [&](int i) { return unit0 + NW * RPG / 16 * i; };
-  auto page_of = [&](const Tile& t, int i) {
-    int x = t.pg[0];
-#pragma unroll
-    for (int u = 1; u < 4; ++u) x = unit_of(i) == u ? t.pg[u] : x;
-    return x;
-  };
-  auto load = [&](const uint16_t* X, const long long (&st)[3], const Tile& t, uint16_t* dst) {
+  const uint32_t voff_k = (uint32_t)row_in_unit * (uint32_t)(2 * p.ks[2]) + at.col;
+  const uint32_t voff_v = (uint32_t)row_in_unit * (uint32_t)(2 * p.vs[2]) + at.col;
+  auto load = [&](const Tile& t, int lane0, uint32_t voff, uint16_t* dst) {
     const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)dst;
-    const uint32_t voff = (uint32_t)row_in_unit * (uint32_t)(2 * st[2]) + at.col;
 #pragma unroll
     for (int i = 0; i < AT::NI; ++i) {
-      const int n = t.n0 + 16 * unit_of(i);
-      const uint16_t* base = X + (long long)max(page_of(t, i), 0) * st[0] + (long long)(n & ((1 << p.page_shift) - 1)) * st[2];
-      async_copy16(uniform(base), voff, __builtin_amdgcn_readfirstlane(lds + (wave + NW * i) * (AT::GROUP * 2)));
+      const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)t.base, lane0 + unit_of(i));
+      const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(t.base >> 32), lane0 + unit_of(i));
+      async_copy16((const void*)((uint64_t)hi << 32 | lo), voff,
+                   __builtin_amdgcn_readfirstlane(lds + (wave + NW * i) * (AT::GROUP * 2)));
     }
   };
+  auto load_k = [&](const Tile& t, uint16_t* dst) { load(t, 0, voff_k, dst); };
+  auto load_v = [&](const Tile& t, uint16_t* dst) { load(t, 4, voff_v, dst); };
   // Rows of V that are no key: 0 x NaN is NaN.  (Each lane clears what it copied.)
   auto clear = [&](const Tile& t, uint16_t* dst) {
     if (whole(t)) return;
 #pragma unroll
     for (int i = 0; i < AT::NI; ++i) {
       const int n = t.n0 + 16 * unit_of(i) + row_in_unit;
-      if (n >= t.end || page_of(t, i) < 0)
+      if (n >= t.end || !(t.valid >> unit_of(i) & 1))
         *reinterpret_cast<u32x4*>(dst + (wave + NW * i) * AT::GROUP + 8 * lane) = u32x4{0, 0, 0, 0};
     }
   };
 
-  Tile cur_t = tile_at(0), nxt_t = tile_at(min(1, nt - 1));
-  load(K, p.ks, cur_t, akst(0));
-  load(V, p.vs, cur_t, avst(0));
-  if (nt > 1) load(K, p.ks, nxt_t, akst(1));
-  Tile far_t = tile_at(min(2, nt - 1));
+  Tile cur_t = place_of(0), nxt_t = place_of(min(1, nt - 1)), far_t = place_of(min(2, nt - 1));
+  {
+    const int e0 = entry_of(cur_t), e1 = entry_of(nxt_t), e2 = entry_of(far_t);
+    settle(cur_t, e0);
+    settle(nxt_t, e1);
+    settle(far_t, e2);
+  }
+  load_k(cur_t, akst(0));
+  load_v(cur_t, avst(0));
+  if (nt > 1) load_k(nxt_t, akst(1));
 
   // Query operand (B of S^T = K Q^T): lane holds its row, dims 16 s + 8 lg .. +7.
   u32x4 qreg[KS];
@@ -247,12 +254,14 @@ void paged_tiles_kernel(TilesParams p) {
     if (!whole(t) || (!t.prefix && t.n0 + BN - 1 > lim_wave)) {   // (wave-uniform)
       const int seen = (t.prefix ? t.end - 1 : lim) - t.n0 - 4 * lg;
 #pragma unroll
-      for (int kt = 0; kt < 2; ++kt)
+      for (int u = 0; u < 4; ++u) {
+        const int last = t.valid >> u & 1 ? seen : -1;
 #pragma unroll
-        for (int r = 0; r < 16; ++r) {
-          const bool ok = 32 * kt + 8 * (r >> 2) + (r & 3) <= seen && t.pg[2 * kt + (r >> 3)] >= 0;
-          sc[kt][r] = ok ? sc[kt][r] : -INFINITY;
+        for (int r = 0; r < 8; ++r) {
+          const float x = sc[u >> 1][8 * (u & 1) + r];
+          sc[u >> 1][8 * (u & 1) + r] = 16 * u + 8 * (r >> 2) + (r & 3) <= last ? x : -INFINITY;
         }
+      }
     }
     float mx = -INFINITY;
 #pragma unroll
@@ -309,8 +318,10 @@ void paged_tiles_kernel(TilesParams p) {
   int t = 0;
   auto iteration = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], auto parity) {
     constexpr int PAR = decltype(parity)::value;   // t & 1
-    load(K, p.ks, far_t, akst(PAR));
-    load(V, p.vs, nxt_t, avst(1 - PAR));
+    load_k(far_t, akst(PAR));
+    load_v(nxt_t, avst(1 - PAR));
+    Tile after = place_of(min(t + 3, nt - 1));
+    int e = entry_of(after);
     if (live) {
       probs(cur, pop);
       scores(nxt, akst(1 - PAR));
@@ -319,9 +330,9 @@ void paged_tiles_kernel(TilesParams p) {
       pv(pop, avst(PAR));
       raise();
     }
-    const Tile after = tile_at(min(t + 3, nt - 1));
-    async_wait();
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(e)::"memory");   // the copies, and the pages behind them
     clear(nxt_t, avst(1 - PAR));
+    settle(after, e);
     __syncthreads();
     nxt_t = far_t;
     far_t = after;
