@@ -91,31 +91,48 @@ void paged_tiles_kernel(TilesParams p) {
   int i = blockIdx.x / p.Hkv, r0, nrows, first, np = 0, share, ns, part, shift_keys = 0;
   const int* table = p.table;
   const bool prefix_list = i < p.prefix_items;             // (apart: a list of all tokens' rows)
-  if (p.prefix_pages > 0 && (prefix_list || p.joined))
-    np = p.prefix_len ? min(max(scalar_load(p.prefix_len), 0), p.P) : p.P;
-  int own = 0;                                             // own keys that any row of the workgroup sees
+  int b = 0;
   if (prefix_list) {
     ns = p.nsp;
     share = i % ns;
     r0 = i / ns * ROWS;
-    nrows = p.T * p.G;
-    first = 0;
     part = share;
   } else {
     i -= p.prefix_items;
     ns = p.nso;
     share = i % ns;
-    const int b = __builtin_amdgcn_readfirstlane(sequence_of(p, i / ns, ROWS, lane, r0));
+    b = __builtin_amdgcn_readfirstlane(sequence_of(p, i / ns, ROWS, lane, r0));
     r0 = __builtin_amdgcn_readfirstlane(r0);
     if (b < 0) return;
+    table += (size_t)b * p.max_pages;
+    part = p.nsp + share;
+  }
+  // A tile's page numbers come by a vector load, lane u that of unit u % 4 (and its rows'
+  // addresses are formed there: lanes 0 .. 3 hold K's units', lanes 4 .. 7 V's).
+  const int lane_unit = lane & 3;
+  auto entry_of = [&](bool prefix, int n0) {
+    const int* pages = prefix ? p.prefix_table : table;
+    const int last = (prefix ? p.prefix_pages : p.max_pages) - 1;
+    return pages[min((n0 + 16 * lane_unit) >> p.page_shift, last)];
+  };
+  int e[3];
+  if (!p.joined) {   // apart, the first tiles' places do not depend on any length: one trip to memory less
+#pragma unroll
+    for (int j = 0; j < 3; ++j) e[j] = entry_of(prefix_list, BN * (share + j * ns));
+  }
+  if (p.prefix_pages > 0 && (prefix_list || p.joined))
+    np = p.prefix_len ? min(max(scalar_load(p.prefix_len), 0), p.P) : p.P;
+  int own = 0;                                             // own keys that any row of the workgroup sees
+  if (prefix_list) {
+    nrows = p.T * p.G;
+    first = 0;
+  } else {
     const Sequence s = sequence_at(p, b);
     nrows = s.n * p.G;
     if (r0 >= nrows) return;
     first = s.first;
-    table += (size_t)b * p.max_pages;
     shift_keys = s.keys - s.n;                             // token t sees its keys up to shift_keys + t
     own = max(0, shift_keys + (min(r0 + ROWS, nrows) - 1) / p.G + 1);
-    part = p.nsp + share;
   }
   const int tp = (np + BN - 1) / BN, all = tp + (own + BN - 1) / BN;
   const int nt = all > share ? (all - share + ns - 1) / ns : 0;
@@ -144,10 +161,8 @@ void paged_tiles_kernel(TilesParams p) {
   const int lim_wave = shift_keys + min(r0 + 32 * wave, nrows - 1) / G;   // the least of the wave's
 
   // ---- tiles
-  // A tile's page numbers come by a vector load, lane u that of unit u % 4, and so do its
-  // rows' addresses: lanes 0 .. 3 hold K's units', lanes 4 .. 7 V's.  They are read two
-  // tiles ahead, on the way behind the copies that the loop waits for anyway.
-  const int lane_unit = lane & 3;
+  // (Page numbers are read two tiles ahead, on the way behind the copies that the loop
+  // waits for anyway.)
   const bool lane_v = lane & 4;
   const uint16_t* lane_base = static_cast<const uint16_t*>(lane_v ? p.v : p.k) + g * (lane_v ? p.vs[1] : p.ks[1]);
   const long long lane_page = lane_v ? p.vs[0] : p.ks[0];
@@ -161,15 +176,10 @@ void paged_tiles_kernel(TilesParams p) {
   auto place_of = [&](int i) {   // of the workgroup's i-th tile
     Tile t{};
     const int idx = share + i * ns;
-    t.prefix = idx < tp;
+    t.prefix = prefix_list || idx < tp;                    // (apart, no length has to be known for it)
     t.n0 = BN * (t.prefix ? idx : idx - tp);
     t.end = t.prefix ? np : own;
     return t;
-  };
-  auto entry_of = [&](const Tile& t) {
-    const int* pages = t.prefix ? p.prefix_table : table;
-    const int last = (t.prefix ? p.prefix_pages : p.max_pages) - 1;
-    return pages[min((t.n0 + 16 * lane_unit) >> p.page_shift, last)];
   };
   auto settle = [&](Tile& t, int e) {
     const bool ok = (unsigned)e < (unsigned)p.num_pages;
@@ -210,13 +220,15 @@ void paged_tiles_kernel(TilesParams p) {
     }
   };
 
-  Tile cur_t = place_of(0), nxt_t = place_of(min(1, nt - 1)), far_t = place_of(min(2, nt - 1));
-  {
-    const int e0 = entry_of(cur_t), e1 = entry_of(nxt_t), e2 = entry_of(far_t);
-    settle(cur_t, e0);
-    settle(nxt_t, e1);
-    settle(far_t, e2);
+  Tile cur_t = place_of(0), nxt_t = place_of(1), far_t = place_of(2);
+  if (p.joined) {
+    e[0] = entry_of(cur_t.prefix, cur_t.n0);
+    e[1] = entry_of(nxt_t.prefix, nxt_t.n0);
+    e[2] = entry_of(far_t.prefix, far_t.n0);
   }
+  settle(cur_t, e[0]);
+  settle(nxt_t, e[1]);
+  settle(far_t, e[2]);
   load_k(cur_t, akst(0));
   load_v(cur_t, avst(0));
   if (nt > 1) load_k(nxt_t, akst(1));
@@ -314,14 +326,14 @@ void paged_tiles_kernel(TilesParams p) {
   __syncthreads();
   // Iteration t turns tile t's scores into its share of O while tile t + 1's scores are
   // formed; it copies K of tile t + 2 and V of tile t + 1 into the stage halves that the
-  // last barrier freed (past the last tile: that one again, which nobody reads).
+  // last barrier freed.
   int t = 0;
   auto iteration = [&](f32x16 (&cur)[2], f32x16 (&nxt)[2], auto parity) {
     constexpr int PAR = decltype(parity)::value;   // t & 1
-    load_k(far_t, akst(PAR));
+    if (t + 2 < nt) load_k(far_t, akst(PAR));
     load_v(nxt_t, avst(1 - PAR));
-    Tile after = place_of(min(t + 3, nt - 1));
-    int e = entry_of(after);
+    Tile after = place_of(t + 3);
+    int entry = entry_of(after.prefix, after.n0);
     if (live) {
       probs(cur, pop);
       scores(nxt, akst(1 - PAR));
@@ -330,9 +342,9 @@ void paged_tiles_kernel(TilesParams p) {
       pv(pop, avst(PAR));
       raise();
     }
-    asm volatile("s_waitcnt vmcnt(0)" : "+v"(e)::"memory");   // the copies, and the pages behind them
+    asm volatile("s_waitcnt vmcnt(0)" : "+v"(entry)::"memory");   // the copies, and the pages behind them
     clear(nxt_t, avst(1 - PAR));
-    settle(after, e);
+    settle(after, entry);
     __syncthreads();
     nxt_t = far_t;
     far_t = after;
@@ -402,21 +414,33 @@ __global__ __launch_bounds__(256) void tiles_join_kernel(TilesParams p) {
     const int token = (int)(r / p.H);
     live = token >= p.starts[0] && token < p.starts[p.B];
   }
+  // What a partial (m2, l2, x) adds to (M, l, sum).
   float M = -INFINITY, l = 0.f;
   float4 sum = {0.f, 0.f, 0.f, 0.f};
+  auto fold = [&](const float2& ml, const float4& x) {
+    const float m = fmaxf(M, ml.x);
+    const float a = M == -INFINITY ? 0.f : fast_exp2(M - m), w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+    sum.x = __builtin_fmaf(sum.x, a, x.x * w);
+    sum.y = __builtin_fmaf(sum.y, a, x.y * w);
+    sum.z = __builtin_fmaf(sum.z, a, x.z * w);
+    sum.w = __builtin_fmaf(sum.w, a, x.w * w);
+    l = __builtin_fmaf(l, a, ml.y * w);
+    M = m;
+  };
   if (live) {
-    for (int i = gp; i < p.parts; i += GP) {
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + 2 * (i * rows + r));
-      if (ml.x == -INFINITY && ml.y == 0.f) continue;
-      const float4 x = *reinterpret_cast<const float4*>(p.part_acc + (i * rows + r) * D + 4 * c);
-      const float m = fmaxf(M, ml.x);
-      const float a = M == -INFINITY ? 0.f : fast_exp2(M - m), w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
-      sum.x = __builtin_fmaf(sum.x, a, x.x * w);
-      sum.y = __builtin_fmaf(sum.y, a, x.y * w);
-      sum.z = __builtin_fmaf(sum.z, a, x.z * w);
-      sum.w = __builtin_fmaf(sum.w, a, x.w * w);
-      l = __builtin_fmaf(l, a, ml.y * w);
-      M = m;
+    // Four partials on their way at once; where there is no O, what is read in its place is not used.
+    for (int i0 = gp; i0 < p.parts; i0 += 4 * GP) {
+      float2 ml[4];
+      float4 x[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const size_t at = min(i0 + j * GP, p.parts - 1) * rows + r;
+        ml[j] = *reinterpret_cast<const float2*>(p.part_ml + 2 * at);
+        x[j] = *reinterpret_cast<const float4*>(p.part_acc + at * D + 4 * c);
+      }
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+        if (i0 + j * GP < p.parts && !(ml[j].x == -INFINITY && ml[j].y == 0.f)) fold(ml[j], x[j]);
     }
   }
   if constexpr (GP > 1) {
@@ -426,15 +450,7 @@ __global__ __launch_bounds__(256) void tiles_join_kernel(TilesParams p) {
     if (gp != 0 || !live) return;
     for (int i = 1; i < GP; ++i) {
       const float2 ml = stat[grp + i];
-      const float4 x = red[grp + i][c];
-      const float m = fmaxf(M, ml.x);
-      const float a = M == -INFINITY ? 0.f : fast_exp2(M - m), w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
-      sum.x = __builtin_fmaf(sum.x, a, x.x * w);
-      sum.y = __builtin_fmaf(sum.y, a, x.y * w);
-      sum.z = __builtin_fmaf(sum.z, a, x.z * w);
-      sum.w = __builtin_fmaf(sum.w, a, x.w * w);
-      l = __builtin_fmaf(l, a, ml.y * w);
-      M = m;
+      if (!(ml.x == -INFINITY && ml.y == 0.f)) fold(ml, red[grp + i][c]);
     }
   }
   if (!live) return;
