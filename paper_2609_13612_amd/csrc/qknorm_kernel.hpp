@@ -97,15 +97,30 @@ __device__ __forceinline__ float row_sum(float x) {
 // What p.axis says of the thread's pairs (see Angles): two bits for each of its 8.
 template <int D, int ROPE>
 __device__ __forceinline__ uint32_t axes_of(const QkNormParams& p, int c) {
-  auto word = [&](int w) {   // (selects: an index that differs by lane would go through memory)
-    uint32_t x = w & 1 ? p.axis[1] : p.axis[0];
-    if constexpr (D == 128) x = w & 2 ? (w & 1 ? p.axis[3] : p.axis[2]) : x;
-    return x;
+  // Values, not places, are chosen by lane here and below: a place that differs by lane
+  // would go through memory (one token's append took 7.9 us instead of 3.9).
+  const u32x4 axis = {p.axis[0], p.axis[1], p.axis[2], p.axis[3]};
+  auto word = [&](int w) {
+    const uint32_t lo = w & 1 ? axis.y : axis.x;
+    if constexpr (D == 64) return lo;
+    const uint32_t hi = w & 1 ? axis.w : axis.z;
+    return w & 2 ? hi : lo;
   };
   if constexpr (ROPE == ROPE_NEOX) return word(c >> 1) >> (16 * (c & 1)) & 0xffffu;
   const uint32_t lo = word(c >> 2) >> (8 * (c & 3)) & 0xffu, hi = word((D / 64) + (c >> 2)) >> (8 * (c & 3)) & 0xffu;
   return lo | hi << 8;
 }
+
+// The positions of a row of the call, of which there are n, on its axes.  Asked for before
+// the row itself: the table's rows wait for them, and nothing else of the thread's does.
+struct RowPositions {
+  u32x4 at;   // (a vector, not an array: see axes_of)
+  __device__ __forceinline__ void load(const QkNormParams& p, size_t row, size_t n) {
+    const int* x = p.positions + row;
+    const int last = p.axes - 1;
+    at = u32x4{(uint32_t)x[0], (uint32_t)x[min(1, last) * n], (uint32_t)x[min(2, last) * n], (uint32_t)x[min(3, last) * n]};
+  }
+};
 
 // cos and sin of the thread's 8 pairs at position pos: NeoX pair 8c + i is
 // (v[i], v[8 + i]); interleaved pairs are (v[2i], v[2i + 1]), 4c + i and D/4 + 4c
@@ -133,22 +148,17 @@ struct Angles {
       }
     }
   }
-  // The same, each pair at the position on its axis: those of row `row` of the call, of
-  // which there are n, in p.positions[axis][row].  Two neighbours on one axis, in every
+  // The same, each pair at the position on its axis.  Two neighbours on one axis, in every
   // thread (p.by_two), share a load.
-  __device__ __forceinline__ void load_axes(const QkNormParams& p, size_t row, size_t n, int ch) {
-    int at[4];
-    bool ok = true;
-#pragma unroll
-    for (int a = 0; a < 4; ++a) {
-      const int pos = p.positions[min(a, p.axes - 1) * n + row];
-      ok = ok && (unsigned)pos < (unsigned)p.rows;
-      at[a] = (unsigned)pos < (unsigned)p.rows ? pos : 0;
-    }
-    const uint32_t bits = axes_of<D, ROPE>(p, ch);
+  __device__ __forceinline__ void load_axes(const QkNormParams& p, const RowPositions& pos, int ch) {
+    const uint32_t rows = (uint32_t)p.rows;
+    const bool ok = pos.at.x < rows && pos.at.y < rows && pos.at.z < rows && pos.at.w < rows;
+    const u32x4 at = ok ? pos.at : u32x4{0, 0, 0, 0};
+    uint32_t bits = axes_of<D, ROPE>(p, ch);
+    asm volatile("" : "+v"(bits));   // (in the backward's loop the choices are formed anew, not kept in registers)
     auto entry = [&](int i) {
       const uint32_t a = bits >> (2 * i) & 3u;
-      const int t = a & 2u ? (a & 1u ? at[3] : at[2]) : (a & 1u ? at[1] : at[0]);
+      const uint32_t lo = a & 1u ? at.y : at.x, hi = a & 1u ? at.w : at.z, t = a & 2u ? hi : lo;
       const int pair = ROPE == ROPE_NEOX ? 8 * ch + i : (i < 4 ? 4 * ch + i : D / 4 + 4 * ch + i - 4);
       return p.table + (size_t)t * (D / 2) + pair;
     };
@@ -239,11 +249,13 @@ __global__ __launch_bounds__(256) void qknorm_rope_kernel(QkNormParams p) {
   const int nh = p.heads[t], h0 = hg * HPT;
   const char* x = static_cast<const char*>(p.x[t]) + (b * p.xs[t][0] + n * p.xs[t][2]) * EB;
 
+  [[maybe_unused]] RowPositions pos;
+  if constexpr (AXES) pos.load(p, (size_t)b * p.S + n, (size_t)p.B * p.S);
   RowChunk<FP32> r[HPT];
 #pragma unroll
   for (int j = 0; j < HPT; ++j) r[j].load(x + min(h0 + j, nh - 1) * p.xs[t][1] * EB, d0, d1);
   Angles<D, ROPE> a;
-  if constexpr (AXES) a.load_axes(p, (size_t)b * p.S + n, (size_t)p.B * p.S, c);
+  if constexpr (AXES) a.load_axes(p, pos, c);
   else a.load(p.table, p.rows, p.positions ? p.positions[(size_t)b * p.S + n] : n, d0);
   float w[16];
   load_weights(w, p.w[t], p.w32, d0, d1);
@@ -282,6 +294,10 @@ __global__ __launch_bounds__(256) void qknorm_append_kernel(QkNormParams p) {
   const int nh = t ? p.heads[1] : p.heads[0], h0 = hg * HPT;
   const char* x = static_cast<const char*>(p.x[t]) + n * p.xs[t][2] * EB;
 
+  [[maybe_unused]] RowPositions pos;
+  if constexpr (AXES) {
+    if (t < 2) pos.load(p, n, p.S);
+  }
   RowChunk<FP32> r[HPT];
 #pragma unroll
   for (int j = 0; j < HPT; ++j) r[j].load(x + min(h0 + j, nh - 1) * p.xs[t][1] * EB, d0, d1);
@@ -301,7 +317,7 @@ __global__ __launch_bounds__(256) void qknorm_append_kernel(QkNormParams p) {
   }
   if (t < 2) {
     Angles<D, ROPE> a;
-    if constexpr (AXES) a.load_axes(p, n, p.S, c);
+    if constexpr (AXES) a.load_axes(p, pos, c);
     else a.load(p.table, p.rows, ROPE != ROPE_NONE ? p.positions[n] : 0, d0);
     float w[16];
     load_weights(w, p.w[t], p.w32, d0, d1);
@@ -343,6 +359,8 @@ __global__ __launch_bounds__(256) void qknorm_rope_bwd_kernel(QkNormParams p) {
     const int hb = u / nblk, h0 = (hb % groups) * HPT, i = threadIdx.x / TPR;
     int b = hb / groups, n = u % nblk * R + i;
     if (place(p, i, b, n)) {   // (rows' lanes together)
+      [[maybe_unused]] RowPositions pos;
+      if constexpr (AXES) pos.load(p, (size_t)b * p.S + n, (size_t)p.B * p.S);
       const char* x = static_cast<const char*>(p.x[t]) + (b * p.xs[t][0] + n * p.xs[t][2]) * EB;
       const char* dy = static_cast<const char*>(p.dy[t]) + ((size_t)b * nh * p.S + n) * D * EB;
       char* dx = static_cast<char*>(p.y[t]) + (b * p.ys[t][0] + n * p.ys[t][2]) * EB;
@@ -354,7 +372,7 @@ __global__ __launch_bounds__(256) void qknorm_rope_bwd_kernel(QkNormParams p) {
         rd[j].load(dy + (size_t)h * p.S * D * EB, d0, d1);
       }
       Angles<D, ROPE> a;
-      if constexpr (AXES) a.load_axes(p, (size_t)b * p.S + n, (size_t)p.B * p.S, c);
+      if constexpr (AXES) a.load_axes(p, pos, c);
       else a.load(p.table, p.rows, p.positions ? p.positions[(size_t)b * p.S + n] : n, d0);
 #pragma unroll
       for (int j = 0; j < HPT; ++j) {
