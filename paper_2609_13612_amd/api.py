@@ -707,14 +707,15 @@ def attnfuse_qknorm_rope(q, k=None, q_weight=None, k_weight=None, *, eps=1e-6, r
 
 def _axes_fwd(q, k, q_weight, k_weight, eps, rope, theta, positions, max_positions, out_q, out_k, rope_table, sections,
               section_order, frequencies, norm):
+    if _native is not None:
+        r = _native.axes(q, k, q_weight, k_weight, out_q, out_k, positions, rope_table, _TABLES, eps, ROPE.get(rope, -1),
+                         theta, max_positions, int(bool(norm)), sections, section_order, SECTION_ORDER.get(section_order, -1),
+                         FREQUENCIES.get(frequencies, -1))
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_axes")
     dev = _device(q)
     axes = _axes(sections, section_order, frequencies, norm, rope, q.shape[-1], positions)
     tab = _axes_table(axes, frequencies, rope, theta, q.shape[-1], dev, max_positions, rope_table)
-    if _native is not None:
-        r = _native.axes(q, k, q_weight, k_weight, out_q, out_k, positions, tab, eps, ROPE[rope], theta, max_positions,
-                         int(bool(norm)), axes[0], SECTION_ORDER[axes[1]])
-        if r is not None:
-            return _result(r, "attnfuse_qknorm_axes")
     dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
     wt = _axes_weights(q_weight, k_weight, norm, D, q.dtype, dev)
     _need(positions, "positions", (len(axes[0]), B, S), torch.int32, dev)
@@ -784,19 +785,20 @@ def attnfuse_qknorm_rope_bwd(q, k, dqr, dkr, q_weight=None, k_weight=None, *, ep
 
 def _axes_bwd(q, k, dqr, dkr, q_weight, k_weight, eps, rope, theta, positions, max_positions, weight_grads, dq, dk, workspace,
               rope_table, sections, section_order, frequencies, norm):
+    if not norm:
+        q = k = None
+        weight_grads = False
+    if _native is not None:
+        r = _native.axes_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, rope_table, _TABLES, eps,
+                             ROPE.get(rope, -1), theta, max_positions, int(bool(weight_grads)), int(bool(norm)), sections,
+                             section_order, SECTION_ORDER.get(section_order, -1), FREQUENCIES.get(frequencies, -1))
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_axes_bwd")
     dev = _device(dqr)
     if dqr.dim() != 4 or (dkr is not None and (not isinstance(dkr, torch.Tensor) or dkr.dim() != 4)):
         raise ValueError("dqr must be [B, H, S, D] and dkr [B, H_kv, S, D]")
     axes = _axes(sections, section_order, frequencies, norm, rope, dqr.shape[-1], positions)
     tab = _axes_table(axes, frequencies, rope, theta, dqr.shape[-1], dev, max_positions, rope_table)
-    if not norm:
-        q = k = None
-        weight_grads = False
-    if _native is not None:
-        r = _native.axes_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, tab, eps, ROPE[rope], theta,
-                             max_positions, int(bool(weight_grads)), int(bool(norm)), axes[0], SECTION_ORDER[axes[1]])
-        if r is not None:
-            return _result(r, "attnfuse_qknorm_axes_bwd")
     if norm:
         dev, (B, H, Hkv, S, D), qs, ks = _qknorm_shape(q, k)
         if k is None and (dkr is not None or dk is not None or k_weight is not None):
@@ -881,14 +883,15 @@ def attnfuse_qknorm_rope_append(q, k, v, k_cache, v_cache, slots, q_weight=None,
 
 def _axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, norm, eps, rope, theta, positions, max_positions, out_q,
                  rope_table, sections, section_order, frequencies):
+    if _native is not None:
+        r = _native.axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, rope_table, _TABLES,
+                                eps, ROPE.get(rope, -1), theta, max_positions, int(bool(norm)), sections, section_order,
+                                SECTION_ORDER.get(section_order, -1), FREQUENCIES.get(frequencies, -1))
+        if r is not None:
+            return _result(r, "attnfuse_qknorm_axes_append")[0]
     dev = _device(q)
     axes = _axes(sections, section_order, frequencies, norm, rope, q.shape[-1], positions)
     tab = _axes_table(axes, frequencies, rope, theta, q.shape[-1], dev, max_positions, rope_table)
-    if _native is not None:
-        r = _native.axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, tab, eps, ROPE[rope],
-                                theta, max_positions, int(bool(norm)), axes[0], SECTION_ORDER[axes[1]])
-        if r is not None:
-            return _result(r, "attnfuse_qknorm_axes_append")[0]
     if q.dim() != 3 or not isinstance(k, torch.Tensor) or k.dim() != 3:
         raise ValueError("q must be [T, H, D] and k/v [T, H_kv, D]")
     T, H, D = q.shape

@@ -147,14 +147,15 @@ class _QkNormAxes(torch.autograd.Function):
 
 def _axes_grad(q, k, q_weight, k_weight, eps, rope, theta, positions, max_positions, rope_table, sections, section_order,
                frequencies, norm):
+    if api._native is not None:   # the same function, its backward in C++
+        r = api._native.axes_grad(q, k, q_weight, k_weight, positions, rope_table, api._TABLES, eps, api.ROPE.get(rope, -1),
+                                  theta, max_positions, int(bool(norm)), sections, section_order,
+                                  api.SECTION_ORDER.get(section_order, -1), api.FREQUENCIES.get(frequencies, -1))
+        if r is not None:
+            return api._result(r, "attnfuse_qknorm_axes")
     dev = api._device(q)
     axes = api._axes(sections, section_order, frequencies, norm, rope, q.shape[-1], positions)
     tab = api._axes_table(axes, frequencies, rope, theta, q.shape[-1], dev, max_positions, rope_table)
-    if api._native is not None:   # the same function, its backward in C++
-        r = api._native.axes_grad(q, k, q_weight, k_weight, positions, tab, eps, api.ROPE[rope], theta, max_positions,
-                                  int(bool(norm)), axes[0], api.SECTION_ORDER[axes[1]])
-        if r is not None:
-            return api._result(r, "attnfuse_qknorm_axes")
     cfg = dict(eps=eps, rope=rope, theta=theta, max_positions=max_positions, sections=axes[0], section_order=section_order,
                frequencies=frequencies, norm=bool(norm))
     return _QkNormAxes.apply(q, k, q_weight, k_weight, positions, tab, cfg)

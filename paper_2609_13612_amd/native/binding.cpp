@@ -141,14 +141,19 @@ int dtype_of(const Tensor& q) {
 
 // ---------------------------------------------------------------- RoPE table
 // The call's cos/sin table: the caller's, or one of the binding's (api._TABLES:
-// a dict of (device index, D, theta) -> list of tables).
+// a dict of (device index, D, theta) -> list of tables; own: of (device index, D, theta,
+// sections, section_order), where every axis has its own frequencies).
 struct Table {
   const float* ptr = nullptr;
   int rows = 0;
   Tensor own;   // the tensor itself: a differentiable call keeps it for its backward
 };
 
-Table table_of(Args& a, int rope, double theta, int64_t D, int64_t S, c10::Device dev) {
+struct OwnKey {
+  PyObject *sections, *order;
+};
+
+Table table_of(Args& a, int rope, double theta, int64_t D, int64_t S, c10::Device dev, const OwnKey* own = nullptr) {
   const Tensor* given = a.tensor();
   PyObject* tables = a.next();
   Table r;
@@ -165,7 +170,8 @@ Table table_of(Args& a, int rope, double theta, int64_t D, int64_t S, c10::Devic
     return r;
   }
   if (!PyDict_CheckExact(tables)) throw NotPlain{};
-  PyObject* key = Py_BuildValue("(iid)", (int)dev.index(), (int)D, (double)(float)theta);
+  PyObject* key = own ? Py_BuildValue("(iidOO)", (int)dev.index(), (int)D, (double)(float)theta, own->sections, own->order)
+                      : Py_BuildValue("(iid)", (int)dev.index(), (int)D, (double)(float)theta);
   if (!key) {
     PyErr_Clear();
     throw NotPlain{};
@@ -525,7 +531,9 @@ struct Norm {
   int n = 0, sections[4] = {0, 0, 0, 0}, order = 0;
   explicit Norm(Args& a) : eps((float)a.number()), rope(a.index()), theta(a.number()) {}
   Norm(float e, int r, double t) : eps(e), rope(r), theta(t) {}
-  void take_axes(Args& a) {   // norm, sections, section_order
+  bool own = false;   // every axis has its own frequencies
+  OwnKey key = {nullptr, nullptr};
+  void take_axes(Args& a) {   // norm, sections, section_order's name and value, frequencies
     norm = a.whole() != 0;
     PyObject* s = a.next();
     if (!PyTuple_CheckExact(s) || PyTuple_GET_SIZE(s) < 1 || PyTuple_GET_SIZE(s) > 4) throw NotPlain{};
@@ -535,7 +543,9 @@ struct Norm {
       Args one{&x, 1};
       sections[i] = one.size();
     }
+    key = {s, a.next()};
     order = a.index();
+    own = a.index() == AF_FREQUENCIES_OWN;
   }
 };
 
@@ -628,19 +638,21 @@ PyObject* qknorm_bwd(Args a) {
   return rc ? PyLong_FromLong(rc) : tuple_of({&dq, &dk, &dqw, &dkw});
 }
 
-// The angles of positions of several axes [axes, lead...]: the given table, of its rows
-// the first max_positions (0: all).
+// Positions of several axes [axes, lead...] and the table of their angles, of its rows the
+// first max_positions (0: all of the given one); late: the table and the binding's tables.
 struct AxesPlaced {
   const int* positions;
   Table table;
-  AxesPlaced(const Tensor& pos, const Tensor& tab, int64_t D, at::IntArrayRef shape, long long most, c10::Device dev) {
+  AxesPlaced(const Tensor& pos, Args late, const Norm& n, int64_t D, at::IntArrayRef shape, long long most, c10::Device dev) {
+    int64_t pairs = 0;
+    for (int s : n.sections) pairs += s;
+    if (n.rope == AF_ROPE_NONE || 2 * pairs != D) throw NotPlain{};
     same(pos, shape, at::kInt, dev);
     positions = static_cast<const int*>(pos.const_data_ptr());
-    if (tab.dim() != 3 || tab.size(0) > INT_MAX || most > tab.size(0)) throw NotPlain{};
-    same(tab, {tab.size(0), D / 2, 2}, at::kFloat, dev);
-    table.ptr = static_cast<const float*>(tab.const_data_ptr());
-    table.rows = (int)(most > 0 ? most : tab.size(0));
-    table.own = tab;
+    Args peek = late;
+    if (most <= 0 && !peek.tensor()) throw NotPlain{};
+    table = table_of(late, n.rope, n.theta, D, most > 0 ? most : 1, dev, n.own ? &n.key : nullptr);
+    if (most > 0) table.rows = (int)most;
   }
 };
 
@@ -668,19 +680,21 @@ int unturn(const Tensor& dqr, const Tensor* dkr, Tensor& dq, Tensor& dk, const N
   });
 }
 
-// axes(q, k, q_weight, k_weight, out_q, out_k, positions, table, eps, rope, theta, max_positions, norm, sections,
-//      section_order) -> (Qr, Kr)
+// axes(q, k, q_weight, k_weight, out_q, out_k, positions, table, tables, eps, rope, theta, max_positions, norm, sections,
+//      section_order, its value, frequencies) -> (Qr, Kr)
 PyObject* axes(Args a) {
   const Tensor &q = a.need(), *k = a.tensor();
   const Qk x(q, k);
   const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *ok_ = a.tensor();
-  const Tensor &pos = a.need(), &tab = a.need();
+  const Tensor& pos = a.need();
+  Args late = a;
+  a.i += 2;
   Norm n(a);
   const long long most = a.positive();
   n.take_axes(a);
   if ((!x.k && (kw || ok_)) || (!n.norm && (qw || kw))) throw NotPlain{};
   const Weights w(qw, kw, x.D, x.type, x.dev);
-  const AxesPlaced at_(pos, tab, x.D, {n.n, x.B, x.S}, most, x.dev);
+  const AxesPlaced at_(pos, late, n, x.D, {n.n, x.B, x.S}, most, x.dev);
   const Tensor oq = out_or(oq_, x.q.sizes(), x.type, x.dev);
   Tensor ok;
   if (x.k) ok = out_or(ok_, x.k->sizes(), x.type, x.dev);
@@ -688,12 +702,15 @@ PyObject* axes(Args a) {
   return rc ? PyLong_FromLong(rc) : tuple_of({&oq, &ok});
 }
 
-// axes_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, table, eps, rope, theta, max_positions,
-//          weight_grads, norm, sections, section_order) -> (dQ, dK, dq_weight, dk_weight); without norm q and k are None
+// axes_bwd(q, k, dqr, dkr, q_weight, k_weight, dq, dk, workspace, positions, table, tables, eps, rope, theta,
+//          max_positions, weight_grads, norm, sections, section_order, its value, frequencies)
+//     -> (dQ, dK, dq_weight, dk_weight); without norm q and k are None
 PyObject* axes_bwd(Args a) {
   const Tensor *q = a.tensor(), *k = a.tensor(), &dqr = a.need();
   const Tensor *dkr = a.tensor(), *qw = a.tensor(), *kw = a.tensor(), *dq_ = a.tensor(), *dk_ = a.tensor(), *ws_ = a.tensor();
-  const Tensor &pos = a.need(), &tab = a.need();
+  const Tensor& pos = a.need();
+  Args late = a;
+  a.i += 2;
   Norm n(a);
   const long long most = a.positive();
   const bool grads = a.whole() != 0;
@@ -704,13 +721,13 @@ PyObject* axes_bwd(Args a) {
   int rc;
   if (!n.norm) {
     if (q || k || qw || kw || grads || (!dkr && dk_) || dqr.dim() != 4 || (dkr && dkr->dim() != 4)) throw NotPlain{};
-    const AxesPlaced at_(pos, tab, dqr.size(3), {n.n, dqr.size(0), dqr.size(2)}, most, dqr.device());
+    const AxesPlaced at_(pos, late, n, dqr.size(3), {n.n, dqr.size(0), dqr.size(2)}, most, dqr.device());
     rc = unturn(dqr, dkr, dq, dk, n, at_.table, at_.positions);
   } else {
     if (!q || !k != !dkr || (!k && (kw || dk_))) throw NotPlain{};
     const Qk x(*q, k);
     const Weights w(qw, kw, x.D, x.type, x.dev);
-    const AxesPlaced at_(pos, tab, x.D, {n.n, x.B, x.S}, most, x.dev);
+    const AxesPlaced at_(pos, late, n, x.D, {n.n, x.B, x.S}, most, x.dev);
     if (!dq_) dq = at::empty_like(x.q);
     if (k && !dk_) dk = at::empty_like(*k);
     rc = norm_bwd(x, w, n, at_.table, at_.positions, dqr, dkr, dq, dk, dqw, dkw, ws_, grads);
@@ -720,21 +737,16 @@ PyObject* axes_bwd(Args a) {
 
 // append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, table, tables, norm, eps, rope, theta,
 //        max_positions) -> (Qr,)
-// axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, table, eps, rope, theta,
-//             max_positions, norm, sections, section_order) -> (Qr,)
+// axes_append(q, k, v, k_cache, v_cache, slots, q_weight, k_weight, out_q, positions, table, tables, eps, rope, theta,
+//             max_positions, norm, sections, section_order, its value, frequencies) -> (Qr,)
 template <bool AXES>
 PyObject* append(Args a) {
   const Tensor &q = a.need(), &k = a.need(), &v = a.need(), &kc = a.need(), &vc = a.need(), &slots = a.need();
   const Tensor *qw = a.tensor(), *kw = a.tensor(), *oq_ = a.tensor(), *pos = a.tensor();
   Args late = a;
-  const Tensor* tab = nullptr;
+  a.i += 2;
   bool norm = true;
-  if constexpr (AXES) {
-    tab = &a.need();
-  } else {
-    a.i += 2;
-    norm = a.whole() != 0;
-  }
+  if constexpr (!AXES) norm = a.whole() != 0;
   Norm n(a);
   const float eps = n.eps;
   const int rope = n.rope;
@@ -757,7 +769,7 @@ PyObject* append(Args a) {
   const Weights w(qw, kw, D, type, dev);
   if constexpr (AXES) {
     if (!norm && (qw || kw)) throw NotPlain{};
-    const AxesPlaced at_(*pos, *tab, D, {n.n, T}, most, dev);
+    const AxesPlaced at_(*pos, late, n, D, {n.n, T}, most, dev);
     const Tensor oq = out_or(oq_, q.sizes(), type, dev);
     const int rc = enqueue(dev, [&](void* st) {
       return attnfuse_qknorm_axes_append(
@@ -1137,20 +1149,22 @@ struct TurnFunction : torch::autograd::Function<TurnFunction> {
   }
 };
 
-// axes_grad(q, k, q_weight, k_weight, positions, table, eps, rope, theta, max_positions, norm, sections, section_order)
-//     -> (Qr, Kr)
+// axes_grad(q, k, q_weight, k_weight, positions, table, tables, eps, rope, theta, max_positions, norm, sections,
+//           section_order, its value, frequencies) -> (Qr, Kr)
 PyObject* axes_grad(Args a) {
   const Tensor &q = a.need(), *k = a.tensor();
-  const Tensor *qw = a.tensor(), *kw = a.tensor(), &pos = a.need(), &tab = a.need();
+  const Tensor *qw = a.tensor(), *kw = a.tensor(), &pos = a.need();
+  Args late = a;
+  a.i += 2;
   Norm n(a);
   const long long most = a.positive();
   n.take_axes(a);
   if ((!k && kw) || (!n.norm && (qw || kw))) throw NotPlain{};
   const Qk x(q, k);
-  const AxesPlaced at_(pos, tab, x.D, {n.n, x.B, x.S}, most, x.dev);
+  const AxesPlaced at_(pos, late, n, x.D, {n.n, x.B, x.S}, most, x.dev);
   if (n.norm) return norm_apply(q, k, qw, kw, &pos, at_.table, n);
   try {
-    const variable_list r = TurnFunction::apply(q, k ? *k : q, pos, tab, (int64_t)at_.table.rows, n, k != nullptr);
+    const variable_list r = TurnFunction::apply(q, k ? *k : q, pos, at_.table.own, (int64_t)at_.table.rows, n, k != nullptr);
     const Tensor ok = r.size() > 1 ? r[1] : Tensor();
     return tuple_of({&r[0], &ok});
   } catch (const Failed& f) {

@@ -279,12 +279,54 @@ def test_native_and_python_marshalling_agree(monkeypatch, norm):
     def calls():
         return api.attnfuse_qknorm_rope(q, k, qw, kw, **cfg) + api.attnfuse_qknorm_rope_bwd(q, k, dq, dk, qw, kw, **cfg)
 
+    calls()   # (builds the table)
     monkeypatch.setattr(api, "_native", Spy())
     a = calls()
     assert taken == [("axes", True), ("axes_bwd", True)]
     monkeypatch.setattr(api, "_native", None)
     b = calls()
     assert all(x is y is None or (torch.equal(x, y) and x.stride() == y.stride()) for x, y in zip(a, b))
+
+
+@pytest.mark.parametrize("native", [True, False])
+def test_refusals(monkeypatch, native):
+    need_gpu()
+    announce(f"axes refusals native={native}")
+    if not native:
+        monkeypatch.setattr(api, "_native", None)
+    g = torch.Generator().manual_seed(10)
+    q, pos = rows((1, 4, 9, 64), BF, g, "bhsd"), positions(2, (1, 9), g).cuda()
+    good = cfg_of("neox", 10000.0, (16, 16), "blocks", "own", True, pos)
+    w = torch.ones(64, device="cuda")
+    api.attnfuse_qknorm_rope(q, None, w, **good)
+    for bad in (dict(sections=(16, 17)), dict(sections=(32, 0)), dict(sections=(8, 8, 16)), dict(sections=()), dict(rope="none"),
+                dict(section_order="rows"), dict(frequencies="mine"), dict(positions=None), dict(positions=pos[0]),
+                dict(positions=pos.long()), dict(positions=pos.cpu()), dict(max_positions=None), dict(max_positions=0),
+                dict(norm=False), dict(sections=None, norm=False)):
+        with pytest.raises((ValueError, TypeError)):
+            api.attnfuse_qknorm_rope(q, None, w, **{**good, **bad})
+        with pytest.raises((ValueError, TypeError)):
+            autograd.qknorm_rope(q, None, w, **{**good, **bad})
+    table = api.rope_table(64, 10000.0, 100, sections=(16, 16), frequencies="own")
+    with pytest.raises(ValueError):   # a table of fewer rows than max_positions
+        api.attnfuse_qknorm_rope(q, None, w, **good, rope_table=table)
+    with pytest.raises(api.AttnFuseError):
+        api.attnfuse_qknorm_rope(q[..., :32].contiguous(), None, **{**good, "sections": (8, 8)})   # no kernel for D = 32
+
+
+def test_a_given_table_is_used_to_its_rows():
+    """rope_table without max_positions: positions below its rows, others NaN; the bits of the binding's own table."""
+    need_gpu()
+    announce("axes given table")
+    g = torch.Generator().manual_seed(14)
+    q, pos = rows((1, 4, 9, 128), BF, g, "bhsd"), positions(3, (1, 9), g) % 100
+    pos[1, 0, 4] = 100
+    table = api.rope_table(128, 10000.0, 100, sections=(24, 20, 20), section_order="turns", frequencies="own")
+    cfg = cfg_of("neox", 10000.0, (24, 20, 20), "turns", "own", False, pos.cuda())
+    want = api.attnfuse_qknorm_rope(q, **cfg)[0]
+    got = api.attnfuse_qknorm_rope(q, **{**cfg, "max_positions": None}, rope_table=table)[0]
+    hit = torch.arange(9) == 4
+    assert got[:, :, hit].isnan().all() and torch.equal(got[:, :, ~hit], want[:, :, ~hit])
 
 
 def test_captured_step_replays():
