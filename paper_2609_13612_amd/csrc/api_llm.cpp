@@ -436,59 +436,64 @@ struct TilesLayout {
 
 // How the work of T queries of B sequences (one_each: one of each) against up to S own
 // keys and P of the prefix is cut (paged_tiles.hip says what is apart and joined): the
-// numbers of shares with the least estimated time, from what a workgroup's tile takes, what
-// starting and ending one takes, the rounds of workgroups that are resident together,
-// the bytes of K and V at the rate they are read with, and the partials' bytes.  us with the
-// prefix's tiles in n shares (own tiles in one), n taken first:
+// waves to a workgroup and the numbers of shares with the least estimated time, from what a
+// workgroup's tile takes, what starting and ending one takes, the rounds of workgroups that
+// are resident together, the bytes of K and V at the rate they are read with, and the
+// partials' bytes.  us with the prefix's tiles in n shares (own tiles in one), n taken first:
 //   H32/8 D128: 4 sequences behind 500 keys 8 11.4, 2 12.7, 1 16.9;  32 behind 32768, own to 1024 24 59, 16 66, 48 72;
 //   64 behind 16384 12 53, 8 62, 24 59;  256 behind 8192 of H64/8 2 144, 3 155, 4 164;
-//   532 tokens of 8 behind 8192 3 97, 2 120, 4 116, 8 120;  H12 D64, 24 behind 5001 16 16.2, 8 18.6, 24 20.0
-// Eight waves and joined lists where the rows fill them (3500 tokens of 6 sequences behind
-// 32768: 1890; apart in four waves 2020), else four (532 tokens of 8: 97 against 120).
+//   760 tokens of 4 behind 16384 in eight waves 5 221, 4 255, in four 4 227, 2 244;
+//   881 tokens of 24 behind 16384 in eight waves 2 252, in four 264;  H12 D64, 24 behind 5001 16 16.2, 8 18.6, 24 20.0
+// Joined where the rows of a sequence fill eight waves (3500 tokens of 6 sequences behind
+// 32768: 1890, apart in four waves 2020); four waves at D 64 otherwise (1630 tokens of 12
+// behind 8192: 69, in eight 76).
 TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, int P, int D) {
   TilesLayout L{};
   const int G = H / H_kv;
   const long long rows = (long long)T * G;
-  const bool many = rows >= 1024LL * B;
+  const bool many = rows >= 1024LL * B, apart = P > 0 && !many;
   L.joined = P > 0 && many;
-  L.nw = many ? 8 : 4;
-  const long long R = 32 * L.nw;
-  const long long lists = one_each ? B * ((G + R - 1) / R) : rows / R + B;   // tiles of rows of the sequences
-  const long long flat = (rows + R - 1) / R;                                 // and of all tokens
-  const bool apart = P > 0 && !L.joined;
   const int tiles_p = (P + 63) / 64, tiles_o = (S + 63) / 64 + (L.joined ? tiles_p : 0);
-  const float slots = many ? 256.f : 512.f;
-  const float tile = (many ? 1.75f : 1.9f) * (D == 64 ? 0.6f : 1.f), ends = 5.f;   // us
-  const float partial = (float)T * H * D * 8.f / 5e6f;
+  const float ends = 5.f, partial = (float)T * H * D * 8.f / 5e6f;   // us
   const float read = ((apart ? tiles_p : 0.f) + (float)B * tiles_o) * H_kv * D * 256.f / 5e6f;
-  const float units_o = (float)(lists * H_kv), units_p = (float)(flat * H_kv);
-  static const short kShares[] = {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64};
+  static const short kShares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
   float best = INFINITY;
-  for (const int no : kShares) {
-    if (no > 1 && no > tiles_o) break;
-    if (apart && no > 1 && tiles_o / no < 4) break;
-    const float one_o = (tiles_o + no - 1) / no * tile + ends, all_o = units_o * no;
-    for (const int n : kShares) {
-      if (n > 1 && (!apart || n > tiles_p)) break;
-      float t;
-      if (apart) {   // the prefix's workgroups start first; the others run in the slots they leave free, then alone
-        const float one = (tiles_p + n - 1) / n * tile + ends, all = units_p * n, full = std::floor(all / slots);
-        const float rest = all - full * slots, left = all_o - (rest > 0.f ? (slots - rest) * std::floor(one / one_o) : 0.f);
-        t = (full + (rest > 0.f)) * one + (left > 0.f ? std::ceil(left / slots) * one_o : 0.f);
-        t = (t > read ? t : read) + (n + no) * partial;
-      } else {
-        t = std::ceil(all_o / slots) * one_o;
-        t = (t > read ? t : read) + (no > 1 ? no * partial + 3.f : 0.f);
-      }
-      if (t < best) {
-        best = t;
-        L.nsp = apart ? n : 0;
-        L.nso = no;
+  for (const int nw : {4, 8}) {
+    if (nw == 4 ? many : !many && (D == 64 || rows <= 128)) continue;
+    const long long R = 32 * nw;
+    const long long lists = one_each ? B * ((G + R - 1) / R) : rows / R + B;   // tiles of rows of the sequences
+    const long long flat = (rows + R - 1) / R;                                 // and of all tokens
+    const float slots = nw == 8 ? 256.f : 512.f, pair = (nw == 8 ? 1.75f : 2.f) * (D == 64 ? 0.6f : 1.f);
+    const float units_o = (float)(lists * H_kv), units_p = (float)(flat * H_kv);
+    for (const int no : kShares) {
+      if (no > 1 && (no > tiles_o || (apart && tiles_o / no < 4))) break;
+      const float all_o = units_o * no;
+      for (const int n : kShares) {
+        if (n > 1 && (!apart || n > tiles_p)) break;
+        // (a workgroup of four waves alone on its CU is done with a tile sooner)
+        const float tile = nw == 4 && all_o + (apart ? units_p * n : 0.f) <= 256.f ? 0.75f * pair : pair;
+        const float one_o = (tiles_o + no - 1) / no * tile + ends;
+        float t;
+        if (apart) {   // the prefix's workgroups start first; the others run in the slots they leave free, then alone
+          const float one = (tiles_p + n - 1) / n * tile + ends, all = units_p * n, full = std::floor(all / slots);
+          const float rest = all - full * slots, left = all_o - (rest > 0.f ? (slots - rest) * std::floor(one / one_o) : 0.f);
+          t = (full + (rest > 0.f)) * one + (left > 0.f ? std::ceil(left / slots) * one_o : 0.f);
+          t = (t > read ? t : read) + (n + no) * partial;
+        } else {
+          t = std::ceil(all_o / slots) * one_o;
+          t = (t > read ? t : read) + (no > 1 ? no * partial + 3.f : 0.f);
+        }
+        if (t < best) {
+          best = t;
+          L.nw = nw;
+          L.nsp = apart ? n : 0;
+          L.nso = no;
+          L.prefix_items = (int)(L.nsp * flat);
+          L.own_items = (int)(no * lists);
+        }
       }
     }
   }
-  L.prefix_items = (int)(L.nsp * flat);
-  L.own_items = (int)(L.nso * lists);
   const size_t parts = L.nsp + L.nso, all = parts > 1 ? parts * (size_t)T * H : 0;
   L.acc = align256(all * 2 * sizeof(float));
   L.total = L.acc + align256(all * D * sizeof(float));
