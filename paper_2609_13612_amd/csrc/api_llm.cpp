@@ -430,7 +430,7 @@ int qknorm_append(const void* Q, const void* K, const void* V, void* Qr, void* K
 // ---------------------------------------------------------------- new tokens over pages
 struct TilesLayout {
   int nw, nsp, nso, prefix_items, own_items;
-  bool joined;
+  bool joined, by_length;
   size_t ml, acc, total;
 };
 
@@ -454,6 +454,7 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
   const bool many = rows >= 1024LL * B, apart = P > 0 && !many;
   L.joined = P > 0 && many;
   const int tiles_p = (P + 63) / 64, tiles_o = (S + 63) / 64 + (L.joined ? tiles_p : 0);
+  const bool sorted = B > 1 && B <= 64;
   const float ends = 5.f, partial = (float)T * H * D * 8.f / 5e6f;   // us
   const float read = ((apart ? tiles_p : 0.f) + (float)B * tiles_o) * H_kv * D * 256.f / 5e6f;
   static const short kShares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
@@ -481,7 +482,11 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
           t = (t > read ? t : read) + (n + no) * partial;
         } else {
           t = std::ceil(all_o / slots) * one_o;
-          t = (t > read ? t : read) + (no > 1 ? no * partial + 3.f : 0.f);
+          if (all_o > slots && sorted) {   // the longest first: the end is filled (a quarter of the work is taken to be missing)
+            t = 0.75f * all_o / slots * one_o + 0.25f * one_o;
+            t = t > one_o ? t : one_o;
+          }
+          t = (t > read ? t : read) + (no > 1 ? 2.f * no * partial + 3.f : 0.f);
         }
         if (t < best) {
           best = t;
@@ -494,6 +499,7 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
       }
     }
   }
+  L.by_length = sorted && (long long)L.own_items * H_kv > (L.nw == 8 ? 256 : 512);
   const size_t parts = L.nsp + L.nso, all = parts > 1 ? parts * (size_t)T * H : 0;
   L.acc = align256(all * 2 * sizeof(float));
   L.total = L.acc + align256(all * D * sizeof(float));
@@ -723,6 +729,7 @@ int attnfuse_fwd_paged(const void* Q, const void* K_pages, const void* V_pages, 
   p.joined = L.joined;
   p.nsp = L.nsp; p.nso = L.nso; p.parts = L.nsp + L.nso;
   p.prefix_items = L.prefix_items; p.own_items = L.own_items;
+  p.by_length = cache_lens && L.by_length;
   p.scale = softmax_scale;
   return map_launch(af::launch_paged_tiles(D, p, L.nw, static_cast<hipStream_t>(stream)));
 }

@@ -172,6 +172,7 @@ struct TilesParams {
   int nsp, nso;           // shares of the prefix's tiles (0: joined, or no prefix), of a sequence's
   int parts;              // nsp + nso; 1: results are written at once
   int prefix_items, own_items;   // workgroups per K/V head over the prefix, over the sequences' lists
+  bool by_length;         // the longest sequences' workgroups first (B <= 64, lens given)
   float scale;
 };
 

@@ -52,10 +52,30 @@ __device__ __forceinline__ Sequence sequence_at(const TilesParams& p, int b) {
   return s;
 }
 
-// The sequence of a slot (a tile of rows) and the tile's first row.  Sequence b has the
-// slots from first_b G / rows + b on, which leaves it room for a tile that is not full; its
-// number is that of the sequences that start at or before the slot.  -1: no sequence's.
+// The sequence of a slot (a tile of rows) and the tile's first row.  Unless they are sorted
+// by length, sequence b has the slots from first_b G / rows + b on, which leaves it room for a
+// tile that is not full; its number is that of the sequences that start at or before the
+// slot.  -1: no sequence's.
 __device__ __forceinline__ int sequence_of(const TilesParams& p, int slot, int rows, int lane, int& r0) {
+  if (p.by_length) {   // (up to 64 sequences with lengths) the longest one's slots first, so that short ones fill the end
+    int count = 0, key = -1;
+    if (lane < p.B) {
+      int n = 1;
+      if (p.starts) {
+        const int first = min(max(p.starts[lane], 0), p.T);
+        n = min(max(p.starts[lane + 1], first), p.T) - first;
+      }
+      count = (n * p.G + rows - 1) / rows;
+      key = min(max(p.lens[lane], 0), p.S) * 64 + (63 - lane);   // (S <= 2^20)
+    }
+    int before = 0;
+    for (int j = 0; j < p.B; ++j) before += __builtin_amdgcn_readlane(key, j) > key ? __builtin_amdgcn_readlane(count, j) : 0;
+    const unsigned long long mine = __ballot(before <= slot && slot < before + count);
+    if (!mine) return -1;
+    const int b = __ffsll(mine) - 1;
+    r0 = (slot - __builtin_amdgcn_readlane(before, b)) * rows;
+    return b;
+  }
   if (!p.starts) {
     const int per = (p.G + rows - 1) / rows;
     r0 = slot % per * rows;
