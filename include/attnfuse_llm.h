@@ -330,11 +330,11 @@ size_t attnfuse_fwd_paged_workspace_bytes(int T, int B, int H, int H_kv, int D, 
  *   max_pages * page_size <= 2^20; H <= 16384, a multiple of H_kv
  *
  * A NaN in a query, or in a key or value that it sees, comes out as NaN.  A NaN or an
- * infinity in the value of a later own key of the same sequence reaches queries that do
- * not see it yet, where both lie in a 64-key tile that some query in between sees (its
- * weight is 0); what lies in pages past a sequence's length, and in places that are no
- * key, is never used.  Keys are shared out among workgroups by sizes alone (T, B and the
- * tables' widths): with others a result is the same to the rounding of fp32 sums.
+ * infinity in the value of one of the sequence's newest n_b own keys may reach queries of
+ * the call that do not see it yet (with weight 0); what lies in places past a sequence's
+ * length or the prefix's, and in pages of neither, is never used.  The keys are shared out by sizes alone (T, B and the tables' widths)
+ * and the same call gives the same bits; in another batch a sequence's result is the same to
+ * the rounding of its weights and sums.
  */
 int attnfuse_fwd_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table, const int* q_starts,
                        const int* cache_lens, const int* prefix_table, const int* prefix_len, void* O, float* LSE,

@@ -471,6 +471,7 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
       const float all_o = units_o * no;
       for (const int n : kShares) {
         if (n > 1 && (!apart || n > tiles_p)) break;
+        if ((n > 1 || no > 1) && all_o + units_p * n > 1e6f) break;   // (nothing to gain, and grids stay inside their type)
         // (a workgroup of four waves alone on its CU is done with a tile sooner)
         const float tile = nw == 4 && all_o + (apart ? units_p * n : 0.f) <= 256.f ? 0.75f * pair : pair;
         const float one_o = (tiles_o + no - 1) / no * tile + ends;
@@ -509,7 +510,7 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
 bool tiles_sizes(int T, int B, int H, int H_kv, long long S, long long P, int D) {
   return T >= 1 && T <= kMaxS && B >= 1 && B < (1 << 16) && H >= 1 && H <= kMaxHeads && H_kv >= 1 && H % H_kv == 0 && S >= 1 &&
          S <= kMaxS && P >= 0 && P <= kMaxS && D >= 2 && D % 2 == 0 && (long long)T * H <= (1 << 30) &&
-         ((long long)T * (H / H_kv) / 128 + B) * H_kv * 1024 < (1LL << 31);
+         2 * ((long long)T * (H / H_kv) / 128 + B + 1) * H_kv < (1LL << 31);   // workgroups, with one share of each list
 }
 
 }  // namespace

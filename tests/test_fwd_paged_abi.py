@@ -43,6 +43,8 @@ def test_workspace_bytes():
         n = f(T, B, H, Hkv, 128, own, ahead)
         parts = n // (T * H * (128 + 2) * 4)
         assert parts >= 2 and n - parts * T * H * (128 + 2) * 4 < 512
+    assert f(65535, 65535, 64, 64, 128, 64, 64) > 0 and f(1 << 20, 1, 1024, 8, 128, 1 << 20, 0) == 0   # (results are written at once)
+    assert f(1 << 20, 65535, 1024, 1024, 128, 64, 0) == 0 and f(1 << 20, 4, 1024, 1, 128, 64, 1 << 20) == 0
     assert api.attnfuse_fwd_paged_workspace_bytes(4, 4, 32, 8, 128, 64, 512) == f(4, 4, 32, 8, 128, 64, 512)
 
 
