@@ -11,7 +11,8 @@ D = NORM["D"]
 
 
 def ints(*x):
-    return (ctypes.c_int * len(x))(*x)
+    """A C array of ints that names itself by its values (the tests' names)."""
+    return type("Ints", (ctypes.c_int * len(x),), {"__repr__": lambda self: "-".join(map(str, self))})(*x)
 
 
 def with_axes(base, norm=True):
