@@ -453,7 +453,7 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
   const long long rows = (long long)T * G;
   const bool many = rows >= 1024LL * B, apart = P > 0 && !many;
   L.joined = P > 0 && many;
-  const int tiles_p = (P + 63) / 64, tiles_o = (S + 63) / 64 + (L.joined ? tiles_p : 0);
+  const int tiles_p = (P + 63) / 64, tiles_s = (S + 63) / 64, tiles_o = tiles_s + (L.joined ? tiles_p : 0);
   const bool sorted = B > 1 && B <= 64;
   const float ends = 5.f, partial = (float)T * H * D * 8.f / 5e6f;   // us
   const float read = ((apart ? tiles_p : 0.f) + (float)B * tiles_o) * H_kv * D * 256.f / 5e6f;
@@ -483,9 +483,9 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
           t = (t > read ? t : read) + (n + no) * partial;
         } else {
           t = std::ceil(all_o / slots) * one_o;
-          if (all_o > slots && sorted) {   // the longest first: the end is filled (a quarter of the work is taken to be missing)
-            t = 0.75f * all_o / slots * one_o + 0.25f * one_o;
-            t = t > one_o ? t : one_o;
+          if (all_o > slots && sorted) {   // the longest first: as far as lengths differ, the end is filled (a quarter of
+            const float fill = 0.75f * all_o / slots * one_o + 0.25f * one_o;          // the own keys is taken to be missing)
+            t += ((fill > one_o ? fill : one_o) - t) * tiles_s / tiles_o;
           }
           t = (t > read ? t : read) + (no > 1 ? 2.f * no * partial + 3.f : 0.f);
         }
