@@ -1,7 +1,8 @@
 /*
  * attnfuse_llm.h -- operators of language models around the attention of
- * attnfuse.h, in the same library: the norm and rotation of queries and keys,
- * paged caches, and windows whose first tokens stay visible (sinks).
+ * attnfuse.h, in the same library: the norm and rotation of queries and keys, at
+ * positions of one axis or several, paged caches, prefixes that a batch shares, and
+ * windows whose first tokens stay visible (sinks).
  *
  * The conventions of attnfuse.h hold (ownership, streams, RoPE tables, error
  * codes, validation before any HIP call), with two additions:
