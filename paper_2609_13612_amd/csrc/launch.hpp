@@ -92,7 +92,7 @@ struct RopeParams {
   const float2* table;
 };
 
-// Norm and rotation of query and key rows (qknorm.hip).  Index 0 is q, 1 k, 2 v;
+// Norm and rotation of query and key rows (qknorm_kernel.hpp).  Index 0 is q, 1 k, 2 v;
 // strides in elements: batch (of a cache: page), head, position.
 // UNTURN: the inverse rotation alone (y with strides), for positions of several axes.
 enum { QKNORM_FWD = 0, QKNORM_BWD = 1, QKNORM_APPEND = 2, QKNORM_UNTURN = 3 };

@@ -26,7 +26,8 @@
 // gathers its 8 pairs' angles from as many rows of the table.  Such a call may leave
 // the norm out (r = 1, no weights): its backward is the inverse rotation of dout alone.
 // us of B1 H32/8 S8192 D128 bf16 in replayed graphs, three axes and one: forward 28.3 and
-// 27.0, backward 52.4 and 48.5 (three waves per SIMD instead of four), without norm 27 each.
+// 27.0, backward 52.4 and 48.5 (a thread gathers its angles for two heads there, for four in
+// the forward; held to 128 registers for a fourth wave per SIMD, 53.5), without norm 27 each.
 #pragma once
 #include <type_traits>
 

@@ -363,6 +363,25 @@ def test_captured_step_replays():
         assert all(torch.equal(a, b) for a, b in zip(got, want)), f"replay {i}"
 
 
+def test_longest_sequence():
+    """S = 2^20: sampled rows against the definition, forward and backward."""
+    need_gpu()
+    announce("axes S=2^20")
+    g = torch.Generator().manual_seed(18)
+    S, variant = 1 << 20, ("neox", 500000.0, (10, 11, 11), "turns", "shared")
+    q, w = rows((1, 2, S, 64), BF, g, "bshd"), weights(64, "rows", BF, g)[0]
+    do, pos = rows((1, 2, S, 64), BF, g, "bhsd"), positions(3, (1, S), g)
+    cfg = cfg_of(*variant, True, pos.cuda())
+    out = api.attnfuse_qknorm_rope(q, None, w, **cfg)[0]
+    dq = api.attnfuse_qknorm_rope_bwd(q, None, do, None, w, **cfg)[0]
+    at = torch.cat((torch.arange(5), torch.randint(0, S, (300,), generator=g), torch.arange(S - 5, S)))
+    take = lambda t: t[:, :, at.cuda()].cpu()   # noqa: E731
+    want, size = axes_fwd(take(q), w, pos[:, :, None][..., at], variant, True, EPS)
+    assert_within(take(out), want, half_step(BF) * want.abs() + 64 * U32 * size, "q'")
+    dx, _, dsize, _ = axes_bwd(take(q), w, take(do), pos[:, :, None][..., at], variant, True, EPS)
+    assert_within(take(dq), dx, half_step(BF) * dx.abs() + 128 * U32 * dsize, "dq")
+
+
 def test_on_another_stream():
     need_gpu()
     announce("axes stream")

@@ -340,6 +340,53 @@ def test_offsets_past_32_bits():
     check(o, lse, batch(q, ks, vs, small[0], [0, 3, 43], lens, small[1][0], P), "far")
 
 
+def test_pages_named_twice():
+    """A page may be in a table twice, in several sequences' and in the prefix's."""
+    need_gpu()
+    announce("fwd_paged shared pages")
+    g = torch.Generator().manual_seed(15)
+    q, k, v, table, starts, prefix = setup([20, 1, 5], [60, 64, 33], 8, 2, 64, 16, 200, g)
+    prefix[7] = prefix[2]
+    table[1] = table[0]
+    table[2, 0], table[2, 1] = prefix[0], prefix[0]
+    o, lse = api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32([60, 64, 33]), prefix_table=prefix, prefix_len=i32([199]))
+    check(o, lse, batch(q, k, v, table, starts, [60, 64, 33], prefix, 199), "shared pages")
+
+
+@pytest.mark.parametrize("ahead", [True, False])
+def test_longest_lists(ahead):
+    """2^20 keys of a prefix, or of a sequence."""
+    need_gpu()
+    announce(f"fwd_paged 2^20 keys ahead={ahead}")
+    g = torch.Generator().manual_seed(16)
+    n, page = 1 << 20, 256
+    q, k, v, table, starts, prefix = setup([3, 1], [n, 7] if not ahead else [10, 7], 2, 1, 64, page, n if ahead else 0, g)
+    lens = [n, 7] if not ahead else [10, 7]
+    kw = dict(prefix_table=prefix, prefix_len=i32([n])) if ahead else {}
+    o, lse = api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32(lens), **kw)
+    check(o, lse, batch(q, k, v, table, starts, lens, prefix, n if ahead else 0), "2^20 keys")
+    if ahead:
+        with pytest.raises(api.AttnFuseError):
+            api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32(lens), prefix_table=torch.cat((prefix, prefix[:1])))
+
+
+def test_many_tokens():
+    """Tokens by the ten thousands, of many sequences of any length: sampled against the definition."""
+    need_gpu()
+    announce("fwd_paged many tokens")
+    g = torch.Generator().manual_seed(17)
+    counts = [int(x) for x in torch.randint(0, 90, (700,), generator=g)]
+    lens = [c + int(x) for c, x in zip(counts, torch.randint(0, 60, (700,), generator=g))]
+    q, k, v, table, starts, prefix = setup(counts, lens, 4, 2, 64, 16, 90, g, pad=5)
+    o, lse = api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32(lens), prefix_table=prefix, prefix_len=i32([90]))
+    pick = [0, 1, 63, 64, 65, 127, 128, 350, 640, 698, 699]
+    kc, vc = k.cpu(), v.cpu()
+    for b in pick:
+        at = [starts[b], starts[b + 1]]
+        refs = batch(q, kc, vc, table[b:b + 1], at, [lens[b]], prefix, 90)
+        check(o, lse, refs, f"sequence {b}")
+
+
 def test_append_prompts_decode():
     """A server's run: a prefix of patches and text at positions of three axes is appended once, questions of some tokens are
     appended and attend, and then tokens one at a time."""
