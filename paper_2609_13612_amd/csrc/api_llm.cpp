@@ -431,7 +431,7 @@ int qknorm_append(const void* Q, const void* K, const void* V, void* Qr, void* K
 struct TilesLayout {
   int nw, nsp, nso, prefix_items, own_items;
   bool joined, by_length;
-  size_t ml, acc, total;
+  size_t acc, total;   // workspace: (max, sum) pairs, from acc on the accumulators
 };
 
 // How the work of T queries of B sequences (one_each: one of each) against up to S own

@@ -180,6 +180,12 @@ __device__ __forceinline__ u32x4 ld16(const void* p) {
   return *reinterpret_cast<const u32x4*>(p);
 }
 __device__ __forceinline__ void st16(void* p, u32x4 v) { *reinterpret_cast<u32x4*>(p) = v; }
+// A value that no kernel writes while this one runs, at a wave-uniform address: a
+// scalar load.  (A vector load would be waited for with vmcnt, behind every load of
+// the tiles in flight.)
+__device__ __forceinline__ int uniform_load(const int* p) {
+  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
+}
 
 // gfx950 LDS transpose read (ds_read_b64_tr_b16).  Within each group of 16
 // lanes the sixteen 8-byte chunks the lanes address form a 4 x 16 matrix of

@@ -55,13 +55,6 @@ struct PagedCfg {
 // The bits below bit n.
 __device__ __forceinline__ uint32_t below(int n) { return n <= 0 ? 0u : n >= 32 ? ~0u : (1u << n) - 1; }
 
-// A value that no kernel writes while this one runs, at a wave-uniform address: a
-// scalar load.  (A vector load would be waited for with vmcnt, behind every load of
-// the tiles in flight.)
-__device__ __forceinline__ int uniform_load(const int* p) {
-  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
-}
-
 // The visible tiles of a sequence with L keys: tiles [0, ns), then [t0, t0 + n - ns).
 struct Visible {
   int L, lo, sinks, ns, t0, n;

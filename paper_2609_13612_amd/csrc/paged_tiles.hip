@@ -19,11 +19,11 @@
 // lengths, which are known on the device alone.
 //
 // Inside a workgroup the tiles go straight from the pages to LDS (attn_tiles.hpp), one
-// 16-key unit of a page at a time, whose address is wave-uniform; the page numbers are scalar
-// loads one tile ahead.  The loop is the forward's: while the products S^T = K Q^T of the
+// 16-key unit of a page at a time, whose address is wave-uniform: lanes read the page numbers
+// two tiles ahead, form an address each and hand them out as scalars.  The loop is the forward's: while the products S^T = K Q^T of the
 // next tile run, this tile's scores become probabilities, and its P V runs while the next tile's
 // scores are masked and reduced.  Q and K meet in bf16 exactly; P is rounded to bf16
-// (2^-9 of each weight; the bf16 O is rounded as much), sums, maxima and O stay fp32.
+// (2^-8 of each weight at most; the bf16 O is rounded as much), sums, maxima and O stay fp32.
 //
 // What lies in places that are no key of any row of the workgroup may be anything: scores
 // are replaced and rows of V cleared in LDS after they landed.
@@ -41,11 +41,6 @@
 
 namespace af {
 
-// A value that no kernel writes while this one runs, at a wave-uniform address.
-__device__ __forceinline__ int scalar_load(const int* p) {
-  return *(const __attribute__((address_space(4))) int*)(uintptr_t)p;
-}
-
 // The queries of a sequence: tokens [first, first + n), and its own keys.
 struct Sequence {
   int b, first, n, keys;
@@ -54,10 +49,10 @@ struct Sequence {
 __device__ __forceinline__ Sequence sequence_at(const TilesParams& p, int b) {
   Sequence s{b, b, 1, 0};
   if (p.starts) {
-    s.first = min(max(scalar_load(p.starts + b), 0), p.T);
-    s.n = min(max(scalar_load(p.starts + b + 1), s.first), p.T) - s.first;
+    s.first = min(max(uniform_load(p.starts + b), 0), p.T);
+    s.n = min(max(uniform_load(p.starts + b + 1), s.first), p.T) - s.first;
   }
-  s.keys = p.lens ? min(max(scalar_load(p.lens + b), 0), p.S) : p.S;
+  s.keys = p.lens ? min(max(uniform_load(p.lens + b), 0), p.S) : p.S;
   return s;
 }
 
@@ -150,7 +145,7 @@ void paged_tiles_kernel(TilesParams p) {
     for (int j = 0; j < 3; ++j) e[j] = entry_of(prefix_list, BN * (share + j * ns));
   }
   if (p.prefix_pages > 0 && (prefix_list || p.joined))
-    np = p.prefix_len ? min(max(scalar_load(p.prefix_len), 0), p.P) : p.P;
+    np = p.prefix_len ? min(max(uniform_load(p.prefix_len), 0), p.P) : p.P;
   int own = 0;                                             // own keys that any row of the workgroup sees
   if (prefix_list) {
     nrows = p.T * p.G;

@@ -387,6 +387,36 @@ def test_many_tokens():
         check(o, lse, refs, f"sequence {b}")
 
 
+@pytest.mark.parametrize("P", [0, 100])
+@pytest.mark.parametrize("B", [2, 40, 64])
+def test_longest_first(B, P):
+    """More workgroups than run at once, of up to 64 sequences: they go by length, with ties, empty ones and lengths beyond
+    the table among them.  The lengths alone decide, whatever rows there are."""
+    need_gpu()
+    announce(f"fwd_paged longest first B={B} P={P}")
+    g = torch.Generator().manual_seed(19 + B)
+    H = 64 if B > 2 else 400
+    counts = [int(x) for x in torch.randint(0, 30, (B,), generator=g)]
+    counts[0] = 140
+    lens = [c + int(x) for c, x in zip(counts, torch.randint(0, 200, (B,), generator=g))]
+    lens[1] = lens[0] = 300
+    if B > 2:
+        lens[5], lens[7], counts[9] = 0, -3, 0
+    q, k, v, table, starts, prefix = setup(counts, lens, H, H, 64, 16, P, g, pad=3)
+    lens[-1] = 9999
+    kw = dict(prefix_table=prefix, prefix_len=i32([P])) if P else {}
+    o, lse = api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32(lens), **kw)
+    few = slice(0, 3)   # heads: the reference of three of them
+    refs = batch(q[:, few], k[:, few], v[:, few], table, starts, lens, prefix, P)
+    check(o[:, few], lse[:, few], refs, "prompts")
+    last = slice(H - 2, H)
+    check(o[:, last], lse[:, last], batch(q[:, last], k[:, last], v[:, last], table, starts, lens, prefix, P), "prompts, last heads")
+    if P:
+        o, lse = api.attnfuse_decode_paged(q[:B].contiguous(), k, v, table, i32(lens), **kw)
+        refs = batch(q[:B, few], k[:, few], v[:, few], table, list(range(B + 1)), lens, prefix, P)
+        check(o[:, few], lse[:, few], refs, "decode")
+
+
 def test_append_prompts_decode():
     """A server's run: a prefix of patches and text at positions of three axes is appended once, questions of some tokens are
     appended and attend, and then tokens one at a time."""
