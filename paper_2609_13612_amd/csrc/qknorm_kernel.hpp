@@ -102,7 +102,16 @@ template <int D, int ROPE>
 __device__ __forceinline__ uint32_t axes_of(const QkNormParams& p, int c) {
   // Values, not places, are chosen by lane here and below: a place that differs by lane
   // would go through memory (one token's append took 7.9 us instead of 3.9).
-  const u32x4 axis = {p.axis[0], p.axis[1], p.axis[2], p.axis[3]};
+  // The words are values of their own before a lane chooses: the compiler makes one load of
+  // arguments out of a choice between two, at the index of the wave's first lane (pairs 16 to
+  // 31 of D 64 then took the axes of pairs 0 to 15).
+  u32x4 axis;
+#pragma unroll
+  for (int w = 0; w < D / 32; ++w) {
+    uint32_t x = p.axis[w];
+    asm("" : "+s"(x));
+    axis[w] = x;
+  }
   auto word = [&](int w) {
     const uint32_t lo = w & 1 ? axis.y : axis.x;
     if constexpr (D == 64) return lo;

@@ -256,6 +256,17 @@ def test_append(monkeypatch, T, H, Hkv, D, page, dtype, rope, wkind, norm, secti
     assert torch.equal(vc, v0)
 
 
+@pytest.mark.parametrize("T", [2, 90])
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("order", ["blocks", "turns"])
+@pytest.mark.parametrize("rope", ["neox", "interleaved"])
+@pytest.mark.parametrize("D,sections", [(64, (16, 16)), (64, (5, 27)), (64, (8, 12, 12)), (64, (8, 8, 8, 8)), (128, (32, 32)),
+                                        (128, (7, 28, 29)), (128, (16, 16, 16, 16))], ids=lambda x: str(x).replace(" ", ""))
+def test_append_every_pair(monkeypatch, D, sections, rope, order, dtype, T):
+    """Every pair turns by its own axis's position, in the head sizes, orders and types of the append."""
+    test_append(monkeypatch, T, 12, 4, D, 32, dtype, rope, "rows", True, sections, order, "own", "phsd", True)
+
+
 @pytest.mark.parametrize("norm", [True, False])
 def test_native_and_python_marshalling_agree(monkeypatch, norm):
     need_gpu()
