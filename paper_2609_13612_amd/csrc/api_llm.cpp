@@ -440,10 +440,10 @@ struct TilesLayout {
 // workgroup's tile takes, what starting and ending one takes, the rounds of workgroups that
 // are resident together, the bytes of K and V at the rate they are read with, and the
 // partials' bytes.  us with the prefix's tiles in n shares (own tiles in one), n taken first:
-//   H32/8 D128: 4 sequences behind 500 keys 8 11.4, 2 12.7, 1 16.9;  32 behind 32768, own to 1024 24 59, 16 66, 48 72;
-//   64 behind 16384 12 53, 8 62, 24 59;  256 behind 8192 of H64/8 2 144, 3 155, 4 164;
+//   H32/8 D128: 4 sequences behind 500 keys 4 10.9, 2 10.9, 1 12.1;  32 behind 32768, own to 1024 32 58, 24 59, 16 67, 48 65;
+//   64 behind 16384 16 49, 12 53, 20 53, 8 61;  256 behind 8192 of H64/8 2 130, 3 141, 4 156;
 //   760 tokens of 4 behind 16384 in eight waves 5 221, 4 255, in four 4 227, 2 244;
-//   881 tokens of 24 behind 16384 in eight waves 2 252, in four 264;  H12 D64, 24 behind 5001 16 16.2, 8 18.6, 24 20.0
+//   881 tokens of 24 behind 16384 in eight waves 2 252, in four 264;  H12 D64, 24 behind 5001 8 14.7, 16 15.5, 24 17.6
 // Joined where the rows of a sequence fill eight waves (3500 tokens of 6 sequences behind
 // 32768: 1890, apart in four waves 2020); four waves at D 64 otherwise (1630 tokens of 12
 // behind 8192: 69, in eight 76).
@@ -455,16 +455,22 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
   L.joined = P > 0 && many;
   const int tiles_p = (P + 63) / 64, tiles_s = (S + 63) / 64, tiles_o = tiles_s + (L.joined ? tiles_p : 0);
   const bool sorted = B > 1 && B <= 64;
-  const float ends = 5.f, partial = (float)T * H * D * 8.f / 5e6f;   // us
-  const float read = ((apart ? tiles_p : 0.f) + (float)B * tiles_o) * H_kv * D * 256.f / 5e6f;
+  const float partial = (float)T * H * D * 8.f / 5e6f;   // us
+  const float read_o = (float)B * tiles_s * H_kv * D * 256.f / 5e6f, read = read_o + tiles_p * H_kv * D * 256.f / 5e6f;
   static const short kShares[] = {1, 2, 3, 4, 5, 6, 8, 10, 12, 16, 20, 24, 32, 48, 64};
+  // Work and reading beside each other: the longer; with one token each, and a quarter of the
+  // shorter, which does not overlap.
+  const bool few = one_each && G <= 32;
+  const auto both = [=](float a, float b) { return a > b ? a + (few ? 0.25f * b : 0.f) : b + (few ? 0.25f * a : 0.f); };
   float best = INFINITY;
   for (const int nw : {4, 8}) {
     if (nw == 4 ? many : !many && (D == 64 || rows <= 128)) continue;
     const long long R = 32 * nw;
     const long long lists = one_each ? B * ((G + R - 1) / R) : rows / R + B;   // tiles of rows of the sequences
     const long long flat = (rows + R - 1) / R;                                 // and of all tokens
-    const float slots = nw == 8 ? 256.f : 512.f, pair = (nw == 8 ? 1.75f : 2.f) * (D == 64 ? 0.6f : 1.f);
+    const bool few_o = nw == 4 && few, few_p = few_o && rows <= 32;           // lists of up to 32 rows
+    const float slots = nw == 8 ? 256.f : 512.f, narrow = D == 64 ? 0.6f : 1.f, pair = (nw == 8 ? 1.75f : 2.f) * narrow;
+    const float beside_p = few_o && !few_p ? 0.5f * read_o / flat : 0.f;   // what few rows' lists read before the prefix's go on
     const float units_o = (float)(lists * H_kv), units_p = (float)(flat * H_kv);
     for (const int no : kShares) {
       if (no > 1 && (no > tiles_o || (apart && tiles_o / no < 4))) break;
@@ -472,22 +478,24 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
       for (const int n : kShares) {
         if (n > 1 && (!apart || n > tiles_p)) break;
         if ((n > 1 || no > 1) && all_o + units_p * n > 1e6f) break;   // (nothing to gain, and grids stay inside their type)
-        // (a workgroup of four waves alone on its CU is done with a tile sooner)
-        const float tile = nw == 4 && all_o + (apart ? units_p * n : 0.f) <= 256.f ? 0.75f * pair : pair;
-        const float one_o = (tiles_o + no - 1) / no * tile + ends;
+        // (a workgroup of four waves alone on its CU, or beside short lists, is done with a tile sooner)
+        const float alone = nw == 4 && (few ? 0.f : all_o) + (apart ? units_p * n : 0.f) <= 256.f ? 0.75f : 1.f, tile = alone * pair;
+        const float one_o = (tiles_o + no - 1) / no * (few_o ? 0.55f * narrow : tile) + (few_o ? 6.5f : 5.f);
         float t;
         if (apart) {   // the prefix's workgroups start first; the others run in the slots they leave free, then alone
-          const float one = (tiles_p + n - 1) / n * tile + ends, all = units_p * n, full = std::floor(all / slots);
-          const float rest = all - full * slots, left = all_o - (rest > 0.f ? (slots - rest) * std::floor(one / one_o) : 0.f);
+          const float one = (tiles_p + n - 1) / n * (few_p ? 0.55f * alone * narrow : tile) + (few_p ? 6.5f : 5.f) + beside_p;
+          const float all = units_p * n, full = std::floor(all / slots);
+          const float rest = all - full * slots;
+          const float left = all_o - (rest > 0.f ? (slots - rest) * std::floor(one / one_o) : 0.f);
           t = (full + (rest > 0.f)) * one + (left > 0.f ? std::ceil(left / slots) * one_o : 0.f);
-          t = (t > read ? t : read) + (n + no) * partial;
+          t = both(t, read) + (n + no) * partial;
         } else {
           t = std::ceil(all_o / slots) * one_o;
           if (all_o > slots && sorted) {   // the longest first: as far as lengths differ, the end is filled (a quarter of
             const float fill = 0.75f * all_o / slots * one_o + 0.25f * one_o;          // the own keys is taken to be missing)
             t += ((fill > one_o ? fill : one_o) - t) * tiles_s / tiles_o;
           }
-          t = (t > read ? t : read) + (no > 1 ? 2.f * no * partial + 3.f : 0.f);
+          t = both(t, read) + (no > 1 ? 2.f * no * partial + 3.f : 0.f);
         }
         if (t < best) {
           best = t;

@@ -16,7 +16,8 @@
 //     rows of a sequence walk the prefix's tiles and then their own: fewer partials, none
 //     with one share.
 // The tiles of a list are dealt out in turn to ns shares, so shares are even whatever the
-// lengths, which are known on the device alone.
+// lengths, which are known on the device alone.  In calls of one token each, lists of up to
+// 32 rows have a loop of their own (few_rows).
 //
 // Inside a workgroup the tiles go straight from the pages to LDS (attn_tiles.hpp), one
 // 16-key unit of a page at a time, whose address is wave-uniform: lanes read the page numbers
@@ -30,8 +31,8 @@
 //
 // Bound by reading K and V where few rows meet them, by the matrix units from about 220
 // rows of a K/V head on.  Measured (D 128): 32 sequences' tokens behind 32768 shared keys,
-// own keys to 1024, H 32 of 8, 59 us, of which the join 6: 218 MB, 4.1 TB/s in the first
-// kernel (own keys alone, 64 sequences of 2000 to 8200, 5.1 TB/s).  3500 tokens of 6
+// own keys to 1024, H 32 of 8, 57 to 58 us, of which the join 7: 218 MB, 4.3 TB/s in the
+// first kernel.  3500 tokens of 6
 // sequences behind 32768: 1913 us, 1.02 PFLOP/s, 85 % of a large library product's rate; a
 // tile of a workgroup of eight waves takes 1.75 us, of four waves, two of them on a CU, 1.9.
 // Copies three tiles ahead instead of one (four stages, 32- or 64-key tiles) were nowhere
@@ -97,7 +98,217 @@ __device__ __forceinline__ int sequence_of(const TilesParams& p, int slot, int r
   return count - 1;
 }
 
-template <int D, int NW>
+// All but the newest N copies of this wave have landed; this wave's LDS reads are done.
+template <int N>
+__device__ __forceinline__ void async_wait_but() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(N) : "memory"); }
+__device__ __forceinline__ void lds_wait() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+// What a partial with maximum m counts in a sum of maximum M.  Scores that are all NaN
+// leave m at -inf, as no visible key does, and NaN in the sums: those are added, times
+// 0, and stay NaN.
+__device__ __forceinline__ float share_weight(float m, float M) { return m == -INFINITY ? 0.f : fast_exp2(m - M); }
+
+// A list of up to 32 rows (one token of a sequence and its heads; a prefix under a few
+// sequences): the rows are one wave's, so the four waves take turns at its half tiles of 32
+// keys, each with K and V of its own in LDS and no barrier before the end.  K of a wave's
+// next half tile is on its way from this one's scores on, V from its products on.  Bound by
+// the reads' latency.  Against the other loop: 8 sequences behind 4096 keys, H32/8 D128,
+// 13.3 us to 15.5; 64 with 8128 own keys (H32/8 D128) 245 to 265; 189 sequences of up
+// to 13 own keys behind 23, H16 D128, 34 to 44.
+template <int D, class Place, class Entries>
+__device__ __forceinline__ void few_rows(const TilesParams& p, uint16_t* smem, Place place_of, Entries entries16, int entries,
+                                         int nt, int g, int nrows, int first, int shift_keys, int part, int lane, int wave) {
+  using AT = AsyncTile<D, 1, 32>;
+  constexpr int KS = D / 16, MT = D / 32, RPG = AT::RPG, CPR = D / 8, NI = AT::NI;
+  const int lq = lane & 31, lg = lane >> 5;
+  const AT at(lane, 0);
+  uint16_t* kw = smem + wave * 2 * AT::ELEMS;
+  uint16_t* vw = kw + AT::ELEMS;
+  __shared__ float xml[2][4][32];                          // the waves' maximum and sum of every row
+
+  const int row = min(lq, nrows - 1), token = row / p.G;
+  const size_t at_row = (size_t)(first + token) * p.H + g * p.G + (row - token * p.G);
+  const int lim = shift_keys + token;                      // the last own key that this lane's row sees; the least: shift_keys
+  u32x4 qreg[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) qreg[s] = ld16(static_cast<const uint16_t*>(p.q) + at_row * D + 16 * s + 8 * lg);
+
+  // Lanes 0, 1: K's units of a half tile, 2, 3: V's.
+  const int lane_unit = lane & 1;
+  const bool lane_v = lane & 2;
+  const uint16_t* lane_base = static_cast<const uint16_t*>(lane_v ? p.v : p.k) + g * (lane_v ? p.vs[1] : p.ks[1]);
+  const long long lane_page = lane_v ? p.vs[0] : p.ks[0];
+  const uint32_t lane_place = (uint32_t)(lane_v ? p.vs[2] : p.ks[2]);
+  const uint32_t voff_k = (uint32_t)(lane / CPR) * (uint32_t)(2 * p.ks[2]) + at.col;
+  const uint32_t voff_v = (uint32_t)(lane / CPR) * (uint32_t)(2 * p.vs[2]) + at.col;
+  struct Half {
+    int n0, end;
+    bool prefix;
+    uint32_t valid;
+    uint64_t base;
+  };
+  int batch = 0;
+  auto half_at = [&](int h) {
+    const int i = h >> 1;
+    if (i >> 4 != batch) {
+      batch = i >> 4;
+      entries = entries16(16 * batch);
+    }
+    const int e = __shfl(entries, 4 * (i & 15) + 2 * (h & 1) + lane_unit);
+    const auto t = place_of(i);
+    Half x{t.n0 + 32 * (h & 1), t.end, t.prefix, 0, 0};
+    const bool ok = (unsigned)e < (unsigned)p.num_pages;
+    x.valid = (uint32_t)__ballot(ok) & 3u;
+    const uint32_t place = (uint32_t)(x.n0 + 16 * lane_unit) & ((1u << p.page_shift) - 1);
+    x.base = (uint64_t)(lane_base + (ok ? e : 0) * lane_page + (uint64_t)place * lane_place);
+    return x;
+  };
+  auto load = [&](const Half& x, int lane0, long long place, uint32_t voff, uint16_t* dst) {
+    const uint32_t lds = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) uint16_t*)dst;
+#pragma unroll
+    for (int j = 0; j < NI; ++j) {
+      const uint32_t lo = __builtin_amdgcn_readlane((uint32_t)x.base, lane0 + j * RPG / 16);
+      const uint32_t hi = __builtin_amdgcn_readlane((uint32_t)(x.base >> 32), lane0 + j * RPG / 16);
+      const uint64_t base = ((uint64_t)hi << 32 | lo) + (uint64_t)(2 * (j * RPG % 16)) * (uint64_t)place;
+      async_copy16((const void*)base, voff, __builtin_amdgcn_readfirstlane(lds + j * (AT::GROUP * 2)));
+    }
+  };
+  auto load_k = [&](const Half& x) { load(x, 0, p.ks[2], voff_k, kw); };
+  auto load_v = [&](const Half& x) { load(x, 2, p.vs[2], voff_v, vw); };
+
+  f32x16 acc[MT];
+#pragma unroll
+  for (int m = 0; m < MT; ++m) acc[m] = f32x16{};
+  float m_run = -INFINITY, l_run = 0.f;                    // log2 units
+  const float c2 = p.scale * kLog2e;
+  const int nh = 2 * nt;
+  int h = wave;
+  Half cur{};
+  if (h < nh) {
+    cur = half_at(h);
+    load_k(cur);
+    load_v(cur);
+  }
+  while (h < nh) {
+    const bool more = h + 4 < nh;
+    async_wait_but<NI>();                                  // K is there
+    f32x16 sc = f32x16{};
+#pragma unroll
+    for (int s = 0; s < KS; ++s) sc = mfma32(at.row(kw, 0, s), qreg[s], sc);
+    lds_wait();
+    Half nxt = cur;
+    if (more) {
+      nxt = half_at(h + 4);
+      load_k(nxt);
+    }
+    const bool whole = cur.n0 + 32 <= cur.end && cur.valid == 3u;
+    if (!whole || (!cur.prefix && cur.n0 + 31 > shift_keys)) {
+      const int seen = (cur.prefix ? cur.end - 1 : lim) - cur.n0 - 4 * lg;
+#pragma unroll
+      for (int r = 0; r < 16; ++r) {
+        const int last = cur.valid >> (r >> 3) & 1 ? seen : -1;
+        sc[r] = 8 * (r >> 2) + (r & 3) <= last ? sc[r] : -INFINITY;
+      }
+    }
+    float mx = -INFINITY;
+#pragma unroll
+    for (int r = 0; r < 16; ++r) mx = fmaxf(mx, sc[r]);
+    const float m_new = fmaxf(m_run, pair_max(mx) * c2);
+    if (__any(m_new > m_run + 8.f)) {
+      const float alpha = (m_run == -INFINITY) ? 0.f : fast_exp2(m_run - m_new);
+      l_run *= alpha;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) acc[m] *= alpha;
+      m_run = m_new;
+    }
+    const float m_use = (m_run == -INFINITY) ? 0.f : m_run;
+    u32x4 pop[2];
+    float w[16];
+#pragma unroll
+    for (int r = 0; r < 16; ++r) {
+      w[r] = fast_exp2(__builtin_fmaf(sc[r], c2, -m_use));
+      l_run += w[r];
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int x = 0; x < 4; ++x) pop[hf][x] = pack_bf16(w[8 * hf + 2 * x], w[8 * hf + 2 * x + 1]);
+    if (more) async_wait_but<NI>();                        // V is there
+    else async_wait();
+    if (!whole) {                                          // rows that are no key: 0 x NaN is NaN
+#pragma unroll
+      for (int j = 0; j < NI; ++j) {
+        const int n = cur.n0 + RPG * j + lane / CPR;
+        if (n >= cur.end || !(cur.valid >> (j * RPG / 16) & 1))
+          *reinterpret_cast<u32x4*>(vw + j * AT::GROUP + 8 * lane) = u32x4{0, 0, 0, 0};
+      }
+    }
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+      for (int mt = 0; mt < MT; ++mt) acc[mt] = mfma32(at.tr(vw, 16 * hf, mt), pop[hf], acc[mt]);
+    lds_wait();
+    if (more) load_v(nxt);
+    cur = nxt;
+    h += 4;
+  }
+
+  // Join the waves: each leaves its O in its own LDS, as 16-byte pieces [32-dim tile][piece]
+  // [lane]; wave w sums dims 32 w .. of all four.
+  const float l_tot = pair_sum(l_run);
+  float4* mine = reinterpret_cast<float4*>(kw);
+  static_assert(MT * 4 * 64 * 16 <= 2 * AT::ELEMS * 2, "a wave's O goes through its tiles' memory");
+  static_assert(4 * 2 * AT::ELEMS <= 4 * AsyncTile<D, 4>::ELEMS, "the waves' tiles fit the workgroup's stages");
+#pragma unroll
+  for (int mt = 0; mt < MT; ++mt)
+#pragma unroll
+    for (int a = 0; a < 4; ++a)
+      mine[(4 * mt + a) * 64 + lane] = float4{acc[mt][4 * a], acc[mt][4 * a + 1], acc[mt][4 * a + 2], acc[mt][4 * a + 3]};
+  if (lg == 0) {
+    xml[0][wave][lq] = m_run;
+    xml[1][wave][lq] = l_tot;
+  }
+  __syncthreads();
+  if (wave >= MT || lq >= nrows) return;
+  float M = -INFINITY, l = 0.f;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) M = fmaxf(M, xml[0][w][lq]);
+  float4 o[4] = {};
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    const float a = share_weight(xml[0][w][lq], M);
+    l = __builtin_fmaf(xml[1][w][lq], a, l);
+    const float4* from = reinterpret_cast<const float4*>(smem + w * 2 * AT::ELEMS);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const float4 x = from[(4 * wave + q) * 64 + lane];
+      o[q].x = __builtin_fmaf(x.x, a, o[q].x);
+      o[q].y = __builtin_fmaf(x.y, a, o[q].y);
+      o[q].z = __builtin_fmaf(x.z, a, o[q].z);
+      o[q].w = __builtin_fmaf(x.w, a, o[q].w);
+    }
+  }
+  if (p.parts > 1) {
+    const size_t at_part = (size_t)part * p.T * p.H + at_row;
+    float* dst = p.part_acc + at_part * D + 32 * wave + 4 * lg;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) *reinterpret_cast<float4*>(dst + 8 * q) = o[q];
+    if (wave == 0 && lg == 0) *reinterpret_cast<float2*>(p.part_ml + 2 * at_part) = float2{M, l};
+  } else {
+    const float inv = l == 0.f ? 0.f : 1.f / l;
+    uint16_t* dst = static_cast<uint16_t*>(p.o) + at_row * D + 32 * wave + 4 * lg;
+#pragma unroll
+    for (int q = 0; q < 4; ++q)
+      *reinterpret_cast<u32x2*>(dst + 8 * q) = u32x2{pack_bf16(o[q].x * inv, o[q].y * inv), pack_bf16(o[q].z * inv, o[q].w * inv)};
+    if (wave == 0 && lg == 0) p.lse[at_row] = l == 0.f ? -INFINITY : (M + __log2f(l)) * kLn2;
+  }
+}
+
+// Few: the call is of one token each with up to 32 heads to a K/V head, so that every
+// sequence's list, and a prefix's under a few sequences, is few_rows'.  Other calls have a
+// build without that loop: with it, and page numbers sixteen tiles at a time, prompts took
+// up to 6 % longer (12 x 200 tokens behind 8192 keys, H12 D64: 71.5 us against 67.2).
+template <int D, int NW, bool Few>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(2)))
 void paged_tiles_kernel(TilesParams p) {
   using AT = AsyncTile<D, NW>;
@@ -131,16 +342,18 @@ void paged_tiles_kernel(TilesParams p) {
     table += (size_t)b * p.max_pages;
     part = p.nsp + share;
   }
-  // A tile's page numbers come by a vector load, lane u that of unit u % 4 (and its rows'
-  // addresses are formed there: lanes 0 .. 3 hold K's units', lanes 4 .. 7 V's).
+  // Page numbers come by vector loads, lane l that of unit l % 4 (Few: the first 16 tiles'
+  // at once, lane l that of tile l / 4).
   const int lane_unit = lane & 3;
-  auto entry_of = [&](bool prefix, int n0) {
+  auto entry_of = [=](bool prefix, int n0) {
     const int* pages = prefix ? p.prefix_table : table;
     const int last = (prefix ? p.prefix_pages : p.max_pages) - 1;
     return pages[min((n0 + 16 * lane_unit) >> p.page_shift, last)];
   };
-  int e[3];
-  if (!p.joined) {   // apart, the first tiles' places do not depend on any length: one trip to memory less
+  int e[3], first16 = 0;
+  if constexpr (Few) {        // (never joined: that takes 1024 rows a sequence)
+    first16 = entry_of(prefix_list, BN * (share + (lane >> 2) * ns));
+  } else if (!p.joined) {     // apart, the first tiles' places do not depend on any length: one trip to memory less
 #pragma unroll
     for (int j = 0; j < 3; ++j) e[j] = entry_of(prefix_list, BN * (share + j * ns));
   }
@@ -180,24 +393,16 @@ void paged_tiles_kernel(TilesParams p) {
     return;
   }
 
-  const bool live = r0 + 32 * wave < nrows;                // (a wave without rows only copies)
-  const int lim = shift_keys + token;                      // the last own key that this lane's row sees
-  const int lim_wave = shift_keys + min(r0 + 32 * wave, nrows - 1) / G;   // the least of the wave's
-
   // ---- tiles
-  // (Page numbers are read two tiles ahead, on the way behind the copies that the loop
-  // waits for anyway.)
-  const bool lane_v = lane & 4;
-  const uint16_t* lane_base = static_cast<const uint16_t*>(lane_v ? p.v : p.k) + g * (lane_v ? p.vs[1] : p.ks[1]);
-  const long long lane_page = lane_v ? p.vs[0] : p.ks[0];
-  const uint32_t lane_place = (uint32_t)(lane_v ? p.vs[2] : p.ks[2]);
+  // The units' addresses are formed in lanes (0 .. 3: K's of a tile, 4 .. 7: V's) and handed
+  // out as scalars.
   struct Tile {
     int n0, end;          // its first key in the prefix or in the sequence, and where those end
     bool prefix;
     uint32_t valid;       // bit u: unit u has a page
     uint64_t base;        // lane u: K's unit u, lane 4 + u: V's
   };
-  auto place_of = [&](int i) {   // of the workgroup's i-th tile
+  auto place_of = [=](int i) {   // of the workgroup's i-th tile
     Tile t{};
     const int idx = share + i * ns;
     t.prefix = prefix_list || idx < tp;                    // (apart, no length has to be known for it)
@@ -205,6 +410,26 @@ void paged_tiles_kernel(TilesParams p) {
     t.end = t.prefix ? np : own;
     return t;
   };
+  if constexpr (Few) {
+    static_assert(NW == 4, "few_rows deals with four waves");
+    auto entries16 = [=](int i) {                          // of the workgroup's tiles i .. i + 15
+      const Tile t = place_of(i + (lane >> 2));
+      return entry_of(t.prefix, t.n0);
+    };
+    if (nrows <= 32) {   // (not the last rows of a longer list: those walk the tiles beside the others and share their reads)
+      few_rows<D>(p, smem, place_of, entries16, first16, nt, g, nrows, first, shift_keys, part, lane, wave);
+      return;
+    }
+  }
+
+  const bool live = r0 + 32 * wave < nrows;                // (a wave without rows only copies)
+  const int lim = shift_keys + token;                      // the last own key that this lane's row sees
+  const int lim_wave = shift_keys + min(r0 + 32 * wave, nrows - 1) / G;   // the least of the wave's
+
+  const bool lane_v = lane & 4;
+  const uint16_t* lane_base = static_cast<const uint16_t*>(lane_v ? p.v : p.k) + g * (lane_v ? p.vs[1] : p.ks[1]);
+  const long long lane_page = lane_v ? p.vs[0] : p.ks[0];
+  const uint32_t lane_place = (uint32_t)(lane_v ? p.vs[2] : p.ks[2]);
   auto settle = [&](Tile& t, int e) {
     const bool ok = (unsigned)e < (unsigned)p.num_pages;
     t.valid = (uint32_t)__ballot(ok) & 15u;
@@ -245,7 +470,10 @@ void paged_tiles_kernel(TilesParams p) {
   };
 
   Tile cur_t = place_of(0), nxt_t = place_of(1), far_t = place_of(2);
-  if (p.joined) {
+  if constexpr (Few) {
+#pragma unroll
+    for (int j = 0; j < 3; ++j) e[j] = __shfl(first16, 4 * j + lane_unit);
+  } else if (p.joined) {
     e[0] = entry_of(cur_t.prefix, cur_t.n0);
     e[1] = entry_of(nxt_t.prefix, nxt_t.n0);
     e[2] = entry_of(far_t.prefix, far_t.n0);
@@ -423,8 +651,7 @@ void paged_tiles_kernel(TilesParams p) {
 
 // Join the partials of rows (token, query head): D / 4 lanes hold a row's dims, GP groups
 // of lanes take every GP-th partial, 256 / (D / 4) / GP rows to a workgroup.  A partial of
-// a share without a visible key, (-inf, 0), has no O.  Scores that are all NaN leave -inf
-// and NaN: those are added, times 0, and stay NaN.
+// a share without a visible key, (-inf, 0), has no O.
 template <int D, int GP>
 __global__ __launch_bounds__(256) void tiles_join_kernel(TilesParams p) {
   constexpr int LPR = D / 4, NG = 256 / LPR, NR = NG / GP;
@@ -442,8 +669,7 @@ __global__ __launch_bounds__(256) void tiles_join_kernel(TilesParams p) {
   float M = -INFINITY, l = 0.f;
   float4 sum = {0.f, 0.f, 0.f, 0.f};
   auto fold = [&](const float2& ml, const float4& x) {
-    const float m = fmaxf(M, ml.x);
-    const float a = M == -INFINITY ? 0.f : fast_exp2(M - m), w = ml.x == -INFINITY ? 0.f : fast_exp2(ml.x - m);
+    const float m = fmaxf(M, ml.x), a = share_weight(M, m), w = share_weight(ml.x, m);
     sum.x = __builtin_fmaf(sum.x, a, x.x * w);
     sum.y = __builtin_fmaf(sum.y, a, x.y * w);
     sum.z = __builtin_fmaf(sum.z, a, x.z * w);
@@ -488,8 +714,9 @@ __global__ __launch_bounds__(256) void tiles_join_kernel(TilesParams p) {
 template <int D>
 static int launch_one(const TilesParams& p, int nw, hipStream_t st) {
   const dim3 grid((unsigned)((p.prefix_items + p.own_items) * p.Hkv));
-  if (nw == 8) hipLaunchKernelGGL((paged_tiles_kernel<D, 8>), grid, dim3(512), 0, st, p);
-  else hipLaunchKernelGGL((paged_tiles_kernel<D, 4>), grid, dim3(256), 0, st, p);
+  if (nw == 8) hipLaunchKernelGGL((paged_tiles_kernel<D, 8, false>), grid, dim3(512), 0, st, p);
+  else if (!p.starts && p.G <= 32) hipLaunchKernelGGL((paged_tiles_kernel<D, 4, true>), grid, dim3(256), 0, st, p);
+  else hipLaunchKernelGGL((paged_tiles_kernel<D, 4, false>), grid, dim3(256), 0, st, p);
   if (p.parts > 1) {
     const long long rows = (long long)p.T * p.H;
     constexpr int NG = 1024 / D;

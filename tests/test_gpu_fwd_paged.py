@@ -417,6 +417,94 @@ def test_longest_first(B, P):
         check(o[:, few], lse[:, few], refs, "decode")
 
 
+ONE = [
+    # own keys, H, Hkv, D, page, prefix
+    ([(37 * i) % 3000 for i in range(40)], 16, 16, 64, 16, 100),   # lists of 47 tiles, and none
+    ([5, 70], 2, 1, 64, 256, 131077),                              # a prefix's shares of 32 tiles
+    ([7], 32, 1, 128, 16, 5000),                                   # 32 rows behind the prefix
+    ([7, 9], 17, 1, 64, 16, 5000),                                 # 34 there, 17 of their own
+    ([33, 2000, 0], 64, 2, 128, 16, 40),                           # 32 heads a group
+    ([33, 2000, 0], 66, 2, 128, 16, 40),                           # 33
+    ([33, 2000, 0], 64, 2, 128, 32, 0),                            # no prefix
+    ([64 - i % 9 for i in range(130)], 8, 8, 128, 16, 0),          # one share of each list: nothing to join
+    ([31, 32, 33, 63, 64, 65, 1], 3, 1, 64, 16, 0),
+    ([95, 96, 97, 127, 128, 129, 130], 4, 4, 128, 64, 33),
+]
+
+
+@pytest.mark.parametrize("lens,H,Hkv,D,page,P", ONE, ids=lambda x: str(x)[:20].replace(" ", ""))
+def test_one_token_each(lens, H, Hkv, D, page, P):
+    """Up to 32 rows a list, and just more.  Places that hold no key are NaN; entries behind the lengths, and one in the middle
+    of a long list, name no page."""
+    need_gpu()
+    announce(f"one token each keys={lens[:5]} B={len(lens)} H={H}/{Hkv} D={D} page={page} P={P}")
+    g = torch.Generator().manual_seed(21 + len(lens) + P)
+    B = len(lens)
+    q, k, v, table, starts, prefix = setup([1] * B, lens, H, Hkv, D, page, P, g, wide=1)
+    kept = torch.zeros(k.shape[0], page, dtype=torch.bool)
+    for pages, n in [(table[b].cpu(), lens[b]) for b in range(B)] + ([(prefix.cpu(), P)] if P else []):
+        at = torch.arange(n)
+        kept[pages.long()[at // page], at % page] = True
+    for x in (k, v):
+        x.copy_(torch.where(kept[:, None, :, None], x.cpu(), torch.tensor(float("nan")).bfloat16()).cuda())
+    for b, n in enumerate(lens):
+        used = -(-n // page)
+        table[b, used:] = -7
+        if used > 2:
+            table[b, used // 2] = k.shape[0]
+    nbytes = api.attnfuse_fwd_paged_workspace_bytes(B, B, H, Hkv, D, table.shape[1] * page, len(prefix) * page if P else 0)
+    guard = torch.full((nbytes + 4096,), 0x5A, dtype=torch.uint8, device="cuda")
+
+    def call(ws):   # without starts, with a prefix or without: the entry below the public ones
+        return api._fwd_paged(q, k, v, table, None, i32(lens), prefix, i32([P]) if P else None, None, None, None, ws)
+
+    o, lse = call(guard[:nbytes] if nbytes else None)
+    torch.cuda.synchronize()
+    assert (guard[nbytes:] == 0x5A).all(), "written past the workspace"
+    check(o, lse, batch(q, k, v, table, starts, lens, prefix, P), "one token")
+    again = call(None)
+    assert torch.equal(again[0], o) and torch.equal(again[1], lse), "another call, other bits"
+
+
+def test_one_token_nan_and_large_scores():
+    """A NaN in a query or an own key is that row's alone; scores of thousands, of keys that different waves meet."""
+    need_gpu()
+    announce("one token NaN and large scores")
+    g = torch.Generator().manual_seed(22)
+    lens, P = [300, 20, 900], 3000
+    q, k, v, table, starts, prefix = setup([1] * 3, lens, 8, 2, 128, 16, P, g)
+    kw = dict(prefix_table=prefix, prefix_len=i32([P]))
+    q *= 30
+    k *= 30
+    o, lse = api.attnfuse_decode_paged(q, k, v, table, i32(lens), **kw)
+    check(o, lse, batch(q, k, v, table, starts, lens, prefix, P), "large")
+    q[1, 2, 5] = float("nan")
+    k[table[2, 40].long(), 1, 3, 7] = float("nan")
+    got, gl = api.attnfuse_decode_paged(q, k, v, table, i32(lens), **kw)
+    hit = torch.zeros(3, 8, dtype=torch.bool, device="cuda")
+    hit[1, 2] = hit[2, 4:] = True
+    assert got[hit].isnan().all() and gl[hit].isnan().all()
+    assert torch.equal(got[~hit], o[~hit]) and torch.equal(gl[~hit], lse[~hit])
+
+
+@pytest.mark.parametrize("n,D", [(1, 64), (1, 128), (30, 64), (30, 128), (300, 128)])
+def test_keys_and_values_laid_out_otherwise(n, D):
+    """K heads first, V places first, each a slice of wider pages: no stride of one is the other's."""
+    need_gpu()
+    announce(f"fwd_paged K and V of other strides n={n} D={D}")
+    g = torch.Generator().manual_seed(23)
+    Hkv, page, P, lens = 2, 32, 700, [n + 50, n]
+    q, k, v, table, starts, prefix = setup([n, n], lens, 8, Hkv, D, page, P, g)
+    pages = k.shape[0]
+    k = torch.randn(pages, Hkv + 1, page, D + 8, generator=g).bfloat16().cuda()[:, :Hkv, :, :D]
+    v = torch.randn(pages, page, Hkv + 3, D + 24, generator=g).bfloat16().cuda()[:, :, :Hkv, :D].transpose(1, 2)
+    kw = dict(prefix_table=prefix, prefix_len=i32([P]))
+    refs = batch(q, k, v, table, starts, lens, prefix, P)
+    check(*api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32(lens), **kw), refs, "prompts")
+    if n == 1:
+        check(*api.attnfuse_decode_paged(q, k, v, table, i32(lens), **kw), refs, "decode")
+
+
 def test_append_prompts_decode():
     """A server's run: a prefix of patches and text at positions of three axes is appended once, questions of some tokens are
     appended and attend, and then tokens one at a time."""
