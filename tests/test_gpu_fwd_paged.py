@@ -542,3 +542,38 @@ def test_append_prompts_decode():
         if step % 6 == 0:
             check(o, lse, batch(q, kc, vc, table, [0, 1, 2, 3], lens, prefix, P), f"token {step}")
     assert f64(o).isfinite().all()
+
+
+@pytest.mark.parametrize("n", [1 << 17, 1 << 20])
+@pytest.mark.parametrize("one", [True, False])
+def test_equal_weights_of_a_long_list_in_one_share(one, n):
+    """Four keys at the maximum, in the first tiles of every wave, and then n - 4 of one lower score, another in each row: the
+    roundings of a running sum of equal weights all go the same way.  Scores are products of two bf16 numbers, exact in fp32."""
+    need_gpu()
+    announce(f"fwd_paged equal weights n={n} one={one}")
+    g = torch.Generator().manual_seed(24)
+    B, H, D, page = 128, 8, 128, 256
+    assert api.attnfuse_fwd_paged_workspace_bytes(B, B, H, H, D, n) == 0, "more than one share"
+    q, k = torch.zeros(B, H, D, dtype=torch.bfloat16), torch.zeros(2, H, page, D, dtype=torch.bfloat16)
+    v = torch.randn(2, H, page, D, generator=g).bfloat16()
+    q[:, :, 0] = (1 + torch.rand(B, 1, generator=g)).bfloat16()
+    k[:, :, :, 0] = -(0.5 + 1.5 * torch.rand(H, generator=g)).bfloat16()[None, :, None]
+    first = torch.tensor([0, 32, 64, 96])
+    k[0, :, first] = 0
+    table = torch.ones(B, n // page, dtype=torch.int32)
+    table[:, 0] = 0
+    lens = torch.full((B,), n, dtype=torch.int32).cuda()
+    o, lse = api._fwd_paged(q.cuda(), k.cuda(), v.cuda(), table.cuda(), None if one else i32(list(range(B + 1))), lens, None, None,
+                            1.0, None, None, None)
+    low = f64(q[:, :, 0]) * f64(k[1, :, 0, 0])                       # [B, H]
+    w, x = low.exp(), f64(v)
+    rest = torch.ones(page, dtype=torch.bool)
+    rest[first] = False
+
+    def total(x):   # over the keys, of x [2, H, page, ...] times their weights
+        at = w.reshape(B, H, *(1,) * (x.dim() - 3))
+        return x[0][:, first].sum(1) + at * (x[0][:, rest].sum(1) + (n // page - 1) * x[1].sum(1))
+
+    s = total(torch.ones(2, H, page, dtype=torch.float64))
+    refs = [(slice(0, B), total(x) / s[..., None], s.log(), total(x.abs()) / s[..., None], -low)]
+    check(o, lse, refs, "equal weights")
