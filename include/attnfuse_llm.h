@@ -328,7 +328,10 @@ size_t attnfuse_fwd_paged_workspace_bytes(int T, int B, int H, int H_kv, int D, 
  *   workspace                     >= attnfuse_fwd_paged_workspace_bytes bytes,
  *                                 16-byte aligned; may be NULL where that is 0
  *   D in {64, 128}; B < 2^16, T <= 2^20, T * H <= 2^30; prefix_pages * page_size and
- *   max_pages * page_size <= 2^20; H <= 16384, a multiple of H_kv
+ *   max_pages * page_size <= 2^20; H <= 16384, a multiple of H_kv.  Sequences of fewer
+ *   than 1024 (token, head) pairs to a K/V head on average (T * H < 1024 * B * H_kv) take
+ *   at least a workgroup each, of which a launch has fewer than 2^24: T * H / 64 +
+ *   (B + 1) * H_kv < 2^24, and with a prefix T * H * D < 2^34 (else INVALID)
  *
  * A NaN in a query, or in a key or value that it sees, comes out as NaN.  A NaN or an
  * infinity in the value of one of the sequence's newest n_b own keys may reach queries of

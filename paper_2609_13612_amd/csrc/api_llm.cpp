@@ -447,6 +447,10 @@ struct TilesLayout {
 // Joined where the rows of a sequence fill eight waves (3500 tokens of 6 sequences behind
 // 32768: 1890, apart in four waves 2020); four waves at D 64 otherwise (1630 tokens of 12
 // behind 8192: 69, in eight 76).
+// (HIP: fewer than 2^32 threads in a dimension of a grid)
+bool launches(long long workgroups, int threads) { return workgroups * threads < (1LL << 32); }
+bool tiles_join_launches(long long rows, int D) { return launches((rows * D + 1023) / 1024, 256); }   // (paged_tiles.hip)
+
 TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, int P, int D) {
   TilesLayout L{};
   const int G = H / H_kv;
@@ -472,12 +476,13 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
     const float slots = nw == 8 ? 256.f : 512.f, narrow = D == 64 ? 0.6f : 1.f, pair = (nw == 8 ? 1.75f : 2.f) * narrow;
     const float beside_p = few_o && !few_p ? 0.5f * read_o / flat : 0.f;   // what few rows' lists read before the prefix's go on
     const float units_o = (float)(lists * H_kv), units_p = (float)(flat * H_kv);
+    if (!launches((lists + (apart ? flat : 0)) * H_kv, 64 * nw)) continue;    // (four waves, or many: tiles_sizes has seen to it)
     for (const int no : kShares) {
-      if (no > 1 && (no > tiles_o || (apart && tiles_o / no < 4))) break;
+      if (no > 1 && (no > tiles_o || (apart && tiles_o / no < 4) || !tiles_join_launches((long long)T * H, D))) break;
       const float all_o = units_o * no;
       for (const int n : kShares) {
         if (n > 1 && (!apart || n > tiles_p)) break;
-        if ((n > 1 || no > 1) && all_o + units_p * n > 1e6f) break;   // (nothing to gain, and grids stay inside their type)
+        if ((n > 1 || no > 1) && all_o + units_p * n > 1e6f) break;   // (nothing to gain, and few enough to launch)
         // (a workgroup of four waves alone on its CU, or beside short lists, is done with a tile sooner)
         const float alone = nw == 4 && (few ? 0.f : all_o) + (apart ? units_p * n : 0.f) <= 256.f ? 0.75f : 1.f, tile = alone * pair;
         const float one_o = (tiles_o + no - 1) / no * (few_o ? 0.55f * narrow : tile) + (few_o ? 6.5f : 5.f);
@@ -516,9 +521,13 @@ TilesLayout tiles_layout(int T, int B, bool one_each, int H, int H_kv, int S, in
 }
 
 bool tiles_sizes(int T, int B, int H, int H_kv, long long S, long long P, int D) {
-  return T >= 1 && T <= kMaxS && B >= 1 && B < (1 << 16) && H >= 1 && H <= kMaxHeads && H_kv >= 1 && H % H_kv == 0 && S >= 1 &&
-         S <= kMaxS && P >= 0 && P <= kMaxS && D >= 2 && D % 2 == 0 && (long long)T * H <= (1 << 30) &&
-         2 * ((long long)T * (H / H_kv) / 128 + B + 1) * H_kv < (1LL << 31);   // workgroups, with one share of each list
+  if (!(T >= 1 && T <= kMaxS && B >= 1 && B < (1 << 16) && H >= 1 && H <= kMaxHeads && H_kv >= 1 && H % H_kv == 0 && S >= 1 &&
+        S <= kMaxS && P >= 0 && P <= kMaxS && D >= 2 && D % 2 == 0 && (long long)T * H <= (1 << 30)))
+    return false;
+  // What one share of each list launches.  Many rows a sequence: at most 2^30 / 256 tiles of eight waves and 2^30 / 1024 sequences.
+  const long long rows = (long long)T * (H / H_kv);
+  return rows >= 1024LL * B ||
+         (launches(2 * (rows / 128) * H_kv + (B + 1LL) * H_kv, 256) && (P == 0 || tiles_join_launches((long long)T * H, D)));
 }
 
 }  // namespace

@@ -735,10 +735,11 @@ static int launch_one(const TilesParams& p, int nw, hipStream_t st) {
   if (nw == 8) hipLaunchKernelGGL((paged_tiles_kernel<D, 8, false>), grid, dim3(512), 0, st, p);
   else if (!p.starts && p.G <= 32) hipLaunchKernelGGL((paged_tiles_kernel<D, 4, true>), grid, dim3(256), 0, st, p);
   else hipLaunchKernelGGL((paged_tiles_kernel<D, 4, false>), grid, dim3(256), 0, st, p);
+  if (hipGetLastError() != hipSuccess) return -3;   // (no join of what is not there)
   if (p.parts > 1) {
     const long long rows = (long long)p.T * p.H;
     constexpr int NG = 1024 / D;
-    if (p.parts >= 8) hipLaunchKernelGGL((tiles_join_kernel<D, NG>), dim3((unsigned)rows), dim3(256), 0, st, p);
+    if (p.parts >= 8 && rows < (1 << 24)) hipLaunchKernelGGL((tiles_join_kernel<D, NG>), dim3((unsigned)rows), dim3(256), 0, st, p);
     else hipLaunchKernelGGL((tiles_join_kernel<D, 1>), dim3((unsigned)((rows + NG - 1) / NG)), dim3(256), 0, st, p);
   }
   return hipGetLastError() == hipSuccess ? 0 : -3;

@@ -58,3 +58,28 @@ def test_python_refuses():
         api.attnfuse_decode_paged(q, kv, kv, table, prefix_len=table[0])
     with pytest.raises(ValueError, match="rotated"):
         api.attnfuse_decode_paged(q, kv, kv, table, prefix_table=table[0], rope="neox")
+
+
+# A launch has fewer than 2^32 threads: fewer than 2^24 workgroups of 256, or 2^23 of 512, and as many rows of partials to join
+# as 2^32 threads have, D / 4 a row.
+TOO_MANY = [
+    dict(T=65535, B=65535, H=512, H_kv=512),                                # a workgroup for each sequence and K/V head
+    dict(T=65535, B=65535, H=512, H_kv=512, starts=None),
+    dict(T=65535, B=65535, H=512, H_kv=512, ahead=0, prefix=None, plen=None),
+    dict(T=1 << 20, B=65535, H=128, H_kv=8, D=128, kps=128, vps=128),       # 2^27 rows of at least two partials
+    dict(T=1 << 20, B=65535, H=256, H_kv=8, D=64),
+]
+
+
+@pytest.mark.parametrize("over", TOO_MANY, ids=str)
+def test_what_cannot_be_launched_is_refused(over):
+    assert call("attnfuse_fwd_paged", PAGED, over) == INVALID
+    a = {**PAGED, **over}
+    assert _lib.load().attnfuse_fwd_paged_workspace_bytes(a["T"], a["B"], a["H"], a["H_kv"], a["D"], a["most"] * a["page"],
+                                                          a["ahead"] * a["page"]) == 0
+
+
+def test_the_largest_launches_are_not_refused():
+    f = _lib.load().attnfuse_fwd_paged_workspace_bytes
+    assert f((1 << 20) - 1, 65535, 128, 8, 128, 64, 32) > 0 and f((1 << 20) - 1, 65535, 256, 8, 64, 64, 32) > 0
+    assert f(65535, 65535, 250, 250, 128, 64, 32) > 0    # (four waves: eight would be too many threads)
