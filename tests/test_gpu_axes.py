@@ -407,3 +407,13 @@ def test_on_another_stream():
         got = api.attnfuse_qknorm_rope(x, **cfg)[0]
     s.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "fp32"])
+@pytest.mark.parametrize("order", ["blocks", "turns"])
+@pytest.mark.parametrize("rope", ["neox", "interleaved"])
+@pytest.mark.parametrize("D,sections", [(64, (8, 12, 12)), (64, (8, 8, 8, 8)), (128, (16, 24, 24))],
+                         ids=lambda x: str(x).replace(" ", ""))
+def test_append_every_pair_of_many_tokens(monkeypatch, D, sections, rope, order, dtype):
+    """The same where there are workgroups enough for a thread to take several heads: builds of their own."""
+    test_append(monkeypatch, 4500, 32, 8, D, 32, dtype, rope, "rows", True, sections, order, "own", "phsd", True)
