@@ -577,3 +577,23 @@ def test_equal_weights_of_a_long_list_in_one_share(one, n):
     s = total(torch.ones(2, H, page, dtype=torch.float64))
     refs = [(slice(0, B), total(x) / s[..., None], s.log(), total(x.abs()) / s[..., None], -low)]
     check(o, lse, refs, "equal weights")
+
+
+@pytest.mark.parametrize("D", [64, 128])
+@pytest.mark.parametrize("counts,lens", [([40, 200, 130, 260], [1500, 200, 700, 700]), ([0, 700], [2000, 1000]),
+                                         ([300, 1, 150, 150, 150, 90], [300, 5000, 1000, 150, 1000, -3])],
+                         ids=lambda x: str(x).replace(" ", ""))
+def test_joined_and_longest_first(counts, lens, D):
+    """Rows enough to walk the prefix's tiles and then their own, in more workgroups than run at once: by length, which is another
+    order than that of the sequences and of their numbers of rows, ties and a sequence without queries or keys among them."""
+    need_gpu()
+    announce(f"fwd_paged joined, longest first {counts} {lens} D={D}")
+    g = torch.Generator().manual_seed(25 + len(counts))
+    H, Hkv, P, page = 128, 16, 333, 16
+    q, k, v, table, starts, prefix = setup(counts, lens, H, Hkv, D, page, P, g, pad=3)
+    kw = dict(prefix_table=prefix, prefix_len=i32([P]))
+    o, lse = api.attnfuse_fwd_paged(q, k, v, table, i32(starts), i32(lens), **kw)
+    for j in (0, Hkv - 1):   # the reference of two K/V heads
+        h = slice(j * H // Hkv, (j + 1) * H // Hkv)
+        refs = batch(q[:, h], k[:, j:j + 1], v[:, j:j + 1], table, starts, lens, prefix, P)
+        check(o[:, h], lse[:, h], refs, f"K/V head {j}")
