@@ -140,6 +140,8 @@ def rope_table(D, theta, rows, device=None, out=None, *, sections=None, section_
     same D and theta and S <= rows.  With ``sections`` and frequencies="own" it is
     that of positions of several axes, each with its own ladder of frequencies
     (attnfuse_axes_table_fill), for calls with the same sections in the same order."""
+    if sections is not None:
+        sections, section_order = _sections(sections, section_order, frequencies, D)
     device = torch.device("cuda", torch.cuda.current_device()) if device is None else torch.device(device)
     shape = (rows, D // 2, 2)
     if out is None:
@@ -624,20 +626,26 @@ def _position_table(rope, theta, D, n, device, positions, shape, max_positions, 
     return _table(rope, theta, D, int(max_positions), device, rope_table)[:int(max_positions)]
 
 
+def _sections(sections, section_order, frequencies, D):
+    """Sections, checked, as a tuple of whole numbers, and their order."""
+    given, sections = sections, tuple(int(n) for n in sections)
+    if section_order not in SECTION_ORDER or frequencies not in FREQUENCIES:
+        raise ValueError("section_order is 'blocks' or 'turns', frequencies 'shared' or 'own'")
+    if not 1 <= len(sections) <= 4 or min(sections) < 1 or 2 * sum(sections) != D or any(a != b for a, b in zip(sections, given)):
+        raise ValueError(f"sections must be one to four whole numbers of pairs, {D // 2} in all (they are {given})")
+    return sections, section_order
+
+
 def _axes(sections, section_order, frequencies, norm, rope, D, positions):
     """The sections of positions of several axes, as a tuple, and their order; None without any."""
     if sections is None:
         if not norm:
             raise ValueError("norm=False needs sections (one axis: sections=(D // 2,) and positions [1, ...])")
         return None
-    sections = tuple(int(n) for n in sections)
-    if section_order not in SECTION_ORDER or frequencies not in FREQUENCIES:
-        raise ValueError("section_order is 'blocks' or 'turns', frequencies 'shared' or 'own'")
-    if not 1 <= len(sections) <= 4 or min(sections) < 1 or 2 * sum(sections) != D:
-        raise ValueError(f"sections must be one to four numbers of pairs, {D // 2} in all (they are {sections})")
+    axes = _sections(sections, section_order, frequencies, D)
     if rope not in ("neox", "interleaved") or positions is None:
         raise ValueError("sections need positions and rope='neox' or 'interleaved'")
-    return sections, section_order
+    return axes
 
 
 def _axes_table(axes, frequencies, rope, theta, D, device, max_positions, rope_table):

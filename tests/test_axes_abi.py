@@ -90,3 +90,17 @@ def test_python_refuses():
         with pytest.raises(ValueError, match="GPU"):
             f(*([q] * (6 if f is api.attnfuse_qknorm_rope_append else 4)), sections=(16, 16), positions=pos, max_positions=4)
     assert "attnfuse_qknorm_axes" in _lib.LLM_SIGNATURES
+
+
+def test_sections_are_whole_numbers():
+    pos = torch.zeros(2, 1, 4, dtype=torch.int32)
+    assert api._axes((16.0, 16), "blocks", "shared", True, "neox", 64, pos) == ((16, 16), "blocks")
+    with pytest.raises(ValueError, match="whole"):
+        api._axes((16.5, 16.5), "blocks", "shared", True, "neox", 64, pos)   # (not taken as 16, 16)
+
+
+@pytest.mark.parametrize("bad", [dict(sections=(16.5, 16.5)), dict(sections=(16, 17)), dict(sections=()),
+                                 dict(sections=(16, 16), section_order="rows"), dict(sections=(16, 16), frequencies="mine")], ids=str)
+def test_a_table_checks_its_sections_as_the_calls_do(bad):
+    with pytest.raises(ValueError, match="section"):
+        api.rope_table(64, 1e4, 8, "cuda:0", **bad)
