@@ -338,7 +338,8 @@ size_t attnfuse_fwd_paged_workspace_bytes(int T, int B, int H, int H_kv, int D, 
  * the call that do not see it yet (with weight 0); what lies in places past a sequence's
  * length or the prefix's, and in pages of neither, is never used.  The keys are shared out by sizes alone (T, B and the tables' widths)
  * and the same call gives the same bits; in another batch a sequence's result is the same to
- * the rounding of its weights and sums.
+ * the rounding of its weights and sums.  Tables much wider than the keys they hold, and many
+ * tokens of no sequence, are shared out as if they were full, which costs time.
  */
 int attnfuse_fwd_paged(const void* Q, const void* K_pages, const void* V_pages, const int* block_table, const int* q_starts,
                        const int* cache_lens, const int* prefix_table, const int* prefix_len, void* O, float* LSE,

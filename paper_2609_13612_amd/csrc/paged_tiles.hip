@@ -29,11 +29,12 @@
 // What lies in places that are no key of any row of the workgroup may be anything: scores
 // are replaced and rows of V cleared in LDS after they landed.
 //
-// Bound by reading K and V where few rows meet them, by the matrix units from about 220
-// rows of a K/V head on.  Measured (D 128): 32 sequences' tokens behind 32768 shared keys,
-// own keys to 1024, H 32 of 8, 57 to 58 us, of which the join 7: 218 MB, 4.3 TB/s in the
-// first kernel.  3500 tokens of 6
-// sequences behind 32768: 1913 us, 1.02 PFLOP/s, 85 % of a large library product's rate; a
+// Bound by reading K and V where few rows meet them, from about 220 rows of a K/V head on by the
+// products and the softmax between them.  Measured (D 128): 32 sequences' tokens behind 32768 shared
+// keys, own keys to 1024, H 32 of 8, 57 to 58 us, of which the join 7: 224 MB, 4.5 TB/s in the
+// first kernel.  3500 tokens of 6 sequences behind 32768: 1906 to 1999 us, 1.0 PFLOP/s, 81 to 85 % of a
+// large library product's rate, matrix units busy 44 % of the cycles, 6.4 vector instructions to one of
+// theirs, a third of the waves' time waiting; a
 // tile of a workgroup of eight waves takes 1.75 us, of four waves, two of them on a CU, 1.9.
 // Copies three tiles ahead instead of one (four stages, 32- or 64-key tiles) were nowhere
 // faster: 1904 to 2120 us, and 60 to 140 for the first.
